@@ -46,7 +46,7 @@ typedef enum {
                          step committed nothing, length and pending are as before the call     */
 } pv_status;
 
-typedef enum { PV_F32 = 0, PV_BF16 = 1 } pv_dtype;
+typedef enum { PV_F32 = 0, PV_BF16 = 1, PV_F16 = 2 } pv_dtype;      /* PV_F16: the operators below; no model is stored in it */
 
 /* Tensor kinds for pv_load_weights.  Matrices are [out][in]; norm gains are [1][d_model]. */
 typedef enum {
@@ -280,6 +280,61 @@ int pv_step_bytes(const pv_cache *c, int32_t gamma, uint64_t *bytes);
  * on the caller's stream afterwards.  enable = 0 switches to plain launches, for comparison and
  * for callers that capture the step into a graph of their own.  Results are identical. */
 int pv_cache_use_graphs(pv_cache *c, int32_t enable);
+
+/* ---- operators around a key/value cache in 8 bits ----
+ *
+ * The kernels that the steps of a cache with 8-bit keys and values run (pv_cache_create_kv), on the caller's own tensors: a program
+ * with a decoder of its own keeps its cache in the same form.  All pointers are device memory; nothing is allocated,
+ * synchronised or kept, so the calls may be captured into graphs (tables, lengths and data are read when they run).
+ *
+ * The cache: codes in e4m3 (four significant bits, steps of 2^-9 below 2^-6, largest 448, 0x7F and 0xFF are NaN, no infinity), and one power of two for
+ * the keys and one for the values of each block of 16 tokens of a head: a byte b stands for 2^(b - 127), 1 <= b <= 253 (0 is taken for 1, 254 and
+ * 255 for 253); value = code * scale.
+ *   codes  [n_pages][n_kv_heads][2 (K, V)][page_tokens / 16][16 * head_dim] bytes, 16-byte aligned; inside a block
+ *          K [head_dim / 16][token][16 features],  V [head_dim / 64][token / 4][feature % 16][feature / 16 % 4][token % 4]
+ *   scales [n_pages][n_kv_heads][page_tokens / 16][2 (K, V)] bytes, 2-byte aligned
+ * head_dim is 64 or 128, page_tokens a power of two from 16 to 65536.  Neither array has to be cleared before use. */
+typedef struct {
+    void *codes, *scales;
+    int32_t n_pages, n_kv_heads, head_dim, page_tokens;
+} pv_kv8_pool;
+
+/* A ragged batch: sequence s has rows row_start[s] .. row_start[s + 1] - 1 of the call's n_rows rows, at positions prefix_len[s] ... of its
+ * tokens; page_table[s][i] is the physical page of its tokens i * page_tokens ....  Device arrays of n_seq + 1, n_seq and n_seq * table_pages entries.
+ * What they hold is not known to the host: a row that belongs to no sequence (behind the last one, too) is left out, a
+ * sequence with a negative length has no rows, and a position behind the table's end or in a page outside [0, n_pages) does not exist: it is not
+ * written, reads as zeros and no row attends to it.  Limits: n_seq <= 2^20, n_rows <= 2^24. */
+typedef struct {
+    const int32_t *row_start, *prefix_len, *page_table;
+    int32_t n_seq, n_rows, table_pages;
+} pv_kv8_seqs;
+
+/* Bytes of a pool's two arrays. */
+int pv_kv8_bytes(const pv_kv8_pool *pool, size_t *codes_bytes, size_t *scales_bytes);
+
+/* Quantise keys and values as they are written: row i of sequence s becomes token prefix_len[s] + i of it.  The scale of a block is the smallest power of two (from
+ * 2^-100 on) that leaves no code above 448; a block that holds earlier tokens (positions below prefix_len) keeps its scale, or, if a new token needs a larger one, has their codes
+ * rounded to that.  Codes are rounded to nearest, ties to the even code; what is not finite becomes NaN and has no say in the scale.  k, v: element (row, head, feature) at
+ * row * row_stride + head * head_stride + feature, of type dtype (pv_dtype); addresses and strides multiples of 16 bytes.  A page must not be
+ * the place of rows of two sequences of a call. */
+int pv_kv8_append(const pv_kv8_pool *pool, const pv_kv8_seqs *seqs, const void *k, int64_t k_row_stride, int64_t k_head_stride,
+                  const void *v, int64_t v_row_stride, int64_t v_head_stride, int32_t dtype, void *hip_stream);
+
+/* Read tokens back: row i of sequence s receives token prefix_len[s] + i (value = code * scale, rounded to dtype).  Same addressing. */
+int pv_kv8_read(const pv_kv8_pool *pool, const pv_kv8_seqs *seqs, void *k, int64_t k_row_stride, int64_t k_head_stride,
+                void *v, int64_t v_row_stride, int64_t v_head_stride, int32_t dtype, void *hip_stream);
+
+/* Attention of every row over the cache: out = softmax(scale * q K^T) V, query head a over kv head a / (n_q_heads / n_kv_heads).  The keys and values of the call's own rows are in the
+ * cache already (pv_kv8_append with the same tables).  mask == NULL: row i of sequence s sees tokens 0 .. prefix_len[s] + i.  Else (a draft tree) mask[row] has bit t set
+ * if the row sees token prefix_len[s] + t, and every row sees all tokens before prefix_len[s], none from prefix_len[s] + 64 on.  A row that sees no token: zeros, and -infinity in lse.  What a row does
+ * not see has no influence on it, NaN included.  q, out: PV_BF16 or PV_F16, addressed as above (out may be q); lse: NULL, or float [n_rows][n_q_heads],
+ * log(sum(exp(scale * q K^T))).  n_q_heads is a multiple of n_kv_heads, (n_rows + n_seq) * n_q_heads <= 2^24,
+ * table_pages * page_tokens <= 2^30, scale is finite.  workspace: at least
+ * pv_kv8_attention_bytes, 16-byte aligned, for this call alone until it has run. */
+int pv_kv8_attention_bytes(const pv_kv8_pool *pool, const pv_kv8_seqs *seqs, int32_t n_q_heads, size_t *bytes);
+int pv_kv8_attention(const pv_kv8_pool *pool, const pv_kv8_seqs *seqs, const void *q, int64_t q_row_stride, int64_t q_head_stride, int32_t n_q_heads,
+                     const uint64_t *mask, float scale, void *out, int64_t out_row_stride, int64_t out_head_stride, float *lse, int32_t dtype,
+                     void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* ---- instrumentation ---- */
 

@@ -29,12 +29,23 @@ class pv_model_config(ctypes.Structure):
                [(n, ctypes.c_int32) for n in ("dtype", "page_tokens", "max_gamma", "kernel_path", "weight_bits")]
 
 
+class pv_kv8_pool(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("codes", "scales")] + \
+               [(n, ctypes.c_int32) for n in ("n_pages", "n_kv_heads", "head_dim", "page_tokens")]
+
+
+class pv_kv8_seqs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("row_start", "prefix_len", "page_table")] + \
+               [(n, ctypes.c_int32) for n in ("n_seq", "n_rows", "table_pages")]
+
+
 EXPORTS = [
     "pv_model_bytes", "pv_prompt_bytes", "pv_cache_bytes", "pv_model_create", "pv_model_destroy", "pv_load_weights",
     "pv_cache_create", "pv_cache_destroy", "pv_cache_set_page_table", "pv_prefill", "pv_verify",
     "pv_verify_async", "pv_verify_wait", "pv_rollback", "pv_cache_len", "pv_cache_set_pending",
     "pv_debug_logits", "pv_debug_pred", "pv_cache_export", "pv_step_bytes", "pv_strerror", "pv_last_error",
     "pv_profile_select", "pv_profile_read", "pv_cache_readmit", "pv_calib_copy", "pv_calib_read", "pv_verify_async_static", "pv_verify_batch", "pv_verify_tree", "pv_cache_use_graphs", "pv_load_weights_q4",
+    "pv_kv8_bytes", "pv_kv8_append", "pv_kv8_read", "pv_kv8_attention_bytes", "pv_kv8_attention",
 ]
 
 _lib = None
@@ -80,6 +91,13 @@ def lib():
         L.pv_calib_copy.argtypes = [vp, vp, ctypes.c_size_t, vp]
         L.pv_calib_read.argtypes = [vp, ctypes.c_size_t, vp, vp]
         L.pv_cache_use_graphs.argtypes = [vp, i32]
+        poolp, seqsp = P(pv_kv8_pool), P(pv_kv8_seqs)
+        rows = [vp, i64, i64]                              # address, row stride, head stride
+        L.pv_kv8_bytes.argtypes = [poolp, P(sz), P(sz)]
+        L.pv_kv8_append.argtypes = [poolp, seqsp, *rows, *rows, i32, vp]
+        L.pv_kv8_read.argtypes = [poolp, seqsp, *rows, *rows, i32, vp]
+        L.pv_kv8_attention_bytes.argtypes = [poolp, seqsp, i32, P(sz)]
+        L.pv_kv8_attention.argtypes = [poolp, seqsp, *rows, i32, vp, ctypes.c_float, *rows, vp, i32, vp, sz, vp]
         L.pv_strerror.argtypes = [ctypes.c_int]; L.pv_strerror.restype = ctypes.c_char_p
         L.pv_last_error.argtypes = []; L.pv_last_error.restype = ctypes.c_char_p
         _lib = L
