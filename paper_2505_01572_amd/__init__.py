@@ -7,4 +7,4 @@ for device memory and streams.
 from .binding import (  # noqa: F401
     PVError, lib, Model, Cache, KINDS, PV_F32, PV_BF16, PATH_AUTO, PATH_VECTOR, PATH_MATRIX, PROF, calib_copy, calib_read, verify_batch,
 )
-from .operators import KV8Pool, KV8Seqs  # noqa: F401
+from .operators import KV8Pool, KV8Seqs, TokenLogprobs, token_logprobs  # noqa: F401

@@ -45,7 +45,7 @@ EXPORTS = [
     "pv_verify_async", "pv_verify_wait", "pv_rollback", "pv_cache_len", "pv_cache_set_pending",
     "pv_debug_logits", "pv_debug_pred", "pv_cache_export", "pv_step_bytes", "pv_strerror", "pv_last_error",
     "pv_profile_select", "pv_profile_read", "pv_cache_readmit", "pv_calib_copy", "pv_calib_read", "pv_verify_async_static", "pv_verify_batch", "pv_verify_tree", "pv_cache_use_graphs", "pv_load_weights_q4",
-    "pv_kv8_bytes", "pv_kv8_append", "pv_kv8_read", "pv_kv8_attention_bytes", "pv_kv8_attention",
+    "pv_kv8_bytes", "pv_kv8_append", "pv_kv8_read", "pv_kv8_attention_bytes", "pv_kv8_attention", "pv_token_logprobs_bytes", "pv_token_logprobs",
 ]
 
 _lib = None
@@ -98,6 +98,8 @@ def lib():
         L.pv_kv8_read.argtypes = [poolp, seqsp, *rows, *rows, i32, vp]
         L.pv_kv8_attention_bytes.argtypes = [poolp, seqsp, i32, P(sz)]
         L.pv_kv8_attention.argtypes = [poolp, seqsp, *rows, i32, vp, ctypes.c_float, *rows, vp, i32, vp, sz, vp]
+        L.pv_token_logprobs_bytes.argtypes = [i64, i32, i32, P(sz)]
+        L.pv_token_logprobs.argtypes = [vp, i64, i32, i64, i32, vp, i32, vp, vp, vp, i32, vp, vp, vp, sz, vp]
         L.pv_strerror.argtypes = [ctypes.c_int]; L.pv_strerror.restype = ctypes.c_char_p
         L.pv_last_error.argtypes = []; L.pv_last_error.restype = ctypes.c_char_p
         _lib = L

@@ -1,13 +1,15 @@
-"""The operators of an 8-bit key/value cache on the caller's own tensors (include/pipeverify.h, "operators around a key/value cache in 8 bits").
+"""Operators on the caller's own tensors (include/pipeverify.h, "operators around a key/value cache in 8 bits" and pv_token_logprobs).
 
     pool = pv.KV8Pool(n_pages, n_kv_heads, head_dim)                  # pages shared by all sequences (one pool a layer)
     seqs = pv.KV8Seqs(row_start, prefix_len, page_table)              # int32 tensors on the device, read when the kernels run
     pool.append(seqs, k, v)                                           # quantise the rows' keys and values into the pages
     out = pool.attention(seqs, q)                                     # every row over its sequence's prefix and its block
+    got = pv.token_logprobs(logits, tokens, top=5)                    # log probabilities, entropy, alternatives
 
 Argument marshalling only; work is enqueued on `stream` (default: the current stream of the pool's device) and not waited for.  A tensor made on another stream
 is the caller's to order, as everywhere in torch.
 """
+import collections
 import ctypes
 import math
 
@@ -146,3 +148,30 @@ class KV8Pool:
             _check(self.L.pv_kv8_attention(pa, sa, *qa, heads, None if mask is None else mask.data_ptr(), scale, *oa, None if lse is None else lse.data_ptr(),
                                            _DTYPES[q.dtype], None if ws is None else ws.data_ptr(), need.value, s), "pv_kv8_attention")
         return (out, lse) if lse is not None else out
+
+
+TokenLogprobs = collections.namedtuple("TokenLogprobs", "logprobs entropy lse top_ids top_logprobs")
+
+
+def token_logprobs(logits, tokens=None, top=0, stream=None):
+    """Log probabilities under each row of logits [rows, vocab] (float32, bfloat16 or float16): of tokens (int32 [rows, n] or [rows]), and of the `top` <= 32 most
+    probable ones (equal ones: the lower id first), with the row's entropy and log-sum-exp.  float32, in nats; a NaN logit counts as -infinity."""
+    where = "token_logprobs"
+    _need(isinstance(logits, torch.Tensor) and logits.is_cuda and logits.dim() == 2 and logits.dtype in _DTYPES, where, f"logits must be [rows, vocab] of {tuple(_DTYPES)} on the GPU")
+    rows, vocab = logits.shape
+    _need(logits.stride(1) == 1 or vocab <= 1 or rows == 0, where, "the logits of a row must lie next to each other")
+    d = logits.device
+    if tokens is not None:
+        _on(tokens, d, where, "tokens")
+        _need(tokens.dtype == torch.int32 and tokens.dim() in (1, 2) and tokens.shape[0] == rows and tokens.is_contiguous(), where, f"tokens must be a contiguous int32 tensor [{rows}] or [{rows}, n]")
+    n = 0 if tokens is None else tokens.numel() // max(1, rows)
+    L, need = lib(), ctypes.c_size_t()
+    _check(L.pv_token_logprobs_bytes(rows, vocab, top, ctypes.byref(need)), "pv_token_logprobs_bytes")
+    with _Stream(d, stream) as s:
+        f = lambda *shape: torch.empty(*shape, dtype=torch.float32, device=d)  # noqa: E731
+        got = TokenLogprobs(f(*(tokens.shape if tokens is not None else (rows, 0))), f(rows), f(rows), torch.empty(rows, top, dtype=torch.int32, device=d), f(rows, top))
+        ws = torch.empty(need.value, dtype=torch.uint8, device=d) if need.value else None
+        p = lambda t: None if t is None or t.numel() == 0 else t.data_ptr()  # noqa: E731
+        _check(L.pv_token_logprobs(logits.data_ptr(), logits.stride(0), _DTYPES[logits.dtype], rows, vocab, p(tokens), n, p(got.logprobs), p(got.entropy), p(got.lse),
+                                   top, p(got.top_ids), p(got.top_logprobs), p(ws), need.value, s), "pv_token_logprobs")
+    return got

@@ -1,4 +1,4 @@
-"""No kernel of the 8-bit cache's operators may spill registers to scratch memory (compiles the device code to assembly, no GPU needed)."""
+"""No kernel of the operators may spill registers to scratch memory (compiles the device code to assembly, no GPU needed)."""
 import re
 
 import pytest
@@ -6,7 +6,7 @@ import pytest
 from test_no_spills import _kernels
 
 
-@pytest.mark.parametrize("src", ["pv_kernels_kv8.hip", "pv_kernels_kv8_attention.hip"])
+@pytest.mark.parametrize("src", ["pv_kernels_kv8.hip", "pv_kernels_kv8_attention.hip", "pv_kernels_logprobs.hip"])
 def test_kernels_use_no_scratch(src):
     kernels = _kernels(src)
     assert kernels, "no kernel descriptors found"
