@@ -149,6 +149,14 @@ int pv_cache_create(const pv_model *m, void *d_page_pool, size_t page_pool_bytes
                     void *d_workspace, size_t workspace_bytes, int32_t max_tokens, pv_cache **out);
 void pv_cache_destroy(pv_cache *c);
 
+/* The same with keys and values in 8 bits (kv_bits = 8; 0: the model's storage type, which is what the two calls above give): half the memory and half of what a step reads of
+ * them, e4m3 codes with a power-of-two scale for 16 tokens and head (the form is described at pv_kv8_pool below).  Keys and values are rounded to four significant bits when they are stored, and every row, also of
+ * the block that brings them, attends to them as stored.  bf16 models with head_dim 64 or 128.  All calls on a cache work alike; the caches of a batch store alike.
+ * The page pool is the layers' codes ([n_layers] pools' codes), and behind them, rounded up to 256 bytes, their scales.  pv_cache_export gives the stored values (bf16, exact). */
+int pv_cache_bytes_kv(const pv_model *m, int32_t max_tokens, int32_t kv_bits, size_t *page_pool_bytes, size_t *workspace_bytes);
+int pv_cache_create_kv(const pv_model *m, void *d_page_pool, size_t page_pool_bytes, void *d_workspace, size_t workspace_bytes,
+                       int32_t max_tokens, int32_t kv_bits, pv_cache **out);
+
 /* Replace the logical->physical page map (host array, a permutation of 0..n_pages-1 where
  * n_pages = ceil(max_tokens / page_tokens)).  Only on an empty cache (else PV_ESTATE). */
 int pv_cache_set_page_table(pv_cache *c, const int32_t *phys_pages, int32_t n_pages, void *hip_stream);
@@ -267,6 +275,11 @@ int pv_cache_set_pending(pv_cache *c, int32_t token_or_minus1, void *hip_stream)
 int pv_debug_logits(pv_cache *c, float *host_out, int32_t *rows, void *hip_stream);
 /* pred[0..rows) of the last block. */
 int pv_debug_pred(pv_cache *c, int32_t *host_out, int32_t *rows, void *hip_stream);
+/* What the rows of the last verify / last prefill chunk (those of pv_debug_logits) say of tokens: logprobs[row][i] = the log probability of tokens[row * n_tokens + i] as the next token after
+ * that row (tokens, n_tokens <= 64: e.g. the draft that followed), the row's entropy and log-sum-exp (nullable), its `top` <= 32 most probable tokens.  Host arrays; pv_token_logprobs has the
+ * rules.  *rows (nullable) = the row count.  Synchronises hip_stream. */
+int pv_cache_logprobs(pv_cache *c, const int32_t *tokens, int32_t n_tokens, float *logprobs, float *entropy, float *lse, int32_t top,
+                      int32_t *top_ids, float *top_logprobs, int32_t *rows, void *hip_stream);
 /* Logical K/V of the committed tokens, storage type of the model, laid out
  * [n_layers][2 (K,V)][length][n_kv_heads*head_dim]; nbytes must be at least that size. */
 int pv_cache_export(pv_cache *c, void *host_out, size_t nbytes, void *hip_stream);

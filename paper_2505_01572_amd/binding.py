@@ -1,4 +1,5 @@
 """ctypes binding of include/pipeverify.h.  Argument marshalling only."""
+import collections
 import ctypes
 import os
 
@@ -14,6 +15,9 @@ PATH_AUTO, PATH_VECTOR, PATH_MATRIX = 0, 1, 2
 KINDS = {"embed": 0, "attn_norm": 1, "wq": 2, "wk": 3, "wv": 4, "wo": 5,
          "ffn_norm": 6, "wg": 7, "wu": 8, "wd": 9, "final_norm": 10, "lm_head": 11}
 _GLOBAL = ("embed", "final_norm", "lm_head")
+
+
+TokenLogprobs = collections.namedtuple("TokenLogprobs", "logprobs entropy lse top_ids top_logprobs")
 
 
 class PVError(RuntimeError):
@@ -46,6 +50,7 @@ EXPORTS = [
     "pv_debug_logits", "pv_debug_pred", "pv_cache_export", "pv_step_bytes", "pv_strerror", "pv_last_error",
     "pv_profile_select", "pv_profile_read", "pv_cache_readmit", "pv_calib_copy", "pv_calib_read", "pv_verify_async_static", "pv_verify_batch", "pv_verify_tree", "pv_cache_use_graphs", "pv_load_weights_q4",
     "pv_kv8_bytes", "pv_kv8_append", "pv_kv8_read", "pv_kv8_attention_bytes", "pv_kv8_attention", "pv_token_logprobs_bytes", "pv_token_logprobs",
+    "pv_cache_bytes_kv", "pv_cache_create_kv", "pv_cache_logprobs",
 ]
 
 _lib = None
@@ -100,6 +105,9 @@ def lib():
         L.pv_kv8_attention.argtypes = [poolp, seqsp, *rows, i32, vp, ctypes.c_float, *rows, vp, i32, vp, sz, vp]
         L.pv_token_logprobs_bytes.argtypes = [i64, i32, i32, P(sz)]
         L.pv_token_logprobs.argtypes = [vp, i64, i32, i64, i32, vp, i32, vp, vp, vp, i32, vp, vp, vp, sz, vp]
+        L.pv_cache_bytes_kv.argtypes = [vp, i32, i32, P(sz), P(sz)]
+        L.pv_cache_create_kv.argtypes = [vp, vp, sz, vp, sz, i32, i32, P(vp)]
+        L.pv_cache_logprobs.argtypes = [vp, vp, i32, vp, vp, vp, i32, vp, vp, P(i32), vp]
         L.pv_strerror.argtypes = [ctypes.c_int]; L.pv_strerror.restype = ctypes.c_char_p
         L.pv_last_error.argtypes = []; L.pv_last_error.restype = ctypes.c_char_p
         _lib = L
@@ -221,16 +229,18 @@ class Model:
 class Cache:
     """pv_cache plus the torch-owned page pool and workspace."""
 
-    def __init__(self, model, max_tokens):
+    def __init__(self, model, max_tokens, kv_bits=0):
+        """kv_bits: 0, keys and values in the model's storage type, or 8, as 8-bit codes with block scales."""
         self.L, self.m = model.L, model
+        self.h = None
         pb, wb = ctypes.c_size_t(), ctypes.c_size_t()
-        _check(self.L.pv_cache_bytes(model.h, max_tokens, ctypes.byref(pb), ctypes.byref(wb)), "pv_cache_bytes")
+        _check(self.L.pv_cache_bytes_kv(model.h, max_tokens, kv_bits, ctypes.byref(pb), ctypes.byref(wb)), "pv_cache_bytes_kv")
         with torch.cuda.device(model.device):
             self.pool = _dev_bytes(pb.value, model.device)
             self.ws = _dev_bytes(wb.value, model.device)
             self.h = ctypes.c_void_p()
-            _check(self.L.pv_cache_create(model.h, self.pool.data_ptr(), self.pool.numel(), self.ws.data_ptr(),
-                                          self.ws.numel(), max_tokens, ctypes.byref(self.h)), "pv_cache_create")
+            _check(self.L.pv_cache_create_kv(model.h, self.pool.data_ptr(), self.pool.numel(), self.ws.data_ptr(),
+                                             self.ws.numel(), max_tokens, kv_bits, ctypes.byref(self.h)), "pv_cache_create_kv")
         self.max_tokens = max_tokens
 
     def _dev(self):
@@ -325,6 +335,23 @@ class Cache:
             if r.value:
                 _check(self.L.pv_debug_pred(self.h, out.ctypes.data, None, _stream_ptr(stream)), "pv_debug_pred")
         return out
+
+    def logprobs(self, tokens=None, top=0, stream=None):
+        """What the last block's rows say of the token that follows each: log probabilities of tokens ([rows] or [rows, n]: e.g. the draft one further on), entropy,
+        log-sum-exp and the `top` most probable tokens, as numpy arrays."""
+        r = ctypes.c_int32()
+        _check(self.L.pv_debug_logits(self.h, None, ctypes.byref(r), None), "pv_cache_logprobs")
+        rows = r.value
+        t = np.zeros((rows, 0), dtype=np.int32) if tokens is None else np.ascontiguousarray(tokens, dtype=np.int32)
+        if t.ndim not in (1, 2) or t.shape[0] != rows:
+            raise PVError(-1, "pv_cache_logprobs", f"tokens must be [{rows}] or [{rows}, n], got {t.shape}")
+        n = t.size // max(1, rows)
+        lp, en, lse = np.empty(t.shape, np.float32), np.empty(rows, np.float32), np.empty(rows, np.float32)
+        ids, tlp = np.empty((rows, max(top, 0)), np.int32), np.empty((rows, max(top, 0)), np.float32)
+        with self._dev():
+            _check(self.L.pv_cache_logprobs(self.h, t.ctypes.data, n, lp.ctypes.data, en.ctypes.data, lse.ctypes.data, top, ids.ctypes.data, tlp.ctypes.data, None,
+                                            _stream_ptr(stream)), "pv_cache_logprobs")
+        return TokenLogprobs(lp, en, lse, ids, tlp)
 
     def export(self, stream=None):
         s = self.m.shape

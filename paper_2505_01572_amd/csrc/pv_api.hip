@@ -281,8 +281,17 @@ static int model_complete(const pv_model *m)
 }
 
 // ---- workspace layout ----
-// slices: pv_mat_part_floats
-static size_t layout_ws(const pv_model *m, int rows_cap, int units_cap, int n_pages, pv_ws *w, char *base, bool slices = true)
+// What pv_cache_logprobs keeps on the device for a block's rows: ids and log probabilities of PV_SCORE_TOKENS tokens, entropy and log-sum-exp, 32 alternatives, partial results
+#define PV_SCORE_TOKENS 64
+static size_t score_bytes(const pv_model *m, int rows)
+{
+    size_t part = 0;
+    if (m->cfg.vocab > (1 << 21) || pv_token_logprobs_bytes(rows, m->cfg.vocab, m->cfg.vocab < 32 ? m->cfg.vocab : 32, &part) != PV_OK) return 0;
+    return (size_t)rows * (8 * PV_SCORE_TOKENS + 8 + 8 * 32) + align_up(part, 256) + 256;
+}
+
+// slices: pv_mat_part_floats; stage_rows: rows of keys and values that wait to be quantised (0: the cache is in the model's storage type); score: with room for pv_cache_logprobs
+static size_t layout_ws(const pv_model *m, int rows_cap, int units_cap, int n_pages, pv_ws *w, char *base, bool slices, int stage_rows, bool score)
 {
     const pv_model_config &c = m->cfg;
     size_t off = 0;
@@ -300,6 +309,9 @@ static size_t layout_ws(const pv_model *m, int rows_cap, int units_cap, int n_pa
     p = take(4 * R * (size_t)c.vocab); if (w) w->logits = (float *)p;
     const size_t pf = m->path >= PV_PATH_MATRIX ? pv_mat_part_floats(m, rows_cap, units_cap, n_pages * m->cfg.page_tokens, slices) : 0;
     p = take(4 * pf + 256); if (w) { w->part = (float *)p; w->part_floats = pf; }
+    p = stage_rows ? take((size_t)stage_rows * 4 * c.n_kv_heads * c.head_dim) : nullptr; if (w) w->kv_stage = (uint16_t *)p;
+    const size_t sb = score ? score_bytes(m, rows_cap) : 0;
+    p = sb ? take(sb) : nullptr; if (w) { w->score = p; w->score_bytes = sb; }
     return off;
 }
 
@@ -314,25 +326,58 @@ static inline int rows_cap_of(const pv_model *m) { return (prefill_rows_of(m) + 
 // a workspace's attention partials: one sequence of rows_cap rows, or a batch (every further sequence rounds its rows up to whole units)
 static inline int units_cap_of(const pv_model *m) { return m->path >= PV_PATH_MATRIX ? pv_attn_units(m, rows_cap_of(m)) + PV_MAX_SEQ - 1 : 0; }
 
+// an 8-bit cache's staging rows: a block's, or a long prompt's pass
+static inline int stage_rows_of(const pv_model *m, int kv_bits) { return kv_bits != 8 ? 0 : rows_cap_of(m) > m->pre_rows ? rows_cap_of(m) : m->pre_rows; }
+
+static int check_kv_bits(const pv_model *m, int kv_bits)
+{
+    if (kv_bits != 0 && kv_bits != 8) { pv_set_error("kv_bits must be 0 (the model's storage type) or 8, got %d", kv_bits); return PV_EINVAL; }
+    if (kv_bits == 8 && m->path < PV_PATH_MATRIX) { pv_set_error("8-bit keys and values need the matrix path (bf16 models)"); return PV_EINVAL; }
+    if (kv_bits == 8 && m->cfg.head_dim != 64 && m->cfg.head_dim != 128) { pv_set_error("8-bit keys and values: head_dim must be 64 or 128, got %d", m->cfg.head_dim); return PV_EINVAL; }
+    if (kv_bits == 8 && m->cfg.page_tokens > 65536) { pv_set_error("8-bit keys and values: at most 65536 tokens a page"); return PV_EINVAL; }
+    return PV_OK;
+}
+
+// bytes of an 8-bit pool's codes, rounded up to where the scales begin
+static size_t kv8_code_bytes(const pv_model *m, int n_pages)
+{
+    const pv_model_config &c = m->cfg;
+    return align_up((size_t)c.n_layers * n_pages * c.n_kv_heads * 2 * c.page_tokens * c.head_dim, 256);
+}
+
 extern "C" int pv_cache_bytes(const pv_model *m, int32_t max_tokens, size_t *page_pool_bytes, size_t *workspace_bytes)
+{
+    return pv_cache_bytes_kv(m, max_tokens, 0, page_pool_bytes, workspace_bytes);
+}
+
+extern "C" int pv_cache_bytes_kv(const pv_model *m, int32_t max_tokens, int32_t kv_bits, size_t *page_pool_bytes, size_t *workspace_bytes)
 {
     if (!m || !page_pool_bytes || !workspace_bytes) { pv_set_error("null pointer"); return PV_EINVAL; }
     if (max_tokens <= 0) { pv_set_error("max_tokens must be positive"); return PV_ERANGE; }
     if ((max_tokens + m->cfg.page_tokens - 1) / m->cfg.page_tokens >= (1 << 26)) { pv_set_error("max_tokens %d: more than 2^26 pages", max_tokens); return PV_ERANGE; }
+    const int rc = check_kv_bits(m, kv_bits);
+    if (rc != PV_OK) return rc;
     const pv_model_config &c = m->cfg;
     const int n_pages = (max_tokens + c.page_tokens - 1) / c.page_tokens;
-    *page_pool_bytes = align_up((size_t)c.n_layers * n_pages * c.n_kv_heads * 2 * c.page_tokens * c.head_dim * m->elt, 256);
-    *workspace_bytes = layout_ws(m, rows_cap_of(m), units_cap_of(m), n_pages, nullptr, nullptr);
+    if (kv_bits == 8) *page_pool_bytes = kv8_code_bytes(m, n_pages) + align_up((size_t)c.n_layers * n_pages * c.n_kv_heads * 2 * (c.page_tokens / 16), 256);
+    else *page_pool_bytes = align_up((size_t)c.n_layers * n_pages * c.n_kv_heads * 2 * c.page_tokens * c.head_dim * m->elt, 256);
+    *workspace_bytes = layout_ws(m, rows_cap_of(m), units_cap_of(m), n_pages, nullptr, nullptr, true, stage_rows_of(m, kv_bits), true);
     return PV_OK;
 }
 
 extern "C" int pv_cache_create(const pv_model *m, void *d_page_pool, size_t page_pool_bytes, void *d_workspace,
                                size_t workspace_bytes, int32_t max_tokens, pv_cache **out)
 {
+    return pv_cache_create_kv(m, d_page_pool, page_pool_bytes, d_workspace, workspace_bytes, max_tokens, 0, out);
+}
+
+extern "C" int pv_cache_create_kv(const pv_model *m, void *d_page_pool, size_t page_pool_bytes, void *d_workspace,
+                                  size_t workspace_bytes, int32_t max_tokens, int32_t kv_bits, pv_cache **out)
+{
     if (!m || !d_page_pool || !d_workspace || !out) { pv_set_error("null pointer"); return PV_EINVAL; }
     if (((uintptr_t)d_page_pool | (uintptr_t)d_workspace) & 255) { pv_set_error("device buffers must be 256-byte aligned"); return PV_EINVAL; }
     size_t need_p, need_w;
-    int rc = pv_cache_bytes(m, max_tokens, &need_p, &need_w);
+    int rc = pv_cache_bytes_kv(m, max_tokens, kv_bits, &need_p, &need_w);
     if (rc != PV_OK) return rc;
     if (page_pool_bytes < need_p || workspace_bytes < need_w) { pv_set_error("pool %zu < %zu or workspace %zu < %zu", page_pool_bytes, need_p, workspace_bytes, need_w); return PV_ENOMEM; }
     if (m->path >= PV_PATH_MATRIX && (rc = pv_mat_attention_init(m->cfg.head_dim)) != PV_OK) return rc;
@@ -344,7 +389,8 @@ extern "C" int pv_cache_create(const pv_model *m, void *d_page_pool, size_t page
     c->d_ws = (char *)d_workspace; c->ws_bytes = workspace_bytes;
     c->max_tokens = max_tokens; c->n_pages = (max_tokens + m->cfg.page_tokens - 1) / m->cfg.page_tokens;
     c->rows_cap = rows_cap_of(m); c->units_cap = units_cap_of(m);
-    layout_ws(m, c->rows_cap, c->units_cap, c->n_pages, &c->ws, c->d_ws);
+    c->kv_bits = kv_bits == 8 ? 8 : 16; c->kv8_scales = kv_bits == 8 ? kv8_code_bytes(m, c->n_pages) : 0;
+    layout_ws(m, c->rows_cap, c->units_cap, c->n_pages, &c->ws, c->d_ws, true, stage_rows_of(m, c->kv_bits), true);
     c->len = 0; c->pending = -1; c->last_rows = 0; c->blk_start = 0; c->blk_rows = 0; c->blk_units = 0; c->blk_seq_rows = 0; c->attn_keys = 0; c->in_flight = false; c->flight_stream = nullptr; c->io = nullptr;
     c->prof_kind = PV_PROF_NONE; c->prof_pending = 0; c->prof_ev = nullptr; c->prof_ms = 0; c->prof_launches = 0;
     c->use_graphs = true; c->cap_stream = nullptr;
@@ -506,7 +552,7 @@ extern "C" int pv_profile_read(pv_cache *c, double *total_ms, int64_t *launches,
     uint64_t b = 0;
     switch (c->prof_kind) {
     case PV_PROF_QKV: b = (qd + 2 * kvd) * d * e; break;
-    case PV_PROF_ATTENTION: b = 2 * kvd * e * (uint64_t)c->len; break;
+    case PV_PROF_ATTENTION: b = 2 * kvd * (c->kv_bits == 8 ? 1 : e) * (uint64_t)c->len; break;
     case PV_PROF_OPROJ: b = d * qd * e; break;
     case PV_PROF_GATEUP: b = 2 * (uint64_t)f.ffn_dim * d * e; break;
     case PV_PROF_DOWN: b = (uint64_t)f.ffn_dim * d * e; break;
@@ -705,9 +751,10 @@ extern "C" int pv_verify_async_static(pv_cache *c, int32_t prefix_len, const int
     // as a workspace; the cache state and the page table stay where the cache keeps them)
     const int cap = (gamma + PV_ROW_PAD - 1) / PV_ROW_PAD * PV_ROW_PAD;
     const int ucap = m->path >= PV_PATH_MATRIX ? pv_attn_units(m, cap) : 0;          // one sequence: no batch allowance
-    size_t need = layout_ws(m, cap, ucap, c->n_pages, nullptr, nullptr);
+    const int stage = c->kv_bits == 8 ? cap : 0;
+    size_t need = layout_ws(m, cap, ucap, c->n_pages, nullptr, nullptr, true, stage, false);
     const bool slices = need <= PV_STATIC_SCRATCH_BYTES;         // (no room for K-slices' sums: a step without them, as before there were any)
-    if (!slices) need = layout_ws(m, cap, ucap, c->n_pages, nullptr, nullptr, false);
+    if (!slices) need = layout_ws(m, cap, ucap, c->n_pages, nullptr, nullptr, false, stage, false);
     if (need > PV_STATIC_SCRATCH_BYTES) {
         pv_set_error("a %d-row step of this model with max_tokens %d needs %zu bytes of per-step buffers, the fixed array holds %zu",
                      gamma, c->max_tokens, need, (size_t)PV_STATIC_SCRATCH_BYTES);
@@ -721,7 +768,7 @@ extern "C" int pv_verify_async_static(pv_cache *c, int32_t prefix_len, const int
     PV_HIP(hipGetLastError());
     const pv_ws own = c->ws;
     const int own_cap = c->rows_cap, own_ucap = c->units_cap;
-    layout_ws(m, cap, ucap, c->n_pages, &c->ws, base, slices);
+    layout_ws(m, cap, ucap, c->n_pages, &c->ws, base, slices, stage, false);
     c->ws.state = own.state; c->ws.page_table = own.page_table;
     c->rows_cap = cap; c->units_cap = ucap;
     for (int j = 0; j < gamma; ++j)
@@ -779,6 +826,7 @@ extern "C" int pv_verify_batch(pv_cache *const *caches, int32_t n_seq, const int
         for (int k = 0; k < i; ++k) if (caches[k] == c) { pv_set_error("cache %d appears twice in the batch", i); return PV_EINVAL; }
         if (c->m != m) { pv_set_error("cache %d belongs to another model", i); return PV_EINVAL; }
         if (c->max_tokens != lead->max_tokens) { pv_set_error("caches of a batch must have the same max_tokens (%d vs %d)", c->max_tokens, lead->max_tokens); return PV_EINVAL; }
+        if (c->kv_bits != lead->kv_bits) { pv_set_error("caches of a batch must store keys and values alike (cache %d does not)", i); return PV_EINVAL; }
         if ((rc = verify_checks(c, prefix_len[i], draft + rows, gamma[i])) != PV_OK) return rc;
         rows += gamma[i];
     }
@@ -849,7 +897,7 @@ extern "C" int pv_verify_tree(pv_cache *c, int32_t prefix_len, const int32_t *to
     c->last_rows = n; c->attn_keys = c->len + n;
     hipStream_t s = (hipStream_t)hip_stream;
     rc = record_block(c, n, PV_MODE_TREE, s);               // plain launches
-    if (rc == PV_OK) rc = pv_k_tree_compact(c, s);
+    if (rc == PV_OK) rc = c->kv_bits == 8 ? pv_kv8_tree_compact(c, s) : pv_k_tree_compact(c, s);
     const hipError_t e = hipStreamSynchronize(s);
     if (rc != PV_OK) return rc;
     if (e != hipSuccess) { pv_set_error("draft-tree step failed: %s", hipGetErrorString(e)); return PV_EHIP; }
@@ -937,6 +985,34 @@ extern "C" int pv_debug_pred(pv_cache *c, int32_t *host_out, int32_t *rows, void
     return PV_OK;
 }
 
+extern "C" int pv_cache_logprobs(pv_cache *c, const int32_t *tokens, int32_t n_tokens, float *logprobs, float *entropy, float *lse, int32_t top,
+                                 int32_t *top_ids, float *top_logprobs, int32_t *rows, void *hip_stream)
+{
+    if (!c) { pv_set_error("null cache"); return PV_EINVAL; }
+    if (c->in_flight) { pv_set_error("a verify is in flight on this cache"); return PV_ESTATE; }
+    if (n_tokens < 0 || n_tokens > PV_SCORE_TOKENS) { pv_set_error("n_tokens %d outside [0, %d]", n_tokens, PV_SCORE_TOKENS); return PV_ERANGE; }
+    if (top < 0 || top > 32 || top > c->m->cfg.vocab) { pv_set_error("top %d outside [0, min(32, vocab)]", top); return PV_ERANGE; }
+    if ((n_tokens && (!tokens || !logprobs)) || (top && (!top_ids || !top_logprobs))) { pv_set_error("null pointer"); return PV_EINVAL; }
+    const size_t R = c->last_rows;
+    if (rows) *rows = c->last_rows;
+    if (R == 0) return PV_OK;
+    if (!c->ws.score) { pv_set_error("vocabularies of more than 2^21 tokens have no log probabilities"); return PV_ERANGE; }
+    hipStream_t s = (hipStream_t)hip_stream;
+    int32_t *d_tok = (int32_t *)c->ws.score;
+    float *d_lp = (float *)d_tok + R * PV_SCORE_TOKENS, *d_en = d_lp + R * PV_SCORE_TOKENS, *d_lse = d_en + R, *d_tlp = d_lse + R + R * 32;
+    int32_t *d_ids = (int32_t *)(d_lse + R);
+    char *part = (char *)align_up((size_t)(d_tlp + R * 32), 256);
+    if (n_tokens) PV_HIP(hipMemcpyAsync(d_tok, tokens, R * n_tokens * sizeof(int32_t), hipMemcpyHostToDevice, s));
+    const int rc = pv_token_logprobs(c->ws.logits, c->m->cfg.vocab, PV_F32, (int64_t)R, c->m->cfg.vocab, d_tok, n_tokens, d_lp, d_en, d_lse, top, d_ids, d_tlp,
+                                     part, c->ws.score + c->ws.score_bytes - part, s);
+    if (rc != PV_OK) return rc;
+    auto back = [&](void *host, const void *dev, size_t n) { return host && n ? hipMemcpyAsync(host, dev, n * 4, hipMemcpyDeviceToHost, s) : hipSuccess; };
+    PV_HIP(back(logprobs, d_lp, R * n_tokens)); PV_HIP(back(entropy, d_en, R)); PV_HIP(back(lse, d_lse, R));
+    PV_HIP(back(top_ids, d_ids, R * top)); PV_HIP(back(top_logprobs, d_tlp, R * top));
+    PV_HIP(hipStreamSynchronize(s));
+    return PV_OK;
+}
+
 extern "C" int pv_cache_export(pv_cache *c, void *host_out, size_t nbytes, void *hip_stream)
 {
     if (!c || !host_out) { pv_set_error("null pointer"); return PV_EINVAL; }
@@ -946,6 +1022,21 @@ extern "C" int pv_cache_export(pv_cache *c, void *host_out, size_t nbytes, void 
     if (nbytes < total * c->m->elt) { pv_set_error("export needs %zu bytes, got %zu", total * c->m->elt, nbytes); return PV_ENOMEM; }
     // bounce through the logits buffer (dead between steps) in chunks
     hipStream_t s = (hipStream_t)hip_stream;
+    if (c->kv_bits == 8) {
+        const size_t kvd = (size_t)f.n_kv_heads * f.head_dim, room = (size_t)c->rows_cap * f.vocab * sizeof(float) / (4 * kvd);
+        if (room == 0 && c->len > 0) { pv_set_error("no room to read an 8-bit cache back: a token's keys and values take more than a block's logits"); return PV_ENOMEM; }
+        uint16_t *buf = (uint16_t *)c->ws.logits, *out = (uint16_t *)host_out;
+        for (int l = 0; l < f.n_layers; ++l)
+            for (size_t p = 0; p < (size_t)c->len; p += room) {
+                const size_t n = (size_t)c->len - p < room ? (size_t)c->len - p : room;
+                int rc = pv_kv8_export(c, l, (int)p, (int)n, buf, buf + n * kvd, s);
+                if (rc != PV_OK) return rc;
+                for (int w = 0; w < 2; ++w) PV_HIP(hipMemcpyAsync(out + (((size_t)l * 2 + w) * c->len + p) * kvd, buf + w * n * kvd, n * kvd * 2, hipMemcpyDeviceToHost, s));
+                PV_HIP(hipStreamSynchronize(s));
+            }
+        c->last_rows = 0; c->blk_rows = 0;
+        return PV_OK;
+    }
     const size_t cap = (size_t)c->rows_cap * f.vocab * sizeof(float) / c->m->elt;
     for (size_t e0 = 0; e0 < total; e0 += cap) {
         const size_t n = total - e0 < cap ? total - e0 : cap;
@@ -972,7 +1063,8 @@ extern "C" int pv_step_bytes(const pv_cache *c, int32_t gamma, uint64_t *bytes)
         const uint64_t tb = (m->wbits == 4 && pv_is_q4_kind(k)) ? (uint64_t)(r / 16) * (cc / 128) * PV_Q4_BATCH : (uint64_t)r * cc * m->elt;
         w += tb * (global ? 1 : f.n_layers);
     }
-    const uint64_t kv_tok = (uint64_t)f.n_layers * 2 * f.n_kv_heads * f.head_dim * m->elt;
+    const uint64_t kv_tok = (uint64_t)f.n_layers * 2 * f.n_kv_heads * f.head_dim * (c->kv_bits == 8 ? 1 : m->elt);
     *bytes = w + kv_tok * (uint64_t)(c->len + gamma) + kv_tok * (uint64_t)gamma;
+    if (c->kv_bits == 8) *bytes += (uint64_t)f.n_layers * 2 * f.n_kv_heads * (((uint64_t)c->len + gamma + 15) / 16 + ((uint64_t)gamma + 15) / 16);      // scales
     return PV_OK;
 }

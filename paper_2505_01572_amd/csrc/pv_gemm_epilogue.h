@@ -21,6 +21,7 @@ struct gemm_args {
     // QKV
     uint16_t *q_hi, *q_lo; int q_rows; uint16_t *pool; const int32_t *page_table; const float2 *rope; pv_kv_geom geom;      // queries: q_at
     int layer, n_q_heads, q_strips, k_strips;
+    uint16_t *kv_stage;         // 8-bit cache: where keys and values wait to be quantised (null: they go to the pages)
     // RESID
     float *x; const uint16_t *gain_next; float *ssq_out; uint16_t *xop_out; int d;
     // output projection that merges the attention's chunks itself (pv_attn_split)
@@ -199,12 +200,13 @@ __device__ inline void epi_apply(const gemm_args &a, int strip, int lane, f32x4 
                     *(uint2 *)(a.q_lo + qo) = ql;
                 } else {
                     const int kvh = h - a.n_q_heads;
-                    uint16_t *kp = pool + pv_kv_block(gm, a.layer, phys, kvh, 0) + pv_k_off(gm, tok, e + side * half);
+                    uint16_t *kp = a.kv_stage != nullptr ? a.kv_stage + (size_t)j * a.k_strips * 32 + kvh * hd + e + side * half : pool + pv_kv_block(gm, a.layer, phys, kvh, 0) + pv_k_off(gm, tok, e + side * half);
                     *(uint2 *)kp = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
                 }
             }
         } else if (live) {
             const int sv = strip - a.q_strips - a.k_strips, kvh = sv / spH, e = (sv - kvh * spH) * 16 + 4 * g;
+            if (a.kv_stage != nullptr) { *(uint2 *)(a.kv_stage + ((size_t)j * 2 + 1) * a.k_strips * 16 + kvh * hd + e) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])); return; }
             uint16_t *vp = pool + pv_kv_block(gm, a.layer, phys, kvh, 1);
 #pragma unroll
             for (int r = 0; r < 4; ++r) vp[pv_v_off(gm, tok, e + r)] = bf16_rne(v[r]);

@@ -102,6 +102,8 @@ struct pv_ws {                  // pointers into the caller's workspace
     float *x, *q, *attn, *gate, *up, *logits;
     float *part;                // matrix path: operands, partial sums, attention partials
     size_t part_floats;
+    uint16_t *kv_stage;         // 8-bit cache: keys and values of the running block on their way into it, bf16 [row][K | V][n_kv_heads * head_dim]
+    char *score; size_t score_bytes;   // pv_cache_logprobs: token ids in, results out, partial results
 };
 
 struct pv_cache {
@@ -117,6 +119,8 @@ struct pv_cache {
     int32_t blk_start, blk_rows;   // positions the last block wrote K/V for (blk_rows = 0: none on record)
     int32_t attn_keys;          // keys the attention launch of the step being enqueued has to cover (host-side bound: length + rows)
     int32_t blk_units, blk_seq_rows; // batched step in the making: attention row-group units in all, most rows of one sequence (0: plain step)
+    int32_t kv_bits;            // 16: keys and values in the model's storage type; 8: codes and scales (pv_kv8.h), the scales kv8_scales bytes behind the codes
+    size_t kv8_scales;
     bool in_flight; hipStream_t flight_stream;
     // instrumentation: one kernel kind bracketed by events, one pair per layer
     int32_t prof_kind, prof_pending;
@@ -200,6 +204,13 @@ int pv_mat_gemm_init(int wbits);
 struct pv_attn_split_info { const float *part_o, *part_ml; int chunks, max_chunks, chunk_shift, units; };   // partial results: chunks launched, room per unit, log2 keys a chunk, row groups
 pv_attn_split_info pv_attn_split(const pv_cache *c, int rows, const float *part);   // how the attention of a plain step cuts its keys
 int pv_mat_attention(pv_cache *c, int layer, int rows, float *part, uint16_t *xop_o, bool merge, hipStream_t s);   // merge: false leaves the partial results to the output projection
+// 8-bit cache: a step's keys and values from the staging rows into the pages, its attention over them (operand of the output projection, as pv_mat_attention; n_part: floats of `part`; prompt: a long prompt's
+// pass, causal), and after a draft tree
+struct pv_kv8_step { int layer, rows; const uint16_t *q_hi, *q_lo; int q_rows; uint16_t *xop_o; float *part; size_t n_part; bool prompt; };
+int pv_kv8_step_append(pv_cache *c, int layer, int rows, hipStream_t s);
+int pv_kv8_step_attention(pv_cache *c, const pv_kv8_step &a, hipStream_t s);
+int pv_kv8_tree_compact(pv_cache *c, hipStream_t s);
+int pv_kv8_export(pv_cache *c, int layer, int first, int n, uint16_t *k, uint16_t *v, hipStream_t s);
 void pv_set_error(const char *fmt, ...);
 
 #define PV_HIP(call)                                                                        \

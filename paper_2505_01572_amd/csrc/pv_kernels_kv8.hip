@@ -34,85 +34,126 @@ __device__ inline void kv8_each_block(const kv8_seqs &seqs, const kv8_pool &pool
     }
 }
 
-// One wave a block, head and kind (K or V).  Reads each new number once, writes its code; of earlier tokens' codes it touches those of a block
-// that needs a larger scale, and of V those that share a lane's 16 bytes with the new ones.
+// A wave writes n new tokens behind the `off` that a block of 16 holds; load(t, p, x): 16 numbers, piece p of the t-th new token.  Each new number is read once, its code written; of earlier tokens' codes
+// it touches those of a block that needs a larger scale, and of V those that share a lane's 16 bytes with the new ones.  tile: LDS, a byte a number of the block.
+template <int HD, typename LOAD>
+__device__ inline void kv8_write_block(uint8_t *codes, uint8_t *scale, int which, int off, int n, uint32_t *tile, LOAD load)
+{
+    constexpr int NP = HD / 64, PR = HD / 16;                 // pieces of 16 numbers a lane; pieces a row
+    const int lane = threadIdx.x & 63;
+    const int old = off > 0 ? kv8_byte(*scale) : 0;
+    float x[NP][16];
+    float amax = 0.f;
+#pragma unroll
+    for (int k = 0; k < NP; ++k) {
+        const int piece = k * 64 + lane, t = piece / PR, p = piece % PR;
+        if (t >= off && t < off + n) load(t - off, p, x[k]);
+        else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[k][e] = 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) { const float m = fabsf(x[k][e]); if (m < INFINITY) amax = fmaxf(amax, m); }
+    }
+    amax = over_wave(amax, op_max);
+    const int b = max(old, kv8_need(amax));
+    const float f = kv8_pow2(127 - b);
+    const bool raise = off > 0 && b != old;
+    const float down = raise ? (old - b > -126 ? kv8_pow2(old - b) : 0.f) : 1.f;
+    uint32_t c[NP][4];
+#pragma unroll
+    for (int k = 0; k < NP; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c[k][i] = kv8_code4(x[k][4 * i], x[k][4 * i + 1], x[k][4 * i + 2], x[k][4 * i + 3], f);
+    if (which == 0) {
+#pragma unroll
+        for (int k = 0; k < NP; ++k) {
+            const int piece = k * 64 + lane, t = piece / PR, p = piece % PR;
+            uint4 *at = (uint4 *)(codes + (p * 16 + t) * 16);
+            if (t >= off && t < off + n) *at = make_uint4(c[k][0], c[k][1], c[k][2], c[k][3]);
+            else if (t < off && raise) { const uint4 v = *at; *at = make_uint4(kv8_recode(v.x, down), kv8_recode(v.y, down), kv8_recode(v.z, down), kv8_recode(v.w, down)); }
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < NP; ++k) {
+            const int piece = k * 64 + lane, t = piece / PR, p = piece % PR;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tile[t * (HD / 4) + p * 4 + i] = c[k][i];
+        }
+        __syncthreads();
+        const int g = lane >> 4, jl = lane & 15;
+        uint32_t keep = 0, mine = 0;                           // bytes of a dword: earlier tokens', the new ones' (the rest is left as it was)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) { const int t = 4 * g + r; if (t < off) keep |= 0xffu << (8 * r); else if (t < off + n) mine |= 0xffu << (8 * r); }
+        const bool touch = mine != 0 || (raise && keep != 0);
+#pragma unroll
+        for (int h = 0; h < NP; ++h) {
+            uint4 *at = (uint4 *)codes + h * 64 + lane;
+            uint32_t v[4], o[4] = {0, 0, 0, 0};
+            if (touch && mine != 0xffffffffu) { const uint4 w = *at; o[0] = w.x; o[1] = w.y; o[2] = w.z; o[3] = w.w; }
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+                uint32_t w = 0;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) w |= (uint32_t)((const uint8_t *)tile)[(4 * g + r) * HD + (4 * h + q4) * 16 + jl] << (8 * r);
+                const uint32_t e = raise ? kv8_recode(o[q4], down) : o[q4];
+                v[q4] = (w & mine) | (e & keep) | (o[q4] & ~(mine | keep));
+            }
+            if (touch) *at = make_uint4(v[0], v[1], v[2], v[3]);
+        }
+        __syncthreads();
+    }
+    if (lane == 0 && b != old) *scale = (uint8_t)b;
+}
+
+// One wave a block, head and kind (K or V).
 template <int HD, typename T>
 __global__ void __launch_bounds__(64)
 k_kv8_append(const kv8_append_args a)
 {
-    constexpr int NP = HD / 64, PR = HD / 16;                 // pieces of 16 numbers a lane; pieces a row
     __shared__ uint32_t tile[16 * HD / 4];                    // codes [token][feature]
-    const int lane = threadIdx.x, which = blockIdx.x & 1, head = blockIdx.x >> 1;
+    const int which = blockIdx.x & 1, head = blockIdx.x >> 1;
     const char *src = a.src[which] + (int64_t)head * a.head_bytes[which];
     kv8_each_block<HD>(a.seqs, a.pool, blockIdx.y * a.chunk, a.chunk, [&](const kv8_seq &q, int row, int pos, int off, int n) {
         const int page = kv8_page(q, pos >> q.pool.page_shift), sub = (pos & ((1 << q.pool.page_shift) - 1)) >> 4;
         if (page < 0) return;
-        uint8_t *codes = q.pool.codes + kv8_block<HD>(q.pool, page, head, which, sub);
-        uint8_t *scale = q.pool.scales + kv8_scale(q.pool, page, head, which, sub);
-        const int old = off > 0 ? kv8_byte(*scale) : 0;
-        float x[NP][16];
-        float amax = 0.f;
-#pragma unroll
-        for (int k = 0; k < NP; ++k) {
-            const int piece = k * 64 + lane, t = piece / PR, p = piece % PR;
-            if (t >= off && t < off + n) kv8_el<T>::load(src + (int64_t)(row + t - off) * a.row_bytes[which] + p * 16 * sizeof(T), x[k]);
-            else {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) x[k][e] = 0.f;
-            }
-#pragma unroll
-            for (int e = 0; e < 16; ++e) { const float m = fabsf(x[k][e]); if (m < INFINITY) amax = fmaxf(amax, m); }
-        }
-        amax = over_wave(amax, op_max);
-        const int b = max(old, kv8_need(amax));
-        const float f = kv8_pow2(127 - b);
-        const bool raise = off > 0 && b != old;
-        const float down = raise ? (old - b > -126 ? kv8_pow2(old - b) : 0.f) : 1.f;
-        uint32_t c[NP][4];
-#pragma unroll
-        for (int k = 0; k < NP; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) c[k][i] = kv8_code4(x[k][4 * i], x[k][4 * i + 1], x[k][4 * i + 2], x[k][4 * i + 3], f);
-        if (which == 0) {
-#pragma unroll
-            for (int k = 0; k < NP; ++k) {
-                const int piece = k * 64 + lane, t = piece / PR, p = piece % PR;
-                uint4 *at = (uint4 *)(codes + (p * 16 + t) * 16);
-                if (t >= off && t < off + n) *at = make_uint4(c[k][0], c[k][1], c[k][2], c[k][3]);
-                else if (t < off && raise) { const uint4 v = *at; *at = make_uint4(kv8_recode(v.x, down), kv8_recode(v.y, down), kv8_recode(v.z, down), kv8_recode(v.w, down)); }
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < NP; ++k) {
-                const int piece = k * 64 + lane, t = piece / PR, p = piece % PR;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) tile[t * (HD / 4) + p * 4 + i] = c[k][i];
-            }
-            __syncthreads();
-            const int g = lane >> 4, jl = lane & 15;
-            uint32_t keep = 0, mine = 0;                       // bytes of a dword: earlier tokens', the new ones' (the rest is left as it was)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) { const int t = 4 * g + r; if (t < off) keep |= 0xffu << (8 * r); else if (t < off + n) mine |= 0xffu << (8 * r); }
-            const bool touch = mine != 0 || (raise && keep != 0);
-#pragma unroll
-            for (int h = 0; h < NP; ++h) {
-                uint4 *at = (uint4 *)codes + h * 64 + lane;
-                uint32_t v[4], o[4] = {0, 0, 0, 0};
-                if (touch && mine != 0xffffffffu) { const uint4 w = *at; o[0] = w.x; o[1] = w.y; o[2] = w.z; o[3] = w.w; }
-#pragma unroll
-                for (int q4 = 0; q4 < 4; ++q4) {
-                    uint32_t w = 0;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) w |= (uint32_t)((const uint8_t *)tile)[(4 * g + r) * HD + (4 * h + q4) * 16 + jl] << (8 * r);
-                    const uint32_t e = raise ? kv8_recode(o[q4], down) : o[q4];
-                    v[q4] = (w & mine) | (e & keep) | (o[q4] & ~(mine | keep));
-                }
-                if (touch) *at = make_uint4(v[0], v[1], v[2], v[3]);
-            }
-            __syncthreads();
-        }
-        if (lane == 0 && b != old) *scale = (uint8_t)b;
+        kv8_write_block<HD>(q.pool.codes + kv8_block<HD>(q.pool, page, head, which, sub), q.pool.scales + kv8_scale(q.pool, page, head, which, sub), which, off, n, tile,
+                            [&](int t, int p, float *x) { kv8_el<T>::load(src + (int64_t)(row + t) * a.row_bytes[which] + p * 16 * sizeof(T), x); });
     });
+}
+
+// After a draft-tree step: the accepted path's tokens, in the slots of their row numbers, are read (values of at most four significant bits: exact in bf16) and written behind the prefix, as
+// appending them would have.  A wave a layer, head and kind.
+template <int HD>
+__global__ void __launch_bounds__(64)
+k_kv8_tree(const kv8_pool pool, const kv8_seqs seqs)
+{
+    __shared__ uint32_t tile[16 * HD / 4];
+    __shared__ __align__(16) uint16_t rows[PV_MAX_ROWS][HD];
+    const int lane = threadIdx.x, which = blockIdx.x & 1, head = blockIdx.x >> 1;
+    const kv8_seq q = kv8_seq_in<HD>(seqs, pool, 0, blockIdx.y);
+    const int n = min(seqs.st->accepted, PV_MAX_ROWS), len0 = q.len - n, shift = q.pool.page_shift;      // (the finishing kernel has added n already)
+    bool moved = false;
+    for (int d = 0; d < n; ++d) {
+        const int from = seqs.st->path[d], pos = len0 + from, page = kv8_page(q, pos >> shift), sub = (pos & ((1 << shift) - 1)) >> 4, t = pos & 15;
+        moved = moved || from != d;
+        if (page < 0) return;
+        const uint8_t *codes = q.pool.codes + kv8_block<HD>(q.pool, page, head, which, sub);
+        const float f = kv8_pow2(kv8_byte(q.pool.scales[kv8_scale(q.pool, page, head, which, sub)]) - 127);
+        for (int e = lane; e < HD; e += 64) {
+            const int at = which ? (e / 64) * 1024 + (t / 4) * 256 + (e % 16) * 16 + (e / 16 % 4) * 4 + t % 4 : (e / 16) * 256 + t * 16 + e % 16;
+            rows[d][e] = pv_f32_to_bf16(__builtin_amdgcn_cvt_f32_fp8((int)codes[at], 0) * f);
+        }
+    }
+    if (!moved) return;
+    __syncthreads();
+    for (int d = 0; d < n;) {
+        const int pos = len0 + d, off = pos & 15, m = min(16 - off, n - d), page = kv8_page(q, pos >> shift), sub = (pos & ((1 << shift) - 1)) >> 4;
+        if (page >= 0)
+            kv8_write_block<HD>(q.pool.codes + kv8_block<HD>(q.pool, page, head, which, sub), q.pool.scales + kv8_scale(q.pool, page, head, which, sub), which, off, m, tile,
+                                [&](int t, int p, float *x) { kv8_el<__bf16>::load(&rows[d + t][p * 16], x); });
+        d += m;
+    }
 }
 
 struct kv8_read_args {
@@ -290,5 +331,55 @@ extern "C" int pv_kv8_bytes(const pv_kv8_pool *pool, size_t *codes_bytes, size_t
     if (rc != PV_OK) return rc;
     const size_t blocks = (size_t)p.n_pages * p.n_kv_heads * (p.page_tokens / 16) * 2;
     *codes_bytes = blocks * 16 * p.head_dim; *scales_bytes = blocks;
+    return PV_OK;
+}
+
+// ---- a model's step ----
+
+kv8_seqs pv_kv8_step_seqs(const pv_cache *c, int layer, int rows, int first, kv8_pool *pool)
+{
+    const pv_model_config &f = c->m->cfg;
+    *pool = {(uint8_t *)c->d_pool, nullptr, c->n_pages, f.n_kv_heads, 0};
+    while ((1 << pool->page_shift) < f.page_tokens) ++pool->page_shift;
+    kv8_seqs q = {};
+    q.st = c->ws.state; q.page_table = c->ws.page_table; q.table_pages = c->n_pages; q.n_rows = rows; q.layer = layer; q.first = first; q.scales_off = c->kv8_scales;
+    q.batched = c->blk_units != 0 && first < 0; q.n_seq = q.batched ? c->io->batch.n_seq : 1;
+    return q;
+}
+
+int pv_kv8_step_append(pv_cache *c, int layer, int rows, hipStream_t s)
+{
+    const pv_model_config &f = c->m->cfg;
+    const int64_t kvd = (int64_t)f.n_kv_heads * f.head_dim;
+    kv8_append_args a = {};
+    a.seqs = pv_kv8_step_seqs(c, layer, rows, -1, &a.pool);
+    for (int w = 0; w < 2; ++w) { a.src[w] = (const char *)(c->ws.kv_stage + w * kvd); a.row_bytes[w] = 4 * kvd; a.head_bytes[w] = 2 * f.head_dim; }
+    unsigned gy;
+    walk(rows, f.n_kv_heads, &a.chunk, &gy);
+    return f.head_dim == 128 ? launch_append<128>(a, PV_BF16, gy, s) : launch_append<64>(a, PV_BF16, gy, s);
+}
+
+// tokens [first, first + n) of one layer, bf16 [n][n_kv_heads * head_dim] each
+int pv_kv8_export(pv_cache *c, int layer, int first, int n, uint16_t *k, uint16_t *v, hipStream_t s)
+{
+    const pv_model_config &f = c->m->cfg;
+    kv8_read_args a = {};
+    a.seqs = pv_kv8_step_seqs(c, layer, n, first, &a.pool);
+    a.dst[0] = (char *)k; a.dst[1] = (char *)v;
+    for (int w = 0; w < 2; ++w) { a.row_bytes[w] = (int64_t)2 * f.n_kv_heads * f.head_dim; a.head_bytes[w] = 2 * f.head_dim; }
+    unsigned gy;
+    walk(n, f.n_kv_heads, &a.chunk, &gy);
+    return f.head_dim == 128 ? launch_read<128>(a, PV_BF16, gy, s) : launch_read<64>(a, PV_BF16, gy, s);
+}
+
+int pv_kv8_tree_compact(pv_cache *c, hipStream_t s)
+{
+    const pv_model_config &f = c->m->cfg;
+    kv8_pool pool;
+    const kv8_seqs q = pv_kv8_step_seqs(c, 0, PV_MAX_ROWS, -1, &pool);
+    const dim3 grid(2 * f.n_kv_heads, f.n_layers);
+    if (f.head_dim == 128) k_kv8_tree<128><<<grid, 64, 0, s>>>(pool, q);
+    else k_kv8_tree<64><<<grid, 64, 0, s>>>(pool, q);
+    PV_HIP(hipGetLastError());
     return PV_OK;
 }

@@ -6,6 +6,7 @@
 // magnitude of keys and values is what it stands for.  Softmax with the running maximum and sum, all in 32 bits, in powers of two.
 // P is carried as bf16 hi + lo: rounded to one bf16 it would add as much error as the rounding of a bf16 output and eight times that of an f16 one; one f16 has no room
 // for the weights of many keys beside one that takes nearly all.  q is exact: bf16 as it is, f16 as bf16 hi + lo.
+#include <stddef.h>
 #include "pv_kv8.h"
 
 enum { KV8_BF16 = 0, KV8_F16 = 1, KV8_STEP1 = 2, KV8_STEP2 = 3 };       // queries and outputs: a caller's, or a model's step (operand layouts of 1 .. 8 rows and of more)
@@ -497,4 +498,25 @@ extern "C" int pv_kv8_attention(const pv_kv8_pool *pool, const pv_kv8_seqs *seqs
     hipStream_t s = (hipStream_t)hip_stream;
     if (pool->head_dim == 128) return dtype == PV_BF16 ? launch<128, KV8_BF16>(a, p, s) : launch<128, KV8_F16>(a, p, s);
     return dtype == PV_BF16 ? launch<64, KV8_BF16>(a, p, s) : launch<64, KV8_F16>(a, p, s);
+}
+
+// ---- a model's step ----
+int pv_kv8_step_attention(pv_cache *c, const pv_kv8_step &st, hipStream_t s)
+{
+    const pv_model_config &f = c->m->cfg;
+    kv8_attn_args a = {};
+    a.seqs = pv_kv8_step_seqs(c, st.layer, st.rows, -1, &a.pool);
+    a.group = f.n_q_heads / f.n_kv_heads; a.n_q_heads = f.n_q_heads;
+    const int64_t room = (int64_t)c->n_pages * f.page_tokens, keys = st.prompt ? c->len + st.rows : c->attn_keys > 0 && c->attn_keys < room ? c->attn_keys : room;
+    kv8_plan p = plan(a.seqs.n_seq, st.rows, a.group, f.n_kv_heads, keys);
+    while (p.nsplit > 1 && part_bytes(p, st.rows, f.n_q_heads, f.head_dim) > st.n_part * sizeof(float)) { p.chunk *= 2; p.nsplit = (int)((keys + p.chunk - 1) / p.chunk); }
+    // a recorded step serves all lengths up to its bound
+    a.nsplit = p.nsplit; a.chunk = p.chunk;
+    a.part_o = st.part; a.part_ml = st.part + (size_t)st.rows * f.n_q_heads * p.nsplit * f.head_dim;
+    a.q_hi = st.q_hi; a.q_lo = st.q_lo; a.q_rows = st.q_rows; a.xop_o = st.xop_o;
+    a.mask = st.prompt ? nullptr : (const uint64_t *)((const char *)c->ws.state + offsetof(pv_dev_state, rowmask));
+    a.scale2 = 1.44269504088896340736f / sqrtf((float)f.head_dim);
+    const bool packed = !st.prompt && pv_packs_rows(c->m, st.rows);
+    if (f.head_dim == 128) return packed ? launch<128, KV8_STEP1>(a, p, s) : launch<128, KV8_STEP2>(a, p, s);
+    return packed ? launch<64, KV8_STEP1>(a, p, s) : launch<64, KV8_STEP2>(a, p, s);
 }

@@ -1663,9 +1663,9 @@ static int run_block(pv_cache *c, hipStream_t s)
     g.n_q_heads = f.n_q_heads; g.q_strips = qd / 16; g.k_strips = kvd / 16;
     g.x = c->ws.x; g.d = d; g.xop_act = mw.xop_d; g.F = F;
     g.logits = c->ws.logits; g.pmax_val = mw.pmax_val; g.pmax_idx = mw.pmax_idx; g.vocab = f.vocab;
-    g.tile_part = mw.tile_part;
+    g.tile_part = mw.tile_part; g.kv_stage = c->ws.kv_stage;
     const pv_attn_split_info sp = pv_attn_split(c, rows, mw.attn_part);
-    const bool fused = NB == 1 && merges_in_oproj(c, rows, sp);
+    const bool fused = NB == 1 && c->kv_bits != 8 && merges_in_oproj(c, rows, sp);
     g.part_o = sp.part_o; g.part_ml = sp.part_ml; g.max_chunks = sp.max_chunks; g.chunk_shift = sp.chunk_shift; g.units = sp.units;
 
     for (int l = 0; l < f.n_layers; ++l) {
@@ -1677,7 +1677,11 @@ static int run_block(pv_cache *c, hipStream_t s)
         if ((prc = pv_prof_mark(c, PV_PROF_QKV, l, 1, s)) != PV_OK) return prc;
         // attention over the paged cache -> operand of the output projection
         if ((prc = pv_prof_mark(c, PV_PROF_ATTENTION, l, 0, s)) != PV_OK) return prc;
-        int rc = pv_mat_attention(c, l, rows, mw.attn_part, mw.xop_o, !fused, s);
+        int rc;
+        if (c->kv_bits == 8) {
+            if ((rc = pv_kv8_step_append(c, l, rows, s)) == PV_OK)
+                rc = pv_kv8_step_attention(c, {l, rows, g.q_hi, g.q_lo, rows, mw.xop_o, mw.attn_part, pv_attn_part_floats(m, c->units_cap, c->n_pages * f.page_tokens), false}, s);
+        } else rc = pv_mat_attention(c, l, rows, mw.attn_part, mw.xop_o, !fused, s);
         if (rc != PV_OK) return rc;
         if ((prc = pv_prof_mark(c, PV_PROF_ATTENTION, l, 1, s)) != PV_OK) return prc;
         // output projection + residual; emits the FFN operand and sum of squares

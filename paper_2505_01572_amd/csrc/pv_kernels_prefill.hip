@@ -1107,7 +1107,7 @@ int pv_pre_block(pv_cache *c, const int32_t *d_host_tokens, int rows, int keep, 
     g.st = c->ws.state; g.inv_d = 1.0f / (float)d; g.eps = (float)f.rms_eps; g.ssq_parts = d / 16;
     g.q_hi = w.q_hi; g.q_lo = w.q_lo; g.q_rows = rows; g.pool = (uint16_t *)c->d_pool; g.page_table = c->ws.page_table; g.rope = w.rope; g.geom = pv_geom(c);
     g.n_q_heads = f.n_q_heads; g.q_strips = qd / 16; g.k_strips = kvd / 16;
-    g.x = w.x; g.d = d; g.xop_act = w.xop_d; g.F = F; g.tile_part = w.part; g.ssq = w.ssq; g.ssq_out = w.ssq; g.xop_out = w.xop;
+    g.x = w.x; g.d = d; g.xop_act = w.xop_d; g.F = F; g.tile_part = w.part; g.ssq = w.ssq; g.ssq_out = w.ssq; g.xop_out = w.xop; g.kv_stage = c->ws.kv_stage;
 
     pre_attn_args at = {};
     at.rows = rows; at.len = len; at.page_table = c->ws.page_table; at.q_hi = w.q_hi; at.q_lo = w.q_lo; at.pool = (const uint16_t *)c->d_pool; at.geom = g.geom;
@@ -1131,7 +1131,9 @@ int pv_pre_block(pv_cache *c, const int32_t *d_host_tokens, int rows, int keep, 
         if ((rc = pv_prof_mark(c, PV_PROF_QKV, l, 1, s)) != PV_OK) return rc;
         at.layer = l;
         if ((rc = pv_prof_mark(c, PV_PROF_ATTENTION, l, 0, s)) != PV_OK) return rc;
-        rc = hd == 128 ? pre_attention<128>(at, f.n_kv_heads, s) : hd == 64 ? pre_attention<64>(at, f.n_kv_heads, s) : pre_attention<32>(at, f.n_kv_heads, s);
+        if (c->kv_bits == 8) {
+            if ((rc = pv_kv8_step_append(c, l, rows, s)) == PV_OK) rc = pv_kv8_step_attention(c, {l, rows, w.q_hi, w.q_lo, rows, w.xop_o, w.part, w.part_floats, true}, s);
+        } else rc = hd == 128 ? pre_attention<128>(at, f.n_kv_heads, s) : hd == 64 ? pre_attention<64>(at, f.n_kv_heads, s) : pre_attention<32>(at, f.n_kv_heads, s);
         if (rc != PV_OK) return rc;
         if ((rc = pv_prof_mark(c, PV_PROF_ATTENTION, l, 1, s)) != PV_OK) return rc;
         g.W = (const uint4 *)(Wb + pv_tref(m, PV_T_WO, l).off); g.xop = (const uint4 *)w.xop_o; g.ktiles = qd / 32; g.gain_next = gainp(PV_T_FFN_NORM, l);

@@ -24,6 +24,7 @@ struct kv8_seqs {
     int n_seq, n_rows, table_pages;
     const pv_dev_state *st;                 // a step: its sequences' states, pools and page tables; n_rows = its rows, table_pages the cache's own
     int batched, layer;                     // several sequences in it
+    int first;                              // position of row 0 (-1: the sequence's length)
     size_t scales_off;                      // where a cache's scales lie behind its codes (all caches of a batch have as many pages)
 };
 
@@ -43,8 +44,8 @@ __device__ inline size_t kv8_scale(const kv8_pool &p, int page, int head, int wh
     return (((((size_t)page * p.n_heads + head) << (p.page_shift - 4)) + sub) << 1) + which;
 }
 
-// Sequence s of the call
-template <int HD> __device__ inline kv8_seq kv8_seq_at(const kv8_seqs &q, const kv8_pool &own, int s)
+// Sequence s of the call (in another layer than the call's)
+template <int HD> __device__ inline kv8_seq kv8_seq_in(const kv8_seqs &q, const kv8_pool &own, int s, int layer)
 {
     kv8_seq r;
     r.pool = own;
@@ -56,10 +57,10 @@ template <int HD> __device__ inline kv8_seq kv8_seq_at(const kv8_seqs &q, const 
             const pv_seq_ref &sq = q.st->blk.seq[s];
             st = sq.st; r.table = sq.page_table; r.table_pages = sq.n_pages; r.row0 = sq.row0; r.rows = sq.gamma; base = (char *)sq.pool;
         }
-        r.len = st->len;
+        r.len = q.first >= 0 ? q.first : st->len;
         const size_t page_codes = ((size_t)(2 * HD) << own.page_shift) * own.n_heads, page_scales = ((size_t)2 << (own.page_shift - 4)) * own.n_heads;
-        r.pool.codes = (uint8_t *)base + (size_t)q.layer * own.n_pages * page_codes;
-        r.pool.scales = (uint8_t *)base + q.scales_off + (size_t)q.layer * own.n_pages * page_scales;
+        r.pool.codes = (uint8_t *)base + (size_t)layer * own.n_pages * page_codes;
+        r.pool.scales = (uint8_t *)base + q.scales_off + (size_t)layer * own.n_pages * page_scales;
         return r;
     }
     r.table = q.page_table + (size_t)s * q.table_pages; r.table_pages = q.table_pages;
@@ -69,6 +70,8 @@ template <int HD> __device__ inline kv8_seq kv8_seq_at(const kv8_seqs &q, const 
     if (r.row0 < 0 || r.rows < 0 || r.len < 0) r.rows = 0;
     return r;
 }
+
+template <int HD> __device__ inline kv8_seq kv8_seq_at(const kv8_seqs &q, const kv8_pool &own, int s) { return kv8_seq_in<HD>(q, own, s, q.layer); }
 
 // The sequence that a row belongs to, -1: none (the row lies behind the last one).  Whole waves call.
 __device__ inline int kv8_seq_of_row(const kv8_seqs &q, int row)
@@ -186,3 +189,4 @@ int pv_kv8_check_seqs(const pv_kv8_seqs *q);
 int pv_kv8_check_rows(const char *what, const void *p, int64_t row_stride, int64_t head_stride, int dtype);   // rows of heads in memory: addresses that 16-byte accesses take
 kv8_pool pv_kv8_pool_args(const pv_kv8_pool *p);
 kv8_seqs pv_kv8_seqs_args(const pv_kv8_seqs *q);
+kv8_seqs pv_kv8_step_seqs(const pv_cache *c, int layer, int rows, int first, kv8_pool *pool);      // of a cache's own step: rows from position `first` on, -1: behind the committed tokens

@@ -109,7 +109,7 @@ def pipespec_closed_form(alpha, n_draft):
 
 
 def main():
-    """python -m paper_2505_01572_amd.drivers [--draft 1b] [--mid 8b] [--target 70b_v128k] [--tokens 128]
+    """python -m paper_2505_01572_amd.drivers [--draft 1b] [--mid 8b] [--target 70b_v128k] [--tokens 128] [--kv-bits 8]
 
     Runs, on one GPU and the same kernels: the target model alone (autoregressive), synchronous
     speculative decoding {draft, target}, the asynchronous two-stage pipeline {draft, target} and
@@ -136,6 +136,7 @@ def main():
     ap.add_argument("--n-draft", type=int, default=7, help="drafts per round; a block has n_draft + 1 rows")
     ap.add_argument("--prefix", type=int, default=1024)
     ap.add_argument("--tokens", type=int, default=128)
+    ap.add_argument("--kv-bits", type=int, default=0, choices=(0, 8), help="8: the stages' caches in 8 bits")
     a = ap.parse_args()
     names = [a.draft, a.mid, a.target]
     shapes = [pv_inputs.CONFIGS[n] for n in names]
@@ -147,7 +148,7 @@ def main():
     for shp in shapes:
         t0 = time.time()
         m = load_stage_model(pv, pv_inputs, shp)
-        c = pv.Cache(m, a.prefix + span)
+        c = pv.Cache(m, a.prefix + span, kv_bits=a.kv_bits)
         c.prefill(prompt)
         print(f"[drivers] {shp.name} ready in {time.time() - t0:.1f}s", file=sys.stderr, flush=True)
         caches.append(c)
@@ -192,7 +193,7 @@ def main():
                 "closed_form_tokens_per_step": closed_form_tokens_per_step(f["alpha_measured"], f["mean_block"] - 1.0)}
 
     out = {"metric": "decoding_drives_tokens_per_s", "unit": "tok/s", "models": names, "prefix": a.prefix, "tokens": a.tokens,
-           "n_draft": a.n_draft, "levels": [a.level_draft, a.level_mid],
+           "n_draft": a.n_draft, "kv_bits": a.kv_bits or 16, "levels": [a.level_draft, a.level_mid],
            "autoregressive": {"tokens_per_s": ar_rate, "target_step_ms": t_target_step * 1e3, "draft_step_ms": t_draft_step * 1e3,
                               "speed_ratio_c": c_ratio},
            "sync_sd": {"tokens_per_s": sd["tokens_per_s"], "speedup_vs_ar": sd["tokens_per_s"] / ar_rate,

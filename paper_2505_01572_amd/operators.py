@@ -9,13 +9,12 @@
 Argument marshalling only; work is enqueued on `stream` (default: the current stream of the pool's device) and not waited for.  A tensor made on another stream
 is the caller's to order, as everywhere in torch.
 """
-import collections
 import ctypes
 import math
 
 import torch
 
-from .binding import PVError, _check, lib, pv_kv8_pool, pv_kv8_seqs
+from .binding import PVError, TokenLogprobs, _check, lib, pv_kv8_pool, pv_kv8_seqs
 
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
@@ -148,9 +147,6 @@ class KV8Pool:
             _check(self.L.pv_kv8_attention(pa, sa, *qa, heads, None if mask is None else mask.data_ptr(), scale, *oa, None if lse is None else lse.data_ptr(),
                                            _DTYPES[q.dtype], None if ws is None else ws.data_ptr(), need.value, s), "pv_kv8_attention")
         return (out, lse) if lse is not None else out
-
-
-TokenLogprobs = collections.namedtuple("TokenLogprobs", "logprobs entropy lse top_ids top_logprobs")
 
 
 def token_logprobs(logits, tokens=None, top=0, stream=None):

@@ -245,6 +245,7 @@ def main():
     ap.add_argument("--gamma", type=int, default=8)
     ap.add_argument("--prefix", type=int, default=1024)
     ap.add_argument("--tokens", type=int, default=256)
+    ap.add_argument("--kv-bits", type=int, default=0, choices=(0, 8), help="8: the stages' caches in 8 bits")
     a = ap.parse_args()
     names = a.stages.split(",")
     levels = [float(x) for x in a.levels.split(",")] + [1.0]
@@ -258,7 +259,7 @@ def main():
     for i, shp in enumerate(shapes):
         t0 = time.time()
         m = load_stage_model(pv, pv_inputs, shp)
-        c = pv.Cache(m, a.prefix + span)
+        c = pv.Cache(m, a.prefix + span, kv_bits=a.kv_bits)
         c.prefill(prompt)
         print(f"[pipeline] stage {i} ({shp.name}) ready in {time.time() - t0:.1f}s", file=sys.stderr, flush=True)
         stages.append(Stage(i, c, levels[i], 1 if i == 0 else a.gamma, torch.cuda.Stream()))
