@@ -10,37 +10,41 @@ Argument marshalling only; work is enqueued on `stream` (default: the current st
 is the caller's to order, as everywhere in torch.
 """
 import ctypes
-import math
 
 import torch
 
 from .binding import PVError, TokenLogprobs, _check, lib, pv_kv8_pool, pv_kv8_seqs
 
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_HALF = {torch.bfloat16: 1, torch.float16: 2}
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else lambda i: torch.cuda.current_stream(i).cuda_stream
+
+# A call's Python takes about as long as its kernels on small batches, so what every call passes through formats no message and makes no object that it does not need.
 
 
-def _need(ok, where, what):
-    if not ok:
-        raise PVError(-1, where, what)
+def _refuse(where, what):
+    raise PVError(-1, where, what)
 
 
-def _on(t, device, where, name):
-    _need(isinstance(t, torch.Tensor) and t.device == device, where, f"{name} is not a tensor on {device}")
-
-
-class _Stream:
+class _Elsewhere:
     """Makes device and stream current, so that what torch allocates belongs to the stream the kernels run on."""
 
     def __init__(self, device, stream):
-        self.stream = torch.cuda.current_stream(device) if stream is None else stream
-        self.ctx = torch.cuda.stream(self.stream)
+        self.device, self.stream = torch.cuda.device(device), torch.cuda.stream(stream) if stream is not None else None
 
     def __enter__(self):
-        self.ctx.__enter__()
-        return ctypes.c_void_p(self.stream.cuda_stream)
+        self.device.__enter__()
+        if self.stream is not None:
+            self.stream.__enter__()
 
     def __exit__(self, *a):
-        return self.ctx.__exit__(*a)
+        if self.stream is not None:
+            self.stream.__exit__(*a)
+        self.device.__exit__(*a)
+
+
+def _elsewhere(index, stream):
+    return stream is not None or torch.cuda.current_device() != index
 
 
 class KV8Seqs:
@@ -51,14 +55,24 @@ class KV8Seqs:
     def __init__(self, row_start, prefix_len, page_table):
         where = "KV8Seqs"
         for name, t, dims in (("row_start", row_start, 1), ("prefix_len", prefix_len, 1), ("page_table", page_table, 2)):
-            _need(isinstance(t, torch.Tensor) and t.dtype == torch.int32 and t.dim() == dims and t.is_contiguous(), where, f"{name} must be a contiguous int32 tensor of {dims} dimension(s)")
-            _need(t.is_cuda and t.device == prefix_len.device, where, f"{name} must be on the GPU, all three on one device")
+            if not (isinstance(t, torch.Tensor) and t.dtype == torch.int32 and t.dim() == dims and t.is_contiguous()):
+                _refuse(where, f"{name} must be a contiguous int32 tensor of {dims} dimension(s)")
+            if not (t.is_cuda and t.device == row_start.device):
+                _refuse(where, f"{name} must be on the GPU, all three on one device")
         n = prefix_len.shape[0]
-        _need(row_start.shape[0] == n + 1 and page_table.shape[0] == n, where, f"{n} sequences: row_start must have {n + 1} entries, page_table {n} rows")
+        if row_start.shape[0] != n + 1 or page_table.shape[0] != n:
+            _refuse(where, f"{n} sequences: row_start must have {n + 1} entries, page_table {n} rows")
         self.row_start, self.prefix_len, self.page_table, self.device = row_start, prefix_len, page_table, prefix_len.device
+        self._fields = (row_start.data_ptr(), prefix_len.data_ptr(), page_table.data_ptr(), n)
+        self._args = {}                                    # a call's rows -> the struct for it
 
     def _arg(self, n_rows):
-        return pv_kv8_seqs(self.row_start.data_ptr(), self.prefix_len.data_ptr(), self.page_table.data_ptr(), self.prefix_len.shape[0], n_rows, self.page_table.shape[1])
+        a = self._args.get(n_rows)
+        if a is None:
+            if len(self._args) > 256:
+                self._args.clear()
+            a = self._args[n_rows] = pv_kv8_seqs(*self._fields, n_rows, self.page_table.shape[1])
+        return a
 
 
 class KV8Pool:
@@ -73,51 +87,67 @@ class KV8Pool:
         self.n_pages, self.n_kv_heads, self.head_dim, self.page_tokens = n_pages, n_kv_heads, head_dim, page_tokens
         shapes = ((n_pages, n_kv_heads, 2, page_tokens * head_dim), (n_pages, n_kv_heads, page_tokens // 16, 2))
         given = codes if codes is not None else scales
-        self.device = given.device if given is not None else torch.device(device)
-        self.codes = torch.empty(shapes[0], dtype=torch.uint8, device=self.device) if codes is None else codes
-        self.scales = torch.empty(shapes[1], dtype=torch.uint8, device=self.device) if scales is None else scales
+        at = given.device if given is not None else torch.device(device)
+        self.codes = torch.empty(shapes[0], dtype=torch.uint8, device=at) if codes is None else codes
+        self.scales = torch.empty(shapes[1], dtype=torch.uint8, device=at) if scales is None else scales
         self.device = self.codes.device
         for name, t, shape in (("codes", self.codes, shapes[0]), ("scales", self.scales, shapes[1])):
-            _on(t, self.device, where, name)
-            _need(t.is_cuda and t.dtype == torch.uint8 and tuple(t.shape) == shape and t.is_contiguous(), where, f"{name} must be a contiguous uint8 tensor {shape} on the GPU")
+            if not (t.is_cuda and t.device == self.device and t.dtype == torch.uint8 and tuple(t.shape) == shape and t.is_contiguous()):
+                _refuse(where, f"{name} must be a contiguous uint8 tensor {shape} on the GPU, both on one device")
+        self._index = self.device.index
+        self._arg = pv_kv8_pool(self.codes.data_ptr(), self.scales.data_ptr(), n_pages, n_kv_heads, head_dim, page_tokens)
+        self._need = {}                                    # (sequences, rows, heads, table's pages) -> bytes of attention's workspace
 
-    def _arg(self):
-        return ctypes.byref(pv_kv8_pool(self.codes.data_ptr(), self.scales.data_ptr(), self.n_pages, self.n_kv_heads, self.head_dim, self.page_tokens))
+    def _rows(self, t, where, name, heads, dtypes):
+        """Rows [n, heads, head_dim], features next to each other: address and strides."""
+        if not isinstance(t, torch.Tensor) or t.device != self.device:
+            _refuse(where, f"{name} is not a tensor on {self.device}")
+        shape, stride = t.shape, t.stride()
+        if t.dtype not in dtypes or len(shape) != 3 or shape[1] != heads or shape[2] != self.head_dim:
+            _refuse(where, f"{name} must be [rows, {heads}, {self.head_dim}] of {tuple(dtypes)}, got {tuple(shape)} of {t.dtype}")
+        if stride[2] != 1:
+            _refuse(where, f"{name}: the features of a head must lie next to each other")
+        return t.data_ptr(), stride[0], stride[1]
 
     def _seqs(self, seqs, where, n_rows):
-        _need(isinstance(seqs, KV8Seqs) and seqs.device == self.device, where, f"seqs must be a KV8Seqs on {self.device}")
-        return ctypes.byref(seqs._arg(n_rows))
-
-    def _rows(self, t, where, name, heads, dtypes, rows=None, like=None):
-        """Address and strides of rows [n, heads, head_dim], features next to each other."""
-        _on(t, self.device, where, name)
-        _need(t.dtype in dtypes and t.dim() == 3 and t.shape[1] == heads and t.shape[2] == self.head_dim, where, f"{name} must be [rows, {heads}, {self.head_dim}] of {dtypes}, got {tuple(t.shape)} of {t.dtype}")
-        _need(rows is None or t.shape[0] == rows, where, f"{name} must have {rows} rows")
-        _need(like is None or t.dtype == like.dtype, where, f"{name} must be {like.dtype if like is not None else None}")
-        _need(t.stride(2) == 1 or t.numel() == 0, where, f"{name}: the features of a head must lie next to each other")
-        return t.data_ptr(), t.stride(0), t.stride(1)
+        if not isinstance(seqs, KV8Seqs) or seqs.device != self.device:
+            _refuse(where, f"seqs must be a KV8Seqs on {self.device}")
+        return seqs._arg(n_rows)
 
     def append(self, seqs, k, v, stream=None):
         """Quantise k, v [rows, n_kv_heads, head_dim] (float32, bfloat16 or float16) into the pages of their sequences."""
         where = "KV8Pool.append"
-        ka = self._rows(k, where, "k", self.n_kv_heads, tuple(_DTYPES))
-        va = self._rows(v, where, "v", self.n_kv_heads, tuple(_DTYPES), k.shape[0], k)
-        sa = self._seqs(seqs, where, k.shape[0])
-        with _Stream(self.device, stream) as s:
-            _check(self.L.pv_kv8_append(self._arg(), sa, *ka, *va, _DTYPES[k.dtype], s), "pv_kv8_append")
+        if _elsewhere(self._index, stream):
+            with _Elsewhere(self.device, stream):
+                return self.append(seqs, k, v)
+        kp, kr, kh = self._rows(k, where, "k", self.n_kv_heads, _DTYPES)
+        vp, vr, vh = self._rows(v, where, "v", self.n_kv_heads, _DTYPES)
+        n = k.shape[0]
+        if v.shape[0] != n or v.dtype != k.dtype:
+            _refuse(where, "k and v must have the same rows and type")
+        rc = self.L.pv_kv8_append(self._arg, self._seqs(seqs, where, n), kp, kr, kh, vp, vr, vh, _DTYPES[k.dtype], _raw_stream(self._index))
+        if rc:
+            _check(rc, "pv_kv8_append")
 
     def read(self, seqs, rows, dtype=torch.bfloat16, out=None, stream=None):
         """The tokens at the rows' positions, dequantised: (k, v), each [rows, n_kv_heads, head_dim].  out: the pair to write to (rows of no
         sequence are left as they are); made here otherwise."""
         where = "KV8Pool.read"
-        with _Stream(self.device, stream) as s:
-            if out is None:
-                _need(dtype in _DTYPES, where, f"dtype must be one of {tuple(_DTYPES)}")
-                out = tuple(torch.empty(rows, self.n_kv_heads, self.head_dim, dtype=dtype, device=self.device) for _ in range(2))
-            k, v = out
-            ka = self._rows(k, where, "k", self.n_kv_heads, tuple(_DTYPES), rows)
-            va = self._rows(v, where, "v", self.n_kv_heads, tuple(_DTYPES), rows, k)
-            _check(self.L.pv_kv8_read(self._arg(), self._seqs(seqs, where, rows), *ka, *va, _DTYPES[k.dtype], s), "pv_kv8_read")
+        if _elsewhere(self._index, stream):
+            with _Elsewhere(self.device, stream):
+                return self.read(seqs, rows, dtype, out)
+        if out is None:
+            if dtype not in _DTYPES:
+                _refuse(where, f"dtype must be one of {tuple(_DTYPES)}")
+            out = torch.empty((2, rows, self.n_kv_heads, self.head_dim), dtype=dtype, device=self.device).unbind(0)
+        k, v = out
+        kp, kr, kh = self._rows(k, where, "k", self.n_kv_heads, _DTYPES)
+        vp, vr, vh = self._rows(v, where, "v", self.n_kv_heads, _DTYPES)
+        if k.shape[0] != rows or v.shape[0] != rows or v.dtype != k.dtype:
+            _refuse(where, f"k and v must have {rows} rows and the same type")
+        rc = self.L.pv_kv8_read(self._arg, self._seqs(seqs, where, rows), kp, kr, kh, vp, vr, vh, _DTYPES[k.dtype], _raw_stream(self._index))
+        if rc:
+            _check(rc, "pv_kv8_read")
         return k, v
 
     def attention(self, seqs, q, scale=None, mask=None, out=None, return_lse=False, lse=None, stream=None):
@@ -125,49 +155,84 @@ class KV8Pool:
         given.  Without a mask a row sees the tokens up to its own position.  mask: int64 or uint64 [rows], bit t: the row sees token prefix_len + t
         (a draft tree: its ancestors and itself); all tokens before prefix_len are seen.  Returns out, or (out, lse) with lse float32 [rows, n_q_heads]."""
         where = "KV8Pool.attention"
-        _need(isinstance(q, torch.Tensor) and q.dim() == 3, where, "q must be [rows, heads, head_dim]")
-        n, heads = q.shape[:2]
-        scale = 1 / math.sqrt(self.head_dim) if scale is None else float(scale)
-        half = (torch.bfloat16, torch.float16)
-        qa = self._rows(q, where, "q", heads, half)
+        if _elsewhere(self._index, stream):
+            with _Elsewhere(self.device, stream):
+                return self.attention(seqs, q, scale, mask, out, return_lse, lse)
+        if not isinstance(q, torch.Tensor) or q.dim() != 3:
+            _refuse(where, "q must be [rows, heads, head_dim]")
+        n, heads, _ = q.shape
+        qp, qr, qh = self._rows(q, where, "q", heads, _HALF)
+        sa, mp = self._seqs(seqs, where, n), None
         if mask is not None:
-            _on(mask, self.device, where, "mask")
-            _need(mask.dtype in (torch.int64, torch.uint64) and tuple(mask.shape) == (n,) and mask.is_contiguous(), where, f"mask must be a contiguous int64 tensor [{n}]")
-        pa, sa, need = self._arg(), self._seqs(seqs, where, n), ctypes.c_size_t()
-        _check(self.L.pv_kv8_attention_bytes(pa, sa, heads, ctypes.byref(need)), "pv_kv8_attention_bytes")
-        with _Stream(self.device, stream) as s:
-            out = torch.empty(n, heads, self.head_dim, dtype=q.dtype, device=self.device) if out is None else out
-            oa = self._rows(out, where, "out", heads, half, n, q)
-            if lse is None and return_lse:
-                lse = torch.empty(n, heads, dtype=torch.float32, device=self.device)
-            if lse is not None:
-                _on(lse, self.device, where, "lse")
-                _need(lse.dtype == torch.float32 and tuple(lse.shape) == (n, heads) and lse.is_contiguous(), where, f"lse must be a contiguous float32 tensor [{n}, {heads}]")
-            ws = torch.empty(need.value, dtype=torch.uint8, device=self.device) if need.value else None
-            _check(self.L.pv_kv8_attention(pa, sa, *qa, heads, None if mask is None else mask.data_ptr(), scale, *oa, None if lse is None else lse.data_ptr(),
-                                           _DTYPES[q.dtype], None if ws is None else ws.data_ptr(), need.value, s), "pv_kv8_attention")
-        return (out, lse) if lse is not None else out
+            if not (isinstance(mask, torch.Tensor) and mask.device == self.device and mask.dtype in (torch.int64, torch.uint64) and mask.shape == (n,) and mask.is_contiguous()):
+                _refuse(where, f"mask must be a contiguous int64 tensor [{n}] on {self.device}")
+            mp = mask.data_ptr()
+        key = (sa.n_seq, n, heads, sa.table_pages)
+        need = self._need.get(key)
+        if need is None:
+            b = ctypes.c_size_t()
+            _check(self.L.pv_kv8_attention_bytes(self._arg, sa, heads, ctypes.byref(b)), "pv_kv8_attention_bytes")
+            if len(self._need) > 256:
+                self._need.clear()
+            need = self._need[key] = b.value
+        if out is None:
+            out = q.new_empty((n, heads, self.head_dim))
+            op, orow, oh = out.data_ptr(), heads * self.head_dim, self.head_dim
+        else:
+            op, orow, oh = self._rows(out, where, "out", heads, _HALF)
+            if out.shape[0] != n or out.dtype != q.dtype:
+                _refuse(where, f"out must have {n} rows of {q.dtype}")
+        if lse is not None:
+            if not (isinstance(lse, torch.Tensor) and lse.device == self.device and lse.dtype == torch.float32 and lse.shape == (n, heads) and lse.is_contiguous()):
+                _refuse(where, f"lse must be a contiguous float32 tensor [{n}, {heads}] on {self.device}")
+        elif return_lse:
+            lse = q.new_empty((n, heads), dtype=torch.float32)
+        ws = q.new_empty(need, dtype=torch.uint8) if need else None
+        rc = self.L.pv_kv8_attention(self._arg, sa, qp, qr, qh, heads, mp, self.head_dim ** -0.5 if scale is None else scale, op, orow, oh, None if lse is None else lse.data_ptr(),
+                                     _HALF[q.dtype], None if ws is None else ws.data_ptr(), need, _raw_stream(self._index))
+        if rc:
+            _check(rc, "pv_kv8_attention")
+        return out if lse is None else (out, lse)
+
+
+_logprobs_need = {}                                        # (rows, vocab, top) -> bytes of workspace
 
 
 def token_logprobs(logits, tokens=None, top=0, stream=None):
     """Log probabilities under each row of logits [rows, vocab] (float32, bfloat16 or float16): of tokens (int32 [rows, n] or [rows]), and of the `top` <= 32 most
     probable ones (equal ones: the lower id first), with the row's entropy and log-sum-exp.  float32, in nats; a NaN logit counts as -infinity."""
     where = "token_logprobs"
-    _need(isinstance(logits, torch.Tensor) and logits.is_cuda and logits.dim() == 2 and logits.dtype in _DTYPES, where, f"logits must be [rows, vocab] of {tuple(_DTYPES)} on the GPU")
+    if not (isinstance(logits, torch.Tensor) and logits.is_cuda and logits.dim() == 2 and logits.dtype in _DTYPES):
+        _refuse(where, f"logits must be [rows, vocab] of {tuple(_DTYPES)} on the GPU")
+    index = logits.device.index
+    if _elsewhere(index, stream):
+        with _Elsewhere(logits.device, stream):
+            return token_logprobs(logits, tokens, top)
     rows, vocab = logits.shape
-    _need(logits.stride(1) == 1 or vocab <= 1 or rows == 0, where, "the logits of a row must lie next to each other")
-    d = logits.device
+    row_stride, one = logits.stride()
+    if one != 1 and vocab > 1 and rows > 0:
+        _refuse(where, "the logits of a row must lie next to each other")
+    n, shape, tp = 0, (rows, 0), None
     if tokens is not None:
-        _on(tokens, d, where, "tokens")
-        _need(tokens.dtype == torch.int32 and tokens.dim() in (1, 2) and tokens.shape[0] == rows and tokens.is_contiguous(), where, f"tokens must be a contiguous int32 tensor [{rows}] or [{rows}, n]")
-    n = 0 if tokens is None else tokens.numel() // max(1, rows)
-    L, need = lib(), ctypes.c_size_t()
-    _check(L.pv_token_logprobs_bytes(rows, vocab, top, ctypes.byref(need)), "pv_token_logprobs_bytes")
-    with _Stream(d, stream) as s:
-        f = lambda *shape: torch.empty(*shape, dtype=torch.float32, device=d)  # noqa: E731
-        got = TokenLogprobs(f(*(tokens.shape if tokens is not None else (rows, 0))), f(rows), f(rows), torch.empty(rows, top, dtype=torch.int32, device=d), f(rows, top))
-        ws = torch.empty(need.value, dtype=torch.uint8, device=d) if need.value else None
-        p = lambda t: None if t is None or t.numel() == 0 else t.data_ptr()  # noqa: E731
-        _check(L.pv_token_logprobs(logits.data_ptr(), logits.stride(0), _DTYPES[logits.dtype], rows, vocab, p(tokens), n, p(got.logprobs), p(got.entropy), p(got.lse),
-                                   top, p(got.top_ids), p(got.top_logprobs), p(ws), need.value, s), "pv_token_logprobs")
-    return got
+        if not (isinstance(tokens, torch.Tensor) and tokens.device == logits.device and tokens.dtype == torch.int32 and tokens.dim() in (1, 2) and tokens.shape[0] == rows and tokens.is_contiguous()):
+            _refuse(where, f"tokens must be a contiguous int32 tensor [{rows}] or [{rows}, n] on {logits.device}")
+        shape, tp = tokens.shape, tokens.data_ptr()
+        n = 1 if len(shape) == 1 else shape[1]
+    L, key = lib(), (rows, vocab, top)
+    need = _logprobs_need.get(key)
+    if need is None:
+        b = ctypes.c_size_t()
+        _check(L.pv_token_logprobs_bytes(rows, vocab, top, ctypes.byref(b)), "pv_token_logprobs_bytes")
+        if len(_logprobs_need) > 256:
+            _logprobs_need.clear()
+        need = _logprobs_need[key] = b.value
+    lp = logits.new_empty(shape, dtype=torch.float32)
+    stats = logits.new_empty((2, rows), dtype=torch.float32)
+    ids, best = logits.new_empty((rows, top), dtype=torch.int32), logits.new_empty((rows, top), dtype=torch.float32)
+    entropy, lse = stats.unbind(0)
+    ws = logits.new_empty(need, dtype=torch.uint8) if need else None
+    rc = L.pv_token_logprobs(logits.data_ptr(), row_stride, _DTYPES[logits.dtype], rows, vocab, tp, n, lp.data_ptr(), entropy.data_ptr(), lse.data_ptr(),
+                             top, ids.data_ptr(), best.data_ptr(), None if ws is None else ws.data_ptr(), need, _raw_stream(index))
+    if rc:
+        _check(rc, "pv_token_logprobs")
+    return TokenLogprobs(lp, entropy, lse, ids, best)
