@@ -2,14 +2,24 @@
 //
 // The query rows of a kv head are packed token by token: row m of a sequence is query head m % group of its token m / group.  Everything is computed transposed, as in the
 // attention over 16-bit pages: S^T (keys x rows) = K Q^T, O^T (features x rows) = V^T P^T; the accumulators of S^T are, two groups of 16 keys side by side, the second
-// operand of the other product.  Codes become bf16 in registers, scale included (v_cvt_scalef32_pk_bf16_fp8: two codes an instruction, exact), so that any
-// magnitude of keys and values is what it stands for.  Softmax with the running maximum and sum, all in 32 bits, in powers of two.
-// P is carried as bf16 hi + lo: rounded to one bf16 it would add as much error as the rounding of a bf16 output and eight times that of an f16 one; one f16 has no room
-// for the weights of many keys beside one that takes nearly all.  q is exact: bf16 as it is, f16 as bf16 hi + lo.
+// operand of the other product.  Softmax with the running maximum and sum, all in 32 bits, in powers of two.
+//
+// Types of the products (codes become 16-bit numbers two an instruction, exactly):
+//   K   bf16 with its scale (a bf16 q has bf16's range), or f16 without, the scale then multiplying the scores (f16 q).  A step's q is a bf16 pair, two products.
+//   V   f16 without its scale.  P = 2^15 times the weight, f16: 11 significant bits for weights from 2^-29 on, so that many small ones beside one that takes nearly all count fully; one bf16
+//       would add as much error as the rounding of a bf16 output.  For f16 outputs P is a pair of f16, or its rounding would be as large as theirs (in a step, whose keys and values have four bits, one is enough).
+//       V's scales 2^ev go into the weights' exponents, relative to the unit of the accumulators, 2^E, the largest so far; where one is below 2^-14 of that, the
+//       groups of 16 keys are gone through one after the other, each in its own unit.  (Of values whose scales are more than 2^100
+//       below others of their kv head little is left.)
+#include <atomic>
 #include <stddef.h>
 #include "pv_kv8.h"
 
 enum { KV8_BF16 = 0, KV8_F16 = 1, KV8_STEP1 = 2, KV8_STEP2 = 3 };       // queries and outputs: a caller's, or a model's step (operand layouts of 1 .. 8 rows and of more)
+template <int IO> struct kv8_types {
+    static constexpr bool half = IO == KV8_F16;                            // K and q in f16
+    static constexpr int NQ = IO >= KV8_STEP1 ? 2 : 1, NP = IO == KV8_F16 ? 2 : 1;
+};
 
 struct kv8_attn_args {
     kv8_pool pool;
@@ -21,7 +31,8 @@ struct kv8_attn_args {
     const uint16_t *q_hi, *q_lo; int q_rows; uint16_t *xop_o;              // a step's
     float *part_o, *part_ml;                // [row][query head][split][HD], [2] (maximum, sum)
     int group, n_q_heads, nsplit, chunk;    // chunk: keys a split, a multiple of 256
-    float scale2;                           // scale * log2(e)
+    float scale2;                           // |scale| log2(e), more than 0 (a scale of 0: 1, and q is 0)
+    uint32_t q_and, q_xor;                  // what q passes through: its sign is the scale's
 };
 
 // Rows of sequence s of the call, cheaply (kv8_seq_at has the rest)
@@ -59,13 +70,24 @@ __device__ inline int kv8_keys(const kv8_seq &s, int page_shift, int last, bool 
     return (int)min(want, there);
 }
 
-// Eight codes, two dwords of them with a scale each, as the bf16 operand of a product
-typedef __attribute__((ext_vector_type(2))) short kv8_s2;
-__device__ inline uint4 kv8_operand(uint32_t a, uint32_t b, float fa, float fb)
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+__device__ inline f32x4 mfma16h(uint4 a, uint4 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0); }
+
+// Codes as 16-bit numbers, four of a dword at a time: f16, and bf16 times a power of two
+__device__ inline uint2 kv8_f16(uint32_t c)
 {
-    return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, fa, false)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, fa, true)),
-                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, fb, false)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, fb, true)));
+    return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c, 1.f, false)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c, 1.f, true)));
 }
+__device__ inline uint2 kv8_bf16(uint32_t c, float f)
+{
+    return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, f, false)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, f, true)));
+}
+template <bool HALF> __device__ inline uint4 kv8_key(uint32_t a, uint32_t b, float f)
+{
+    const uint2 u = HALF ? kv8_f16(a) : kv8_bf16(a, f), v = HALF ? kv8_f16(b) : kv8_bf16(b, f);
+    return make_uint4(u.x, u.y, v.x, v.y);
+}
+template <bool HALF> __device__ inline f32x4 kv8_score(uint4 k, uint4 q, f32x4 s) { return HALF ? mfma16h(k, q, s) : mfma16(k, q, s); }
 
 // 0x80 in each byte of a dword of codes that is NaN
 __device__ inline uint32_t kv8_nans(uint32_t c)
@@ -93,14 +115,9 @@ __device__ inline void kv8_load_q(const kv8_attn_args &a, const kv8_row &r, int 
 #pragma unroll
     for (int ks = 0; ks < HD / 32; ++ks) {
         const int e = 64 * (ks >> 1) + 16 * g + 8 * (ks & 1);
-        if constexpr (IO == KV8_BF16) q[0][ks] = *(const uint4 *)(a.q + r.row * a.q_row_bytes + r.head * a.q_head_bytes + e * 2);
-        else if constexpr (IO == KV8_F16) {
+        if constexpr (NQ == 1) {
             const uint4 v = *(const uint4 *)(a.q + r.row * a.q_row_bytes + r.head * a.q_head_bytes + e * 2);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-            uint32_t h[4], l[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { const f16x2 x = __builtin_bit_cast(f16x2, w[i]); split2((float)x.x, (float)x.y, h[i], l[i]); }
-            q[0][ks] = make_uint4(h[0], h[1], h[2], h[3]); q[1][ks] = make_uint4(l[0], l[1], l[2], l[3]);
+            q[0][ks] = make_uint4((v.x & a.q_and) ^ a.q_xor, (v.y & a.q_and) ^ a.q_xor, (v.z & a.q_and) ^ a.q_xor, (v.w & a.q_and) ^ a.q_xor);
         } else {
             const size_t at = q_at(r.head, r.row, e, HD, a.q_rows);
             q[0][ks] = *(const uint4 *)(a.q_hi + at); q[1][ks] = *(const uint4 *)(a.q_lo + at);
@@ -118,49 +135,118 @@ __device__ inline void kv8_store4(const kv8_attn_args &a, int row, int head, int
     } else store_operand4<(IO == KV8_STEP1 ? 1 : 2)>(a.xop_o, a.n_q_heads * HD, row, head * HD + e, y, a.q_rows);
 }
 
-// Four groups of 16 keys on their way through a wave
-struct kv8_groups {
-    int page;                               // lane: physical page of group lane / 16, -1: none
-    int sub;                                // and the block in it
-    float fk, fv;                           // and its scales
-};
+// Running result for RT tiles of 16 rows: lane (g, jl) has row jl's maximum and its part of 2^15 times the sum, and features 16 e + 4 g .. + 3 of the output times 2^(15 - E)
+template <int HD, int RT> struct kv8_acc { f32x4 O[RT][HD / 16]; float m[RT], l[RT]; int E; };
+#define KV8_NO_SCALE (-1000)                // exponent of a group that does not exist
 
-// Running result for RT tiles of 16 rows: lane (g, jl) has row jl's maximum and its part of the sum, and features 16 e + 4 g .. + 3
-template <int HD, int RT> struct kv8_acc { f32x4 O[RT][HD / 16]; float m[RT], l[RT]; };
-
-// Scores of 64 keys -> weights (bf16 hi, lo) under the new maximum; what was there is scaled to it.  see(t, p): whether the lane's row of tile t may attend to key p.
-template <int HD, int RT, typename SEE>
-__device__ inline void kv8_softmax(kv8_acc<HD, RT> &A, f32x4 (&S)[RT][4], float scale2, bool edge, SEE see, uint32_t (&P)[RT][4][4])
+template <int HD, int RT> __device__ inline void kv8_begin(kv8_acc<HD, RT> &A)
 {
-    const int g = (threadIdx.x & 63) >> 4;
-    float keep[RT];
-    bool same = true;
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-        float mx = A.m[t];
+        A.m[t] = -INFINITY; A.l[t] = 0.f;
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
+        for (int e = 0; e < HD / 16; ++e) A.O[t][e] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+    A.E = KV8_NO_SCALE;
+}
+
+// The accumulators in another unit
+template <int HD, int RT> __device__ inline void kv8_unit_is(kv8_acc<HD, RT> &A, int E)
+{
+    if (A.E != KV8_NO_SCALE) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                S[t][q][r] *= scale2;
-                if (edge && !see(t, 16 * q + 4 * g + r)) S[t][q][r] = -INFINITY;
-                mx = fmaxf(mx, S[t][q][r]);
-            }
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+            for (int e = 0; e < HD / 16; ++e)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) A.O[t][e][r] = ldexpf(A.O[t][e][r], A.E - E);
+    }
+    A.E = E;
+}
+
+// V's exponents of four groups against the accumulators' unit, which grows with them: dv.  Where they are too far apart, `only` one group is looked at at a time, from 0 to 3 (-1: all).
+template <int HD, int RT> __device__ inline void kv8_units(kv8_acc<HD, RT> &A, const int (&ev)[4], int (&dv)[4], int &only)
+{
+    const int top = max(max(max(ev[0], ev[1]), max(ev[2], ev[3])), A.E);
+    if (only < 0) {
+        bool far = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) far = far || (ev[i] != KV8_NO_SCALE && ev[i] - top < -14);
+        if (far) only = 0;
+    }
+    const int mine = only == 0 ? ev[0] : only == 1 ? ev[1] : only == 2 ? ev[2] : ev[3], E = only < 0 ? top : mine == KV8_NO_SCALE ? A.E : max(mine, A.E - 100);
+    if (E != A.E) kv8_unit_is(A, E);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) dv[i] = ev[i] == KV8_NO_SCALE || (only >= 0 && i != only) ? 0 : max(ev[i] - E, -100);
+}
+
+// Which of 64 keys a row sees: those before `end`, without a mask; with one, those before len, and from there on those that the mask names, before nk.  Bit i: key p + i.
+__device__ inline uint64_t kv8_first(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; }
+__device__ inline uint64_t kv8_sees(bool masked, uint64_t mask, int p, int len, int end, int nk)
+{
+    uint64_t w = kv8_first(min(end, nk) - p);
+    if (masked) {
+        const int s = len - p;
+        const uint64_t m = s >= 64 ? 0ull : s >= 0 ? mask << s : s > -64 ? mask >> -s : 0ull;
+        w = (kv8_first(s) | m) & kv8_first(nk - p);
+    }
+    return w;
+}
+
+// Scores of 64 keys -> weights under the new maximum (P[tile][group]: keys 4 g .. + 3; PL: what f16 leaves of them, where that counts); what was there is scaled to it.  fk: K's scales where the scores lack them; see(t): which
+// of the keys from 4 g on the lane's row of tile t may attend to, a bit each.
+template <int HD, int RT, int IO, typename SEE>
+__device__ inline void kv8_softmax(kv8_acc<HD, RT> &A, f32x4 (&S)[RT][4], float scale2, const float (&fk)[4], bool edge, SEE see, const int (&dv)[4], uint2 (&P)[RT][4], uint2 (&PL)[RT][4])
+{
+    constexpr bool HALF = kv8_types<IO>::half;
+    float keep[RT], add[4], back[4];
+    bool same = true;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) { add[q] = (float)dv[q]; back[q] = kv8_pow2(-dv[q]); }
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float f = scale2 * fk[q];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) if (HALF) S[t][q][r] *= f;
+        }
+        if (edge) {
+            const uint64_t w = see(t);
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) S[t][q][r] = ((w >> (16 * q + r)) & 1) ? S[t][q][r] : -INFINITY;
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            mx = fmaxf(fmaxf(mx, fmaxf(S[t][q][0], S[t][q][1])), fmaxf(S[t][q][2], S[t][q][3]));
+        }
         mx = with_lane32(with_lane16(mx, op_max), op_max);
+        if (!HALF) mx *= scale2;
+        mx = fmaxf(mx, A.m[t]);
         const float ref = mx == -INFINITY ? 0.f : mx;                  // (nothing seen so far)
         keep[t] = __builtin_amdgcn_exp2f(A.m[t] - ref);
         same = same && keep[t] == 1.f;
         float ps = 0.f;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
+            const float c = (15.f - ref) + add[q];
             float p[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) { p[r] = __builtin_amdgcn_exp2f(S[t][q][r] - ref); ps += p[r]; }
-            split2(p[0], p[1], P[t][q][0], P[t][q][2]);
-            split2(p[2], p[3], P[t][q][1], P[t][q][3]);
+            for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(HALF ? S[t][q][r] + c : fmaf(S[t][q][r], scale2, c));
+            ps = fmaf((p[0] + p[1]) + (p[2] + p[3]), back[q], ps);
+            const f16x2 a = {(_Float16)p[0], (_Float16)p[1]}, b = {(_Float16)p[2], (_Float16)p[3]};
+            P[t][q] = make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
+            if constexpr (kv8_types<IO>::NP == 2) {
+                const f16x2 al = {(_Float16)(p[0] - (float)a.x), (_Float16)(p[1] - (float)a.y)}, bl = {(_Float16)(p[2] - (float)b.x), (_Float16)(p[3] - (float)b.y)};
+                PL[t][q] = make_uint2(__builtin_bit_cast(uint32_t, al), __builtin_bit_cast(uint32_t, bl));
+            }
         }
         A.l[t] = fmaf(A.l[t], keep[t], ps);
         A.m[t] = mx;
+        __builtin_amdgcn_sched_barrier(0);
     }
     if (!__all(same)) {
 #pragma unroll
@@ -172,12 +258,84 @@ __device__ inline void kv8_softmax(kv8_acc<HD, RT> &A, f32x4 (&S)[RT][4], float 
     }
 }
 
-// One workgroup: a kv head, a tile of 16 RT packed rows of a sequence, a chunk of its keys; the waves take 64 keys in turn and are joined through LDS at the end.
+// O += V^T P^T of 64 keys; v(u, e): tile e of groups 2 u and 2 u + 1, f16
+template <int HD, int RT, int IO, typename V>
+__device__ inline void kv8_output(kv8_acc<HD, RT> &A, const uint2 (&P)[RT][4], const uint2 (&PL)[RT][4], V v)
+{
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < HD / 16; ++e) {
+            const uint4 va = v(u, e);
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                A.O[t][e] = mfma16h(va, make_uint4(P[t][2 * u].x, P[t][2 * u].y, P[t][2 * u + 1].x, P[t][2 * u + 1].y), A.O[t][e]);
+                if constexpr (kv8_types<IO>::NP == 2) A.O[t][e] = mfma16h(va, make_uint4(PL[t][2 * u].x, PL[t][2 * u].y, PL[t][2 * u + 1].x, PL[t][2 * u + 1].y), A.O[t][e]);
+            }
+            if (e & 1) __builtin_amdgcn_sched_barrier(0);                // (or the codes of all tiles are converted first, and no registers are left)
+        }
+}
+
+// Values that are NaN are kept from the rows that do not see them: the products are made without (kv8_without_nans), and in the end the outputs of rows that see one become NaN.  64 keys; v(q, b): a
+// lane's 16 codes of group q.
+template <int HD, int RT, typename SEE, typename V>
+__device__ inline void kv8_put_nans(kv8_acc<HD, RT> &A, SEE see, V v)
+{
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        uint4 seen[RT];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            const uint64_t w = see(t);
+            auto two = [&](int i) { const int o = 16 * (2 * u + i / 2) + 2 * (i & 1); return (uint32_t)((w >> o) & 1) * 0x3f80u | (uint32_t)((w >> (o + 1)) & 1) * 0x3f800000u; };
+            seen[t] = make_uint4(two(0), two(1), two(2), two(3));
+        }
+#pragma unroll
+        for (int b = 0; b < HD / 64; ++b) {
+            const uint4 c0 = v(2 * u, b), c1 = v(2 * u + 1, b);
+            const uint32_t v0[4] = {c0.x, c0.y, c0.z, c0.w}, v1[4] = {c1.x, c1.y, c1.z, c1.w};
+#pragma unroll
+            for (int f4 = 0; f4 < 4; ++f4) {
+                const uint32_t n0 = kv8_nans(v0[f4]) >> 7, n1 = kv8_nans(v1[f4]) >> 7;          // 1 in each NaN byte
+                auto ones = [](uint32_t n, int at) { return ((n >> at) & 1u) * 0x3f80u | ((n >> (at + 8)) & 1u) * 0x3f800000u; };
+                const uint4 va = make_uint4(ones(n0, 0), ones(n0, 16), ones(n1, 0), ones(n1, 16));
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    const f32x4 c = mfma16(va, seen[t], (f32x4){0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) if (c[r] > 0.f) A.O[t][4 * b + f4][r] = __uint_as_float(0x7fc00000u);
+                }
+            }
+        }
+    }
+}
+__device__ inline uint32_t kv8_without_nans(uint32_t c) { return c & ~((kv8_nans(c) >> 7) * 0xffu); }
+// what of a dword of V's codes (tokens 4 g ...) lies before the end: n tokens of the group exist
+__device__ inline uint32_t kv8_there(int n, int g) { const int k = min(max(n - 4 * g, 0), 4); return k == 4 ? 0xffffffffu : (1u << (8 * k)) - 1; }
+
+// a row's output and lse, or its chunk's part of them
+template <int HD, int IO>
+__device__ inline void kv8_finish4(const kv8_attn_args &a, const kv8_row &w, int e, const float o[4], float M, float L, bool whole, int split)
+{
+    const size_t at = (size_t)w.row * a.n_q_heads + w.head;
+    if (whole) {
+        const float inv = L == 0.f ? 0.f : 1.f / L, y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+        kv8_store4<HD, IO>(a, w.row, w.head, e, y);
+        if (a.lse != nullptr && e == 0) a.lse[at] = L == 0.f ? -INFINITY : (M + __log2f(L)) * 0.69314718055994530942f;
+    } else {
+        *(float4 *)(a.part_o + (at * a.nsplit + split) * HD + e) = make_float4(o[0], o[1], o[2], o[3]);
+        if (e == 0) *(float2 *)(a.part_ml + (at * a.nsplit + split) * 2) = make_float2(M, L);
+    }
+}
+
+// Few rows: one workgroup is a kv head, a tile of 16 RT packed rows of a sequence, a chunk of its keys; the waves take 64 keys in turn, straight from memory to registers, and are joined
+// through LDS at the end.  Bound by the read of the codes: the next 64 keys' K is asked for when this one's scores are there, V when its products are.
 template <int HD, int RT, int IO>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 k_kv8_attn(const kv8_attn_args a)
 {
-    constexpr int KB = HD / 64, KS = HD / 32, ET = HD / 16, NQ = IO == KV8_BF16 ? 1 : 2, TR = 16 * RT, OS = 68;
+    constexpr int KB = HD / 64, KS = HD / 32, NQ = kv8_types<IO>::NQ, TR = 16 * RT, OS = 68;
+    constexpr bool HALF = kv8_types<IO>::half;
     __shared__ float2 sh_ml[4][TR];
     __shared__ float sh_o[4][TR][OS];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, jl = lane & 15, g = lane >> 4;
@@ -192,140 +350,146 @@ k_kv8_attn(const kv8_attn_args a)
     const int k0 = split * a.chunk, k1 = min(k0 + a.chunk, nk);
     if (k0 >= nk && split > 0) return;      // (a sequence without keys: split 0 writes its rows)
     const bool whole = nk <= a.chunk;
+    const int sure = a.mask != nullptr ? len : len + m0 / a.group + 1;     // keys before this one are seen by every row
 
+    // groups of 16 keys from p on: lane (i, jl) has group i's page (-1: none), its block in it, its scales' bytes
+    const uint64_t block = (uint64_t)HD << shift;                        // bytes of a head's keys in a page
+    int page = -1, sub = 0;
+    uint32_t bytes = 0;
+    auto pages = [&](int p0) {
+        const int p = p0 + 16 * g;
+        page = p < k1 ? kv8_page(sq, p >> shift) : -1;
+        sub = (p & ((1 << shift) - 1)) >> 4;
+    };
+    auto scales = [&]() { return page < 0 ? 0u : (uint32_t)*(const uint16_t *)(sq.pool.scales + kv8_scale(sq.pool, page, kvh, 0, sub)); };
+    uint4 kt[4][KB], vt[4][KB];
+    const uint8_t *from[4];
+    int bad = 0;
+    auto load_k = [&]() {
+        bad = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int pg = __builtin_amdgcn_readlane(page, 16 * i), sb = __builtin_amdgcn_readlane(sub, 16 * i);
+            if (pg < 0) bad |= 1 << i;
+            from[i] = sq.pool.codes + ((uint64_t)(uint32_t)max(pg, 0) * sq.pool.n_heads + kvh) * 2 * block + (uint32_t)(pg < 0 ? 0 : sb) * (16 * HD);
+#pragma unroll
+            for (int b = 0; b < KB; ++b) kt[i][b] = ((const uint4 *)from[i])[b * 64 + lane];
+        }
+    };
+    auto load_v = [&]() {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int b = 0; b < KB; ++b) vt[i][b] = ((const uint4 *)(from[i] + block))[b * 64 + lane];
+    };
+
+    int p0 = k0 + 64 * wave;
+    pages(p0);
     kv8_row row[RT];
     uint4 q[RT][NQ][KS];
     uint64_t vm[RT];
     kv8_acc<HD, RT> A;
+    kv8_begin(A);
+    if (p0 < k1) { bytes = scales(); load_k(); load_v(); }
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
         row[t] = kv8_row_at(a, sq, kvh, m0 + t * 16 + jl);
         kv8_load_q<HD, IO, NQ>(a, row[t], g, q[t]);
         vm[t] = a.mask != nullptr ? a.mask[row[t].row] : 0;
-        A.m[t] = -INFINITY; A.l[t] = 0.f;
-#pragma unroll
-        for (int e = 0; e < ET; ++e) A.O[t][e] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
-    const uint64_t block = (uint64_t)HD << shift;                        // bytes of a head's keys in a page
-    auto groups = [&](int p0) {
-        kv8_groups r;
-        const int p = p0 + 16 * g;
-        r.page = p < nk ? kv8_page(sq, p >> shift) : -1;
-        r.sub = (p & ((1 << shift) - 1)) >> 4;
-        return r;
-    };
-    auto scales = [&](kv8_groups &r) {
-        const uint32_t b = r.page < 0 ? 0x7f7fu : *(const uint16_t *)(sq.pool.scales + kv8_scale(sq.pool, r.page, kvh, 0, r.sub));
-        r.fk = kv8_pow2(kv8_byte(b & 0xffu) - 127); r.fv = kv8_pow2(kv8_byte(b >> 8) - 127);
-    };
-    for (int p0 = k0 + 64 * wave; p0 < k1; p0 += 256) {
-        kv8_groups G = groups(p0);
-        scales(G);
-        uint4 kt[4][KB], vt[4][KB];
-        int bad = 0;
+    auto sees = [&](int t, int p) { return kv8_sees(a.mask != nullptr, vm[t], p + 4 * g, len, len + row[t].j + 1, nk); };
+    bool spoilt = false;                    // NaN among values that not every row sees
+    int only = -1;
+    pages(p0 + 256);
+    while (p0 < k1) {
+        const bool more = p0 + 256 < k1;
+        const int miss = bad;
+        float fk[4];
+        int ev[4], dv[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int page = __builtin_amdgcn_readlane(G.page, 16 * i), sub = __builtin_amdgcn_readlane(G.sub, 16 * i);
-            if (page < 0) bad |= 1 << i;
-            const uint8_t *kb = sq.pool.codes + ((uint64_t)(uint32_t)max(page, 0) * sq.pool.n_heads + kvh) * 2 * block + sub * (16 * HD);
-#pragma unroll
-            for (int b = 0; b < KB; ++b) { kt[i][b] = ((const uint4 *)kb)[b * 64 + lane]; vt[i][b] = ((const uint4 *)(kb + block))[b * 64 + lane]; }
+            const uint32_t b = __builtin_amdgcn_readlane(bytes, 16 * i);
+            fk[i] = kv8_pow2(kv8_byte(b & 0xffu) - 127);
+            ev[i] = ((miss >> i) & 1) ? KV8_NO_SCALE : kv8_byte(b >> 8) - 127;
         }
         f32x4 S[RT][4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(G.fk), 16 * i));
 #pragma unroll
             for (int t = 0; t < RT; ++t) S[t][i] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int b = 0; b < KB; ++b) {
-                const uint4 ka = kv8_operand(kt[i][b].x, kt[i][b].y, f, f), kc = kv8_operand(kt[i][b].z, kt[i][b].w, f, f);
+                const uint4 ka = kv8_key<HALF>(kt[i][b].x, kt[i][b].y, fk[i]), kc = kv8_key<HALF>(kt[i][b].z, kt[i][b].w, fk[i]);
 #pragma unroll
                 for (int t = 0; t < RT; ++t)
 #pragma unroll
-                    for (int n = 0; n < NQ; ++n) { S[t][i] = mfma16(ka, q[t][n][2 * b], S[t][i]); S[t][i] = mfma16(kc, q[t][n][2 * b + 1], S[t][i]); }
+                    for (int n = 0; n < NQ; ++n) { S[t][i] = kv8_score<HALF>(ka, q[t][n][2 * b], S[t][i]); S[t][i] = kv8_score<HALF>(kc, q[t][n][2 * b + 1], S[t][i]); }
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
-        const bool edge = p0 + 64 > len || p0 + 64 > nk || bad != 0;
-        auto see = [&](int t, int o) {
-            const int p = p0 + o, slot = p - len;
-            const bool in = a.mask != nullptr ? slot < 0 || (slot < 64 && ((vm[t] >> slot) & 1)) : slot <= row[t].j;
-            return in && p < nk && !((bad >> (o >> 4)) & 1);
-        };
-        uint32_t P[RT][4][4];
-        kv8_softmax<HD, RT>(A, S, a.scale2, edge, see, P);
-        // values that do not exist are zeros; NaN among those that do is kept from the rows that do not see it: zero in the product, and added where a row does
-        bool nans = false;
-        if (edge) {
+        kv8_units(A, ev, dv, only);
+        const int without = miss | (only < 0 ? 0 : 15 & ~(1 << only));    // groups that are not looked at
+        const bool last_keys = p0 + 64 > sure || p0 + 64 > nk || miss != 0, edge = last_keys || without != 0;
+        uint64_t there = ~0ull;
+        if (without) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) if ((without >> i) & 1) there &= ~(0xffffull << (16 * i));
+        }
+        auto see = [&](int t) { return sees(t, p0) & there; };
+        uint2 P[RT][4], PL[RT][4];
+        const bool through = only < 0 || only == 3;
+        if (through && more) { bytes = scales(); load_k(); }
+        kv8_softmax<HD, RT, IO>(A, S, a.scale2, fk, edge, see, dv, P, PL);
+        if (last_keys) {
+            bool nans = false;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int n = ((bad >> i) & 1) ? 0 : min(max(nk - (p0 + 16 * i + 4 * g), 0), 4);
-                const uint32_t there = n == 4 ? 0xffffffffu : (1u << (8 * n)) - 1;
-                uint32_t any = 0;
+                const uint32_t there = ((miss >> i) & 1) ? 0u : kv8_there(nk - (p0 + 16 * i), g);
 #pragma unroll
                 for (int b = 0; b < KB; ++b) {
                     vt[i][b].x &= there; vt[i][b].y &= there; vt[i][b].z &= there; vt[i][b].w &= there;
-                    any |= kv8_nans(vt[i][b].x) | kv8_nans(vt[i][b].y) | kv8_nans(vt[i][b].z) | kv8_nans(vt[i][b].w);
+                    nans = nans || (kv8_nans(vt[i][b].x) | kv8_nans(vt[i][b].y) | kv8_nans(vt[i][b].z) | kv8_nans(vt[i][b].w)) != 0;
                 }
-                nans = nans || any != 0;
             }
-            nans = __any(nans);
-        }
-        if (nans) {
+            if (__any(nans)) {
+                spoilt = true;
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                uint32_t seen[RT][4];
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int t = 0; t < RT; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int o = 16 * (2 * u + i / 2) + 4 * g + 2 * (i & 1);
-                        seen[t][i] = (see(t, o) ? 0x3f80u : 0u) | (see(t, o + 1) ? 0x3f800000u : 0u);
-                    }
-#pragma unroll
-                for (int b = 0; b < KB; ++b) {
-                    uint32_t *v0 = &vt[2 * u][b].x, *v1 = &vt[2 * u + 1][b].x;
-#pragma unroll
-                    for (int f4 = 0; f4 < 4; ++f4) {
-                        const uint32_t n0 = kv8_nans(v0[f4]) >> 7, n1 = kv8_nans(v1[f4]) >> 7;          // 1 in each NaN byte
-                        v0[f4] &= ~(n0 * 0xffu); v1[f4] &= ~(n1 * 0xffu);
-                        auto ones = [](uint32_t n, int at) { return ((n >> at) & 1u) * 0x3f80u | ((n >> (at + 8)) & 1u) * 0x3f800000u; };
-                        const uint4 va = make_uint4(ones(n0, 0), ones(n0, 16), ones(n1, 0), ones(n1, 16));
-#pragma unroll
-                        for (int t = 0; t < RT; ++t) {
-                            const f32x4 c = mfma16(va, make_uint4(seen[t][0], seen[t][1], seen[t][2], seen[t][3]), (f32x4){0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) if (c[r] > 0.f) A.O[t][4 * b + f4][r] = __uint_as_float(0x7fc00000u);
-                        }
-                    }
-                }
+                    for (int b = 0; b < KB; ++b)
+                        vt[i][b] = make_uint4(kv8_without_nans(vt[i][b].x), kv8_without_nans(vt[i][b].y), kv8_without_nans(vt[i][b].z), kv8_without_nans(vt[i][b].w));
             }
         }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const float f0 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(G.fv), 32 * u)), f1 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(G.fv), 32 * u + 16));
-#pragma unroll
-            for (int b = 0; b < KB; ++b) {
-                const uint32_t v0[4] = {vt[2 * u][b].x, vt[2 * u][b].y, vt[2 * u][b].z, vt[2 * u][b].w}, v1[4] = {vt[2 * u + 1][b].x, vt[2 * u + 1][b].y, vt[2 * u + 1][b].z, vt[2 * u + 1][b].w};
-#pragma unroll
-                for (int f4 = 0; f4 < 4; ++f4) {
-                    const uint4 va = kv8_operand(v0[f4], v1[f4], f0, f1);
-#pragma unroll
-                    for (int t = 0; t < RT; ++t) {
-                        f32x4 &o = A.O[t][4 * b + f4];
-                        o = mfma16(va, make_uint4(P[t][2 * u][0], P[t][2 * u][1], P[t][2 * u + 1][0], P[t][2 * u + 1][1]), o);
-                        o = mfma16(va, make_uint4(P[t][2 * u][2], P[t][2 * u][3], P[t][2 * u + 1][2], P[t][2 * u + 1][3]), o);
-                    }
-                }
-            }
+        kv8_output<HD, RT, IO>(A, P, PL, [&](int u, int e) {
+            auto part = [&](int i) { const uint4 c = vt[i][e / 4]; return kv8_f16(e % 4 == 0 ? c.x : e % 4 == 1 ? c.y : e % 4 == 2 ? c.z : c.w); };
+            const uint2 x = part(2 * u), y = part(2 * u + 1);
+            return make_uint4(x.x, x.y, y.x, y.y);
+        });
+        if (!through) { ++only; continue; }
+        only = -1;
+        p0 += 256;
+        if (more) { load_v(); pages(p0 + 256); }
+    }
+    if (spoilt) {
+        for (p0 = k0 + 64 * wave; p0 < k1; p0 += 256) {
+            if (p0 + 64 <= sure && p0 + 64 <= nk) continue;
+            pages(p0);
+            kv8_put_nans<HD, RT>(A, [&](int t) { return sees(t, p0); }, [&](int i, int b) {
+                const int pg = __builtin_amdgcn_readlane(page, 16 * i), sb = __builtin_amdgcn_readlane(sub, 16 * i);
+                if (pg < 0) return make_uint4(0u, 0u, 0u, 0u);
+                const uint4 c = ((const uint4 *)(sq.pool.codes + (((uint64_t)(uint32_t)pg * sq.pool.n_heads + kvh) * 2 + 1) * block + (uint32_t)sb * (16 * HD)))[b * 64 + lane];
+                const uint32_t there = kv8_there(nk - (p0 + 16 * i), g);
+                return make_uint4(c.x & there, c.y & there, c.z & there, c.w & there);
+            });
         }
     }
 
     // join the waves: each parks its maximum and sum and, 64 features at a time, its output
+    const int E = A.E == KV8_NO_SCALE ? 0 : A.E;
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
         A.l[t] = with_lane32(with_lane16(A.l[t], op_add), op_add);
-        if (g == 0) sh_ml[wave][t * 16 + jl] = make_float2(A.m[t], A.l[t]);
+        if (g == 0) sh_ml[wave][t * 16 + jl] = make_float2(A.m[t], A.l[t] * 0x1p-15f);
     }
 #pragma unroll
     for (int part = 0; part < KB; ++part) {
@@ -333,43 +497,219 @@ k_kv8_attn(const kv8_attn_args a)
 #pragma unroll
         for (int t = 0; t < RT; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) *(f32x4 *)&sh_o[wave][t * 16 + jl][e * 16 + 4 * g] = A.O[t][4 * part + e];
+            for (int e = 0; e < 4; ++e) {
+                const f32x4 o = A.O[t][4 * part + e];
+                *(float4 *)&sh_o[wave][t * 16 + jl][e * 16 + 4 * g] = make_float4(ldexpf(o[0], E - 15), ldexpf(o[1], E - 15), ldexpf(o[2], E - 15), ldexpf(o[3], E - 15));
+            }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
             const int r = i * 16 + (threadIdx.x >> 4), c4 = threadIdx.x & 15;
             const kv8_row w = kv8_row_at(a, sq, kvh, m0 + r);
             if (!w.live) continue;
-            float M = -INFINITY, L = 0.f;
+            float M = -INFINITY, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < 4; ++k) M = fmaxf(M, sh_ml[k][r].x);
             const float ref = M == -INFINITY ? 0.f : M;
-            f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const float f = __builtin_amdgcn_exp2f(sh_ml[k][r].x - ref);
-                const f32x4 v = *(const f32x4 *)&sh_o[k][r][4 * c4];
-#pragma unroll
-                for (int x = 0; x < 4; ++x) o[x] = fmaf(f, v[x], o[x]);
+                const float4 v = *(const float4 *)&sh_o[k][r][4 * c4];
+                o[0] = fmaf(f, v.x, o[0]); o[1] = fmaf(f, v.y, o[1]); o[2] = fmaf(f, v.z, o[2]); o[3] = fmaf(f, v.w, o[3]);
                 L = fmaf(f, sh_ml[k][r].y, L);
             }
-            const size_t at = (size_t)w.row * a.n_q_heads + w.head;
-            if (whole) {
-                const float inv = L == 0.f ? 0.f : 1.f / L, y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-                kv8_store4<HD, IO>(a, w.row, w.head, part * 64 + 4 * c4, y);
-                if (a.lse != nullptr && part == 0 && c4 == 0) a.lse[at] = L == 0.f ? -INFINITY : (M + __log2f(L)) * 0.69314718055994530942f;
-            } else {
-                *(f32x4 *)(a.part_o + (at * a.nsplit + split) * HD + part * 64 + 4 * c4) = o;
-                if (part == 0 && c4 == 0) *(float2 *)(a.part_ml + (at * a.nsplit + split) * 2) = make_float2(M, L);
+            kv8_finish4<HD, IO>(a, w, part * 64 + 4 * c4, o, M, L, whole, split);
+        }
+    }
+}
+
+// Many rows: a workgroup is a kv head, 64 RT packed rows of a sequence (16 RT a wave), a chunk of its keys.  64 keys at a time go through LDS as 16-bit numbers: each wave asks for a
+// group of 16 two steps ahead and converts it one step ahead, once for all rows, while the products of this step run in the other wave of its SIMD.
+template <int HD, int RT>
+struct kv8_wide {
+    static constexpr int KS = HD / 32, ET = HD / 16;
+    static constexpr int buffer = 4 * KS * 64 + 2 * ET * 64;             // uint4 of 64 keys: K [group][ks][lane], V [pair][e][lane]
+    static constexpr int lds = 2 * buffer * 16 + 64;                     // and of each group its scales' bytes, and what is the matter with it
+};
+template <int HD, int RT, int IO>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
+k_kv8_attn_wide(const kv8_attn_args a)
+{
+    using W = kv8_wide<HD, RT>;
+    constexpr int KB = HD / 64, KS = W::KS, ET = W::ET, NQ = kv8_types<IO>::NQ, TR = 64 * RT;
+    constexpr bool HALF = kv8_types<IO>::half;
+    extern __shared__ uint4 wide_lds[];
+    int4 *about = (int4 *)(wide_lds + 2 * W::buffer);                    // [buffer]: a dword a group: scales' bytes, bit 16: does not exist, bit 17: NaN among its values
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, jl = lane & 15, g = lane >> 4;
+    const int kvh = blockIdx.x % a.pool.n_heads, split = blockIdx.y, units = gridDim.x / a.pool.n_heads;
+    int tile = 0;
+    // (the last tiles of a prompt have the most keys: they begin first)
+    const int si = __builtin_amdgcn_readfirstlane(kv8_unit(a.seqs, units - 1 - blockIdx.x / a.pool.n_heads, a.group, TR, tile));
+    if (si < 0) return;
+    const kv8_seq sq = kv8_seq_at<HD>(a.seqs, a.pool, si);
+    const int m0 = tile * TR, nrows = sq.rows * a.group, shift = sq.pool.page_shift;
+    const int last = (min(m0 + TR, nrows) - 1) / a.group;
+    const int nk = __builtin_amdgcn_readfirstlane(kv8_keys(sq, shift, last, a.mask != nullptr)), len = __builtin_amdgcn_readfirstlane(sq.len);
+    const int k0 = split * a.chunk, k1 = min(k0 + a.chunk, nk);
+    if (k0 >= nk && split > 0) return;
+    const bool whole = nk <= a.chunk;
+    const int sure = a.mask != nullptr ? len : len + m0 / a.group + 1;     // keys before this one are seen by every row
+    const int steps = (k1 - k0 + 63) >> 6;
+
+    // this wave's group of 16 keys of step s
+    const uint64_t block = (uint64_t)HD << shift;
+    auto page_of = [&](int s) { const int p = k0 + 64 * s + 16 * wave; return __builtin_amdgcn_readfirstlane(p < k1 ? kv8_page(sq, p >> shift) : -1); };
+    auto codes_of = [&](int page, int p) { return sq.pool.codes + ((uint64_t)(uint32_t)page * sq.pool.n_heads + kvh) * 2 * block + (uint32_t)((p & ((1 << shift) - 1)) >> 4) * (16 * HD); };
+    uint4 kt[KB], vt[KB];
+    uint32_t bytes = 0;
+    int page = -1;                           // of the group that the registers hold
+    auto load = [&](int s, int pg) {
+        page = pg;
+        if (pg < 0) return;
+        const int p = k0 + 64 * s + 16 * wave;
+        const uint8_t *at = codes_of(pg, p);
+        bytes = *(const uint16_t *)(sq.pool.scales + kv8_scale(sq.pool, pg, kvh, 0, (p & ((1 << shift) - 1)) >> 4));
+#pragma unroll
+        for (int b = 0; b < KB; ++b) { kt[b] = ((const uint4 *)at)[b * 64 + lane]; vt[b] = ((const uint4 *)(at + block))[b * 64 + lane]; }
+    };
+    auto convert = [&](int s, int buf) {
+        uint4 *L = wide_lds + buf * W::buffer;
+        uint4 *Lk = L + wave * KS * 64 + lane;
+        uint2 *Lv = (uint2 *)(L + 4 * KS * 64 + (wave >> 1) * ET * 64 + lane) + (wave & 1);
+        const int p = k0 + 64 * s + 16 * wave;
+        uint32_t what = page < 0 ? 1u << 16 : bytes;
+        if (page < 0) {
+#pragma unroll
+            for (int b = 0; b < KB; ++b) kt[b] = vt[b] = make_uint4(0u, 0u, 0u, 0u);
+        } else if (p + 16 > sure || p + 16 > nk) {
+            const uint32_t there = kv8_there(nk - p, g);
+            bool nans = false;
+#pragma unroll
+            for (int b = 0; b < KB; ++b) {
+                vt[b].x &= there; vt[b].y &= there; vt[b].z &= there; vt[b].w &= there;
+                nans = nans || (kv8_nans(vt[b].x) | kv8_nans(vt[b].y) | kv8_nans(vt[b].z) | kv8_nans(vt[b].w)) != 0;
             }
+            if (__any(nans)) {
+                what |= 1u << 17;
+#pragma unroll
+                for (int b = 0; b < KB; ++b) vt[b] = make_uint4(kv8_without_nans(vt[b].x), kv8_without_nans(vt[b].y), kv8_without_nans(vt[b].z), kv8_without_nans(vt[b].w));
+            }
+        }
+        const float f = kv8_pow2(kv8_byte(__builtin_amdgcn_readfirstlane(bytes) & 0xff) - 127);
+#pragma unroll
+        for (int b = 0; b < KB; ++b) {
+            Lk[(2 * b) * 64] = kv8_key<HALF>(kt[b].x, kt[b].y, f);
+            Lk[(2 * b + 1) * 64] = kv8_key<HALF>(kt[b].z, kt[b].w, f);
+            Lv[(4 * b) * 128] = kv8_f16(vt[b].x); Lv[(4 * b + 1) * 128] = kv8_f16(vt[b].y); Lv[(4 * b + 2) * 128] = kv8_f16(vt[b].z); Lv[(4 * b + 3) * 128] = kv8_f16(vt[b].w);
+        }
+        if (lane == 0) ((uint32_t *)(about + buf))[wave] = what;
+    };
+    auto sync = [&]() {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");             // (not for the loads on their way)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+
+    if (steps > 0) load(0, page_of(0));
+    kv8_row row[RT];
+    uint4 q[RT][NQ][KS];
+    uint64_t vm[RT];
+    kv8_acc<HD, RT> A;
+    kv8_begin(A);
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        row[t] = kv8_row_at(a, sq, kvh, m0 + (wave * RT + t) * 16 + jl);
+        kv8_load_q<HD, IO, NQ>(a, row[t], g, q[t]);
+        vm[t] = a.mask != nullptr ? a.mask[row[t].row] : 0;
+    }
+    auto sees = [&](int t, int p) { return kv8_sees(a.mask != nullptr, vm[t], p + 4 * g, len, len + row[t].j + 1, nk); };
+    bool spoilt = false;
+    int only = -1;
+    int next = page_of(1);
+    if (steps > 0) {
+        convert(0, 0);
+        if (steps > 1) { load(1, next); next = page_of(2); }
+        sync();
+    }
+    for (int s = 0; s < steps;) {
+        const int buf = s & 1, p0 = k0 + 64 * s;
+        if (only < 0 && s + 1 < steps) {
+            convert(s + 1, buf ^ 1);
+            if (s + 2 < steps) { load(s + 2, next); next = page_of(s + 3); }
+        }
+        const uint4 *Lk = wide_lds + buf * W::buffer + lane, *Lv = Lk + 4 * KS * 64;
+        const int4 ab = about[buf];
+        const uint32_t what[4] = {(uint32_t)__builtin_amdgcn_readfirstlane(ab.x), (uint32_t)__builtin_amdgcn_readfirstlane(ab.y), (uint32_t)__builtin_amdgcn_readfirstlane(ab.z), (uint32_t)__builtin_amdgcn_readfirstlane(ab.w)};
+        int miss = 0, ev[4], dv[4];
+        float fk[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (what[i] & 0x10000u) miss |= 1 << i;
+            spoilt = spoilt || (what[i] & 0x20000u);
+            fk[i] = kv8_pow2(kv8_byte(what[i] & 0xffu) - 127);
+            ev[i] = (what[i] & 0x10000u) ? KV8_NO_SCALE : kv8_byte((what[i] >> 8) & 0xffu) - 127;
+        }
+        f32x4 S[RT][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int t = 0; t < RT; ++t) S[t][i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const uint4 k = Lk[(i * KS + ks) * 64];
+#pragma unroll
+                for (int t = 0; t < RT; ++t)
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) S[t][i] = kv8_score<HALF>(k, q[t][n][ks], S[t][i]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        kv8_units(A, ev, dv, only);
+        const int without = miss | (only < 0 ? 0 : 15 & ~(1 << only));    // groups that are not looked at
+        const bool last_keys = p0 + 64 > sure || p0 + 64 > nk || miss != 0, edge = last_keys || without != 0;
+        uint64_t there = ~0ull;
+        if (without) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) if ((without >> i) & 1) there &= ~(0xffffull << (16 * i));
+        }
+        auto see = [&](int t) { return sees(t, p0) & there; };
+        uint2 P[RT][4], PL[RT][4];
+        kv8_softmax<HD, RT, IO>(A, S, a.scale2, fk, edge, see, dv, P, PL);
+        kv8_output<HD, RT, IO>(A, P, PL, [&](int u, int e) { return Lv[(u * ET + e) * 64]; });
+        if (only >= 0 && only < 3) { ++only; continue; }                 // (all waves alike: the exponents are the same for them)
+        only = -1;
+        ++s;
+        sync();
+    }
+    if (spoilt) {
+        for (int p0 = k0; p0 < k1; p0 += 64) {
+            if (p0 + 64 <= sure && p0 + 64 <= nk) continue;
+            kv8_put_nans<HD, RT>(A, [&](int t) { return sees(t, p0); }, [&](int i, int b) {
+                const int p = p0 + 16 * i, pg = p < k1 ? kv8_page(sq, p >> shift) : -1;
+                if (pg < 0) return make_uint4(0u, 0u, 0u, 0u);
+                const uint4 c = ((const uint4 *)(codes_of(pg, p) + block))[b * 64 + lane];
+                const uint32_t there = kv8_there(nk - p, g);
+                return make_uint4(c.x & there, c.y & there, c.z & there, c.w & there);
+            });
+        }
+    }
+    const int E = A.E == KV8_NO_SCALE ? 0 : A.E;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        const float L = with_lane32(with_lane16(A.l[t], op_add), op_add) * 0x1p-15f;
+        if (!row[t].live) continue;
+#pragma unroll
+        for (int e = 0; e < ET; ++e) {
+            const float o[4] = {ldexpf(A.O[t][e][0], E - 15), ldexpf(A.O[t][e][1], E - 15), ldexpf(A.O[t][e][2], E - 15), ldexpf(A.O[t][e][3], E - 15)};
+            kv8_finish4<HD, IO>(a, row[t], e * 16 + 4 * g, o, A.m[t], L, whole, split);
         }
     }
 }
 
 // The chunks of a row's keys joined: a wave a row and query head
-template <int HD, int TR, int IO>
+template <int HD, int IO>
 __global__ void __launch_bounds__(256)
-k_kv8_attn_merge(const kv8_attn_args a)
+k_kv8_attn_merge(const kv8_attn_args a, int TR)
 {
     constexpr int TPC = HD / 4, NG = 64 / TPC;
     const int lane = threadIdx.x & 63;
@@ -411,16 +751,17 @@ k_kv8_attn_merge(const kv8_attn_args a)
 
 // ------------------------------- host side ----------------------------------------
 
-// How a call's work is cut
-struct kv8_plan { int rt, units, nsplit, chunk; };
+// How a call's work is cut: rows a tile, by the mean of a sequence's packed rows (what each has is on the device); chunks of keys until the chip is full
+struct kv8_plan { int tr, units, nsplit, chunk; };
 
 static kv8_plan plan(int n_seq, int n_rows, int group, int kv_heads, int64_t keys)
 {
     kv8_plan p;
-    p.rt = (int64_t)n_rows * group > (int64_t)16 * n_seq ? 2 : 1;
-    p.units = (int)(((int64_t)n_rows * group) / (16 * p.rt)) + n_seq;
-    const int64_t base = (int64_t)p.units * kv_heads, most = (keys + 255) / 256;
-    int64_t n = (2048 + base - 1) / base;
+    const int64_t packed = (int64_t)n_rows * group;
+    p.tr = packed <= (int64_t)16 * n_seq ? 16 : packed <= (int64_t)64 * n_seq ? 64 : 128;
+    p.units = (int)(packed / p.tr) + n_seq;
+    const int64_t base = (int64_t)p.units * kv_heads, most = (keys + 255) / 256, want = p.tr == 16 ? 2048 : 1024;
+    int64_t n = (want + base - 1) / base;
     n = n < most ? n : most;
     n = n < 256 ? n : 256;
     n = n > 1 ? n : 1;
@@ -456,21 +797,38 @@ extern "C" int pv_kv8_attention_bytes(const pv_kv8_pool *pool, const pv_kv8_seqs
     return PV_OK;
 }
 
-template <int HD, int RT, int IO>
-static int launch2(const kv8_attn_args &a, const kv8_plan &p, hipStream_t s)
+// more dynamic LDS than the default limit: allowed once on each device
+template <int HD, int IO>
+static int allow_lds()
 {
-    k_kv8_attn<HD, RT, IO><<<dim3(p.units * a.pool.n_heads, p.nsplit), 256, 0, s>>>(a);
-    PV_HIP(hipGetLastError());
-    if (p.nsplit > 1) {
-        const int64_t waves = (int64_t)a.seqs.n_rows * a.n_q_heads;
-        k_kv8_attn_merge<HD, 16 * RT, IO><<<(unsigned)((waves + 3) / 4), 256, 0, s>>>(a);
-        PV_HIP(hipGetLastError());
-    }
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    PV_HIP(hipGetDevice(&dev));
+    const uint64_t bit = 1ull << (dev & 63);
+    if (dev < 64 && (done.load(std::memory_order_acquire) & bit)) return PV_OK;
+    PV_HIP(hipFuncSetAttribute((const void *)k_kv8_attn_wide<HD, 1, IO>, hipFuncAttributeMaxDynamicSharedMemorySize, kv8_wide<HD, 1>::lds));
+    PV_HIP(hipFuncSetAttribute((const void *)k_kv8_attn_wide<HD, 2, IO>, hipFuncAttributeMaxDynamicSharedMemorySize, kv8_wide<HD, 2>::lds));
+    if (dev < 64) done.fetch_or(bit, std::memory_order_release);
     return PV_OK;
 }
 
 template <int HD, int IO>
-static int launch(const kv8_attn_args &a, const kv8_plan &p, hipStream_t s) { return p.rt == 1 ? launch2<HD, 1, IO>(a, p, s) : launch2<HD, 2, IO>(a, p, s); }
+static int launch(const kv8_attn_args &a, const kv8_plan &p, hipStream_t s)
+{
+    const dim3 grid(p.units * a.pool.n_heads, p.nsplit);
+    if (p.tr == 16) k_kv8_attn<HD, 1, IO><<<grid, 256, 0, s>>>(a);
+    else {
+        if (kv8_wide<HD, 1>::lds > 65536) { const int rc = allow_lds<HD, IO>(); if (rc != PV_OK) return rc; }
+        if (p.tr == 64) k_kv8_attn_wide<HD, 1, IO><<<grid, 256, kv8_wide<HD, 1>::lds, s>>>(a);
+        else k_kv8_attn_wide<HD, 2, IO><<<grid, 256, kv8_wide<HD, 2>::lds, s>>>(a);
+    }
+    PV_HIP(hipGetLastError());
+    if (p.nsplit == 1) return PV_OK;
+    const int64_t waves = (int64_t)a.seqs.n_rows * a.n_q_heads;
+    k_kv8_attn_merge<HD, IO><<<(unsigned)((waves + 3) / 4), 256, 0, s>>>(a, p.tr);
+    PV_HIP(hipGetLastError());
+    return PV_OK;
+}
 
 extern "C" int pv_kv8_attention(const pv_kv8_pool *pool, const pv_kv8_seqs *seqs, const void *q, int64_t q_row_stride, int64_t q_head_stride, int32_t n_q_heads,
                                 const uint64_t *mask, float scale, void *out, int64_t out_row_stride, int64_t out_head_stride, float *lse, int32_t dtype,
@@ -494,7 +852,8 @@ extern "C" int pv_kv8_attention(const pv_kv8_pool *pool, const pv_kv8_seqs *seqs
     a.out = (char *)out; a.out_row_bytes = out_row_stride * 2; a.out_head_bytes = out_head_stride * 2;
     a.lse = lse; a.mask = mask; a.group = group; a.n_q_heads = n_q_heads; a.nsplit = p.nsplit; a.chunk = p.chunk;
     a.part_o = (float *)workspace; a.part_ml = a.part_o + (size_t)seqs->n_rows * n_q_heads * p.nsplit * pool->head_dim;
-    a.scale2 = scale * 1.44269504088896340736f;
+    a.scale2 = scale == 0.f ? 1.f : fabsf(scale) * 1.44269504088896340736f;
+    a.q_and = scale == 0.f ? 0u : ~0u; a.q_xor = scale < 0.f ? 0x80008000u : 0u;
     hipStream_t s = (hipStream_t)hip_stream;
     if (pool->head_dim == 128) return dtype == PV_BF16 ? launch<128, KV8_BF16>(a, p, s) : launch<128, KV8_F16>(a, p, s);
     return dtype == PV_BF16 ? launch<64, KV8_BF16>(a, p, s) : launch<64, KV8_F16>(a, p, s);
