@@ -35,32 +35,46 @@ struct kv8_attn_args {
     uint32_t q_and, q_xor;                  // what q passes through: its sign is the scale's
 };
 
-// Rows of sequence s of the call, cheaply (kv8_seq_at has the rest)
-__device__ inline int kv8_rows_of(const kv8_seqs &q, int s)
+// A lane's value added to those of the lanes before it
+__device__ inline int kv8_sums(int v)
 {
-    if (q.st != nullptr) return q.batched ? q.st->blk.seq[s].gamma : q.n_rows;
-    const int r0 = q.row_start[s], r = min(q.row_start[s + 1], q.n_rows) - r0;
-    return r0 < 0 || r < 0 || q.prefix_len[s] < 0 ? 0 : r;
+#define KV8_STEP(C, M) v += __builtin_amdgcn_update_dpp(0, v, C, M, 0xF, false)
+    KV8_STEP(0x111, 0xF); KV8_STEP(0x112, 0xF); KV8_STEP(0x114, 0xF); KV8_STEP(0x118, 0xF);      // within 16 lanes
+    KV8_STEP(0x142, 0xA); KV8_STEP(0x143, 0xC);                                                  // lane 15 to the next 16, lane 31 to the upper half
+#undef KV8_STEP
+    return v;
 }
 
-// Tile `unit` of the sequences' rows, TR packed rows a tile, counted through all sequences: its sequence (-1: there are not so many) and its number in it
-__device__ inline int kv8_unit(const kv8_seqs &q, int unit, int group, int TR, int &tile)
+// Tile `unit` of the sequences' rows, TR packed rows a tile, counted through all sequences: its sequence and its number in it (false: there are not so many).  A sequence's tables are asked for
+// at once, 64 sequences at a time: one trip to memory in most calls.
+template <int HD, int TR> __device__ inline bool kv8_unit(const kv8_seqs &q, const kv8_pool &own, int unit, int group, kv8_seq &s, int &tile)
 {
-    const int n = q.st != nullptr ? (q.batched ? q.st->blk.n_seq : 1) : q.n_seq, lane = threadIdx.x & 63;
-    for (int k = 0; k < n; k += 64) {
-        const int mine = k + lane < n ? (kv8_rows_of(q, k + lane) * group + TR - 1) / TR : 0;
-        int upto = mine;                    // tiles up to this sequence
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) { const int o = __shfl_up(upto, d, 64); if (lane >= d) upto += o; }
+    const int lane = threadIdx.x & 63;
+    if (q.st != nullptr) {
+        if (!q.batched) { s = kv8_seq_at<HD>(q, own, 0); tile = unit; return tile * TR < s.rows * group; }
+        const int mine = lane < q.n_seq ? (q.st->blk.seq[lane].gamma * group + TR - 1) / TR : 0, upto = kv8_sums(mine);
+        const uint64_t past = __ballot(upto > unit);
+        if (!past) return false;
+        const int l = __ffsll((unsigned long long)past) - 1;
+        tile = unit - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l));
+        s = kv8_seq_at<HD>(q, own, l);
+        return true;
+    }
+    for (int k = 0; k < q.n_seq; k += 64) {
+        const int i = min(k + lane, q.n_seq - 1), r0 = q.row_start[i], r1 = q.row_start[i + 1], len = q.prefix_len[i], r = min(r1, q.n_rows) - r0;
+        const int rows = k + lane >= q.n_seq || r0 < 0 || r < 0 || len < 0 ? 0 : r;
+        const int mine = (rows * group + TR - 1) / TR, upto = kv8_sums(mine);
         const uint64_t past = __ballot(upto > unit);
         if (past) {
             const int l = __ffsll((unsigned long long)past) - 1;
             tile = unit - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l));
-            return k + l;
+            s.pool = own; s.table = q.page_table + (size_t)(k + l) * q.table_pages; s.table_pages = q.table_pages;
+            s.row0 = __builtin_amdgcn_readlane(r0, l); s.rows = __builtin_amdgcn_readlane(rows, l); s.len = __builtin_amdgcn_readlane(len, l);
+            return true;
         }
         unit -= __builtin_amdgcn_readlane(upto, 63);
     }
-    return -1;
+    return false;
 }
 
 // Keys that exist for a sequence, and those that some row of the tile that ends with token `last` may see
@@ -341,9 +355,8 @@ k_kv8_attn(const kv8_attn_args a)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, jl = lane & 15, g = lane >> 4;
     const int kvh = blockIdx.x % a.pool.n_heads, split = blockIdx.y;       // (the tiles and chunks of a head: on one XCD where the heads are a multiple of eight)
     int tile = 0;
-    const int si = __builtin_amdgcn_readfirstlane(kv8_unit(a.seqs, blockIdx.x / a.pool.n_heads, a.group, TR, tile));
-    if (si < 0) return;
-    const kv8_seq sq = kv8_seq_at<HD>(a.seqs, a.pool, si);
+    kv8_seq sq;
+    if (!kv8_unit<HD, TR>(a.seqs, a.pool, blockIdx.x / a.pool.n_heads, a.group, sq, tile)) return;
     const int m0 = tile * TR, nrows = sq.rows * a.group, shift = sq.pool.page_shift;
     const int last = (min(m0 + TR, nrows) - 1) / a.group;
     const int nk = __builtin_amdgcn_readfirstlane(kv8_keys(sq, shift, last, a.mask != nullptr)), len = __builtin_amdgcn_readfirstlane(sq.len);
@@ -352,55 +365,58 @@ k_kv8_attn(const kv8_attn_args a)
     const bool whole = nk <= a.chunk;
     const int sure = a.mask != nullptr ? len : len + m0 / a.group + 1;     // keys before this one are seen by every row
 
-    // groups of 16 keys from p on: lane (i, jl) has group i's page (-1: none), its block in it, its scales' bytes
+    // the four groups of 16 keys from p0 on: their pages (-1: none), known two turns ahead, and, in lanes 16 i .., group i's scales' bytes
     const uint64_t block = (uint64_t)HD << shift;                        // bytes of a head's keys in a page
-    int page = -1, sub = 0;
+    int page[4];
     uint32_t bytes = 0;
     auto pages = [&](int p0) {
-        const int p = p0 + 16 * g;
-        page = p < k1 ? kv8_page(sq, p >> shift) : -1;
-        sub = (p & ((1 << shift) - 1)) >> 4;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) page[i] = kv8_entry(sq, (p0 + 16 * i) >> shift);
     };
-    auto scales = [&]() { return page < 0 ? 0u : (uint32_t)*(const uint16_t *)(sq.pool.scales + kv8_scale(sq.pool, page, kvh, 0, sub)); };
+    auto exists = [&](int p0, int i) { return (int)(p0 + 16 * i < k1) & (int)kv8_is_page(sq, page[i]); };       // (k1 does not lie behind the table's end)
     uint4 kt[4][KB], vt[4][KB];
     const uint8_t *from[4];
     int bad = 0;
-    auto load_k = [&]() {
+    auto load_k = [&](int p0) {
         bad = 0;
+        int at[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { const int ok = exists(p0, i); bad |= (ok ^ 1) << i; at[i] = ok ? page[i] : 0; }
+        const int mine = g == 0 ? at[0] : g == 1 ? at[1] : g == 2 ? at[2] : at[3], sub = ((p0 + 16 * g) & ((1 << shift) - 1)) >> 4;
+        bytes = *(const uint16_t *)(sq.pool.scales + kv8_scale(sq.pool, mine, kvh, 0, sub));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int pg = __builtin_amdgcn_readlane(page, 16 * i), sb = __builtin_amdgcn_readlane(sub, 16 * i);
-            if (pg < 0) bad |= 1 << i;
-            from[i] = sq.pool.codes + ((uint64_t)(uint32_t)max(pg, 0) * sq.pool.n_heads + kvh) * 2 * block + (uint32_t)(pg < 0 ? 0 : sb) * (16 * HD);
+            from[i] = uniform_ptr(sq.pool.codes + ((uint64_t)(uint32_t)at[i] * sq.pool.n_heads + kvh) * 2 * block + (uint32_t)(((p0 + 16 * i) & ((1 << shift) - 1)) >> 4) * (16 * HD));
 #pragma unroll
-            for (int b = 0; b < KB; ++b) kt[i][b] = ((const uint4 *)from[i])[b * 64 + lane];
+            for (int b = 0; b < KB; ++b) kt[i][b] = load_once((const uint4 *)from[i] + b * 64 + lane);
         }
     };
     auto load_v = [&]() {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int b = 0; b < KB; ++b) vt[i][b] = ((const uint4 *)(from[i] + block))[b * 64 + lane];
+            for (int b = 0; b < KB; ++b) vt[i][b] = load_once((const uint4 *)(from[i] + block) + b * 64 + lane);
     };
 
     int p0 = k0 + 64 * wave;
-    pages(p0);
+    if (p0 < k1) pages(p0);
     kv8_row row[RT];
     uint4 q[RT][NQ][KS];
     uint64_t vm[RT];
     kv8_acc<HD, RT> A;
     kv8_begin(A);
-    if (p0 < k1) { bytes = scales(); load_k(); load_v(); }
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
         row[t] = kv8_row_at(a, sq, kvh, m0 + t * 16 + jl);
         kv8_load_q<HD, IO, NQ>(a, row[t], g, q[t]);
         vm[t] = a.mask != nullptr ? a.mask[row[t].row] : 0;
     }
+    asm volatile("" ::: "memory");
+    if (p0 < k1) { load_k(p0); load_v(); }
     auto sees = [&](int t, int p) { return kv8_sees(a.mask != nullptr, vm[t], p + 4 * g, len, len + row[t].j + 1, nk); };
     bool spoilt = false;                    // NaN among values that not every row sees
     int only = -1;
-    pages(p0 + 256);
+    if (p0 < k1) pages(p0 + 256);
     while (p0 < k1) {
         const bool more = p0 + 256 < k1;
         const int miss = bad;
@@ -438,7 +454,7 @@ k_kv8_attn(const kv8_attn_args a)
         auto see = [&](int t) { return sees(t, p0) & there; };
         uint2 P[RT][4], PL[RT][4];
         const bool through = only < 0 || only == 3;
-        if (through && more) { bytes = scales(); load_k(); }
+        if (through && more) { load_k(p0 + 256); pages(p0 + 512); }
         kv8_softmax<HD, RT, IO>(A, S, a.scale2, fk, edge, see, dv, P, PL);
         if (last_keys) {
             bool nans = false;
@@ -468,16 +484,15 @@ k_kv8_attn(const kv8_attn_args a)
         if (!through) { ++only; continue; }
         only = -1;
         p0 += 256;
-        if (more) { load_v(); pages(p0 + 256); }
+        if (more) load_v();
     }
     if (spoilt) {
         for (p0 = k0 + 64 * wave; p0 < k1; p0 += 256) {
             if (p0 + 64 <= sure && p0 + 64 <= nk) continue;
             pages(p0);
             kv8_put_nans<HD, RT>(A, [&](int t) { return sees(t, p0); }, [&](int i, int b) {
-                const int pg = __builtin_amdgcn_readlane(page, 16 * i), sb = __builtin_amdgcn_readlane(sub, 16 * i);
-                if (pg < 0) return make_uint4(0u, 0u, 0u, 0u);
-                const uint4 c = ((const uint4 *)(sq.pool.codes + (((uint64_t)(uint32_t)pg * sq.pool.n_heads + kvh) * 2 + 1) * block + (uint32_t)sb * (16 * HD)))[b * 64 + lane];
+                if (!exists(p0, i)) return make_uint4(0u, 0u, 0u, 0u);
+                const uint4 c = ((const uint4 *)(sq.pool.codes + (((uint64_t)(uint32_t)page[i] * sq.pool.n_heads + kvh) * 2 + 1) * block + (uint32_t)(((p0 + 16 * i) & ((1 << shift) - 1)) >> 4) * (16 * HD)))[b * 64 + lane];
                 const uint32_t there = kv8_there(nk - (p0 + 16 * i), g);
                 return make_uint4(c.x & there, c.y & there, c.z & there, c.w & there);
             });
@@ -544,9 +559,8 @@ k_kv8_attn_wide(const kv8_attn_args a)
     const int kvh = blockIdx.x % a.pool.n_heads, split = blockIdx.y, units = gridDim.x / a.pool.n_heads;
     int tile = 0;
     // (the last tiles of a prompt have the most keys: they begin first)
-    const int si = __builtin_amdgcn_readfirstlane(kv8_unit(a.seqs, units - 1 - blockIdx.x / a.pool.n_heads, a.group, TR, tile));
-    if (si < 0) return;
-    const kv8_seq sq = kv8_seq_at<HD>(a.seqs, a.pool, si);
+    kv8_seq sq;
+    if (!kv8_unit<HD, TR>(a.seqs, a.pool, units - 1 - blockIdx.x / a.pool.n_heads, a.group, sq, tile)) return;
     const int m0 = tile * TR, nrows = sq.rows * a.group, shift = sq.pool.page_shift;
     const int last = (min(m0 + TR, nrows) - 1) / a.group;
     const int nk = __builtin_amdgcn_readfirstlane(kv8_keys(sq, shift, last, a.mask != nullptr)), len = __builtin_amdgcn_readfirstlane(sq.len);
@@ -558,15 +572,15 @@ k_kv8_attn_wide(const kv8_attn_args a)
 
     // this wave's group of 16 keys of step s
     const uint64_t block = (uint64_t)HD << shift;
-    auto page_of = [&](int s) { const int p = k0 + 64 * s + 16 * wave; return __builtin_amdgcn_readfirstlane(p < k1 ? kv8_page(sq, p >> shift) : -1); };
+    auto page_of = [&](int s) { const int p = k0 + 64 * s + 16 * wave; return kv8_entry(sq, p >> shift); };
     auto codes_of = [&](int page, int p) { return sq.pool.codes + ((uint64_t)(uint32_t)page * sq.pool.n_heads + kvh) * 2 * block + (uint32_t)((p & ((1 << shift) - 1)) >> 4) * (16 * HD); };
     uint4 kt[KB], vt[KB];
     uint32_t bytes = 0;
     int page = -1;                           // of the group that the registers hold
     auto load = [&](int s, int pg) {
-        page = pg;
-        if (pg < 0) return;
         const int p = k0 + 64 * s + 16 * wave;
+        page = p < k1 && kv8_is_page(sq, pg) ? pg : -1;
+        if (page < 0) return;
         const uint8_t *at = codes_of(pg, p);
         bytes = *(const uint16_t *)(sq.pool.scales + kv8_scale(sq.pool, pg, kvh, 0, (p & ((1 << shift) - 1)) >> 4));
 #pragma unroll
@@ -625,8 +639,9 @@ k_kv8_attn_wide(const kv8_attn_args a)
     auto sees = [&](int t, int p) { return kv8_sees(a.mask != nullptr, vm[t], p + 4 * g, len, len + row[t].j + 1, nk); };
     bool spoilt = false;
     int only = -1;
-    int next = page_of(1);
+    int next = 0;
     if (steps > 0) {
+        next = page_of(1);
         convert(0, 0);
         if (steps > 1) { load(1, next); next = page_of(2); }
         sync();
@@ -706,16 +721,26 @@ k_kv8_attn_wide(const kv8_attn_args a)
     }
 }
 
-// The chunks of a row's keys joined: a wave a row and query head
-template <int HD, int IO>
+// The chunks of a row's keys joined: WR waves (1, or 4 where the chunks are many) a row and query head, four chunks of each 4 HD bytes on their way a thread
+template <int HD, int IO, int WR>
 __global__ void __launch_bounds__(256)
 k_kv8_attn_merge(const kv8_attn_args a, int TR)
 {
-    constexpr int TPC = HD / 4, NG = 64 / TPC;
-    const int lane = threadIdx.x & 63;
-    const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    constexpr int TPC = HD / 4, NG = WR * (64 / TPC), FL = 4;
+    __shared__ float4 sh[4][TPC];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t id = WR == 4 ? blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
     const int row = __builtin_amdgcn_readfirstlane((int)(id / a.n_q_heads)), head = __builtin_amdgcn_readfirstlane((int)(id % a.n_q_heads));
     if (row >= a.seqs.n_rows) return;
+    const size_t at = (size_t)row * a.n_q_heads + head;
+    const float2 *ml = (const float2 *)(a.part_ml + at * a.nsplit * 2);
+    const int t = lane % TPC, cg = (WR == 4 ? wave * (64 / TPC) : 0) + lane / TPC;
+    const float *po = a.part_o + at * a.nsplit * HD + 4 * t;
+    // asked for beside the sequence's tables, whatever these turn out to say: the statistics of up to 64 chunks, and the first outputs
+    float2 one = ml[min(lane, a.nsplit - 1)];
+    float4 v[FL];
+#pragma unroll
+    for (int i = 0; i < FL; ++i) v[i] = *(const float4 *)(po + (size_t)min(cg + i * NG, a.nsplit - 1) * HD);
     const int si = __builtin_amdgcn_readfirstlane(kv8_seq_of_row(a.seqs, row));
     if (si < 0) return;
     const kv8_seq sq = kv8_seq_at<HD>(a.seqs, a.pool, si);
@@ -725,24 +750,38 @@ k_kv8_attn_merge(const kv8_attn_args a, int TR)
     const int nk = kv8_keys(sq, sq.pool.page_shift, last, a.mask != nullptr);
     if (nk <= a.chunk) return;              // (written already)
     const int n = (nk + a.chunk - 1) / a.chunk;
-    const size_t at = (size_t)row * a.n_q_heads + head;
-    const float2 *ml = (const float2 *)(a.part_ml + at * a.nsplit * 2);
-    const float *po = a.part_o + at * a.nsplit * HD;
-    float M = -INFINITY, L = 0.f;
-    for (int c = lane; c < n; c += 64) M = fmaxf(M, ml[c].x);
+    if (lane >= n) one = make_float2(-INFINITY, 0.f);
+    float M = one.x, L = 0.f;
+    for (int c = 64 + lane; c < n; c += 64) M = fmaxf(M, ml[c].x);
     M = over_wave(M, op_max);
     const float ref = M == -INFINITY ? 0.f : M;
-    for (int c = lane; c < n; c += 64) L = fmaf(ml[c].y, __builtin_amdgcn_exp2f(ml[c].x - ref), L);
+    L = one.y * __builtin_amdgcn_exp2f(one.x - ref);
+    for (int c = 64 + lane; c < n; c += 64) L = fmaf(ml[c].y, __builtin_amdgcn_exp2f(ml[c].x - ref), L);
     L = over_wave(L, op_add);
-    const int t = lane % TPC, cg = lane / TPC;
     float o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int c = cg; c < n; c += NG) {
-        const float w = __builtin_amdgcn_exp2f(ml[c].x - ref);
-        const float4 v = *(const float4 *)(po + (size_t)c * HD + 4 * t);
-        o[0] = fmaf(w, v.x, o[0]); o[1] = fmaf(w, v.y, o[1]); o[2] = fmaf(w, v.z, o[2]); o[3] = fmaf(w, v.w, o[3]);
+    for (int c0 = cg; c0 < n; c0 += FL * NG) {
+        if (c0 != cg) {
+#pragma unroll
+            for (int i = 0; i < FL; ++i) v[i] = *(const float4 *)(po + (size_t)min(c0 + i * NG, n - 1) * HD);
+        }
+#pragma unroll
+        for (int i = 0; i < FL; ++i) {
+            const int c = c0 + i * NG;
+            if (c < n) {                    // (others: anything)
+                const float w = __builtin_amdgcn_exp2f(ml[c].x - ref);
+                o[0] = fmaf(w, v[i].x, o[0]); o[1] = fmaf(w, v[i].y, o[1]); o[2] = fmaf(w, v[i].z, o[2]); o[3] = fmaf(w, v[i].w, o[3]);
+            }
+        }
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) { o[i] = with_lane32(o[i], op_add); if (TPC <= 16) o[i] = with_lane16(o[i], op_add); }
+    if (WR == 4) {
+        if (lane < TPC) sh[wave][lane] = make_float4(o[0], o[1], o[2], o[3]);
+        __syncthreads();
+        if (wave != 0) return;
+        const float4 x = sh[0][t], y = sh[1][t], z = sh[2][t], w = sh[3][t];
+        o[0] = (x.x + y.x) + (z.x + w.x); o[1] = (x.y + y.y) + (z.y + w.y); o[2] = (x.z + y.z) + (z.z + w.z); o[3] = (x.w + y.w) + (z.w + w.w);
+    }
     if (lane >= TPC) return;
     const float inv = L == 0.f ? 0.f : 1.f / L, y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
     kv8_store4<HD, IO>(a, row, head, 4 * t, y);
@@ -751,7 +790,9 @@ k_kv8_attn_merge(const kv8_attn_args a, int TR)
 
 // ------------------------------- host side ----------------------------------------
 
-// How a call's work is cut: rows a tile, by the mean of a sequence's packed rows (what each has is on the device); chunks of keys until the chip is full
+// How a call's work is cut.  Rows a tile, by the mean of a sequence's packed rows (what each has is on the device).  Chunks of keys until there are two workgroups a CU, all begun at once, or twice as many
+// where sequences of different lengths come out at different times: 4 rows over 65000 keys 31, 32, 39, 51 us with 256, 512, 1024, 2048 workgroups, 32 sequences of 256 .. 8192 keys 80, 64, 53, 57,
+// two prompts 540, 540, 583, 583 (128 rows a tile).
 struct kv8_plan { int tr, units, nsplit, chunk; };
 
 static kv8_plan plan(int n_seq, int n_rows, int group, int kv_heads, int64_t keys)
@@ -759,8 +800,8 @@ static kv8_plan plan(int n_seq, int n_rows, int group, int kv_heads, int64_t key
     kv8_plan p;
     const int64_t packed = (int64_t)n_rows * group;
     p.tr = packed <= (int64_t)16 * n_seq ? 16 : packed <= (int64_t)64 * n_seq ? 64 : 128;
-    p.units = (int)(packed / p.tr) + n_seq;
-    const int64_t base = (int64_t)p.units * kv_heads, most = (keys + 255) / 256, want = p.tr == 16 ? 2048 : 1024;
+    p.units = (int)((packed + (int64_t)n_seq * (p.tr - 1)) / p.tr);
+    const int64_t tiles = packed / p.tr > n_seq ? packed / p.tr : n_seq, base = tiles * kv_heads, most = (keys + 255) / 256, want = p.tr == 16 && n_seq > 1 ? 1024 : 512;
     int64_t n = (want + base - 1) / base;
     n = n < most ? n : most;
     n = n < 256 ? n : 256;
@@ -825,7 +866,8 @@ static int launch(const kv8_attn_args &a, const kv8_plan &p, hipStream_t s)
     PV_HIP(hipGetLastError());
     if (p.nsplit == 1) return PV_OK;
     const int64_t waves = (int64_t)a.seqs.n_rows * a.n_q_heads;
-    k_kv8_attn_merge<HD, IO><<<(unsigned)((waves + 3) / 4), 256, 0, s>>>(a, p.tr);
+    if (p.nsplit > 16) k_kv8_attn_merge<HD, IO, 4><<<(unsigned)waves, 256, 0, s>>>(a, p.tr);
+    else k_kv8_attn_merge<HD, IO, 1><<<(unsigned)((waves + 3) / 4), 256, 0, s>>>(a, p.tr);
     PV_HIP(hipGetLastError());
     return PV_OK;
 }

@@ -99,6 +99,16 @@ __device__ inline int kv8_page(const kv8_seq &s, int logical)
     return p >= 0 && p < s.pool.n_pages ? p : -1;
 }
 
+// The same for a whole wave in two parts, so that the load is on its way long before its use: an entry of a table of at least one page, by a scalar load (which does not wait for the vector loads
+// before it; behind the table's end: the last one), and whether it is a page
+__device__ inline int kv8_entry(const kv8_seq &s, int logical)
+{
+    typedef const __attribute__((address_space(4))) int32_t *table;
+    const int l = __builtin_amdgcn_readfirstlane(min(max(logical, 0), s.table_pages - 1));
+    return ((table)(uintptr_t)uniform_ptr(s.table))[l];
+}
+__device__ inline bool kv8_is_page(const kv8_seq &s, int entry) { return (uint32_t)entry < (uint32_t)s.pool.n_pages; }
+
 __device__ inline float kv8_pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }     // -127 < e < 128
 
 __device__ inline int kv8_byte(int b) { return min(max(b, 1), 253); }
