@@ -2,12 +2,13 @@
 //
 //   lse = M + ln Z, Z = sum e^(x - M), M = max x;  log p(t) = x_t - lse;  H = -sum p ln p = ln Z - sum e^(x - M) (x - M) / Z   (two terms that are not negative: nothing cancels)
 //
-// A workgroup reads a segment of a row once and keeps it in registers: every thread takes its own maximum, then sums, and the threads are joined by their maxima.  The
+// A workgroup reads a segment of a row once and keeps it in registers as it comes: every thread takes its own maximum, then sums, and the threads are joined by their maxima.  The
 // most probable tokens from the same registers: the threads' maxima, joined to 64 of them, are 64 different tokens, so that the k-th largest of these is a bound that k tokens reach and few others
 // do (k = 20: 24 are expected); those are written to LDS and each counts the better ones.  What keys are compared by: the value, then the lower index first; all different, so the result is
 // the same whatever order they come in.  Where the bound lets too many through (rows with many equal values, masked rows), k rounds of a plain arg-max.
-// Segments of a row are joined by a second kernel.  Bound by the read of the logits, and nearly as much by the exponentials (some ten cycles of a SIMD a number and 64 lanes).
-#include "pv_kernels_common.h"
+// Segments of a row are joined by a second kernel.  Bound by the read of the logits, and nearly as much by the exponentials: some nine instruction slots a number, so nothing else is done to
+// each; where sums come out as no numbers (masked logits, NaN), they are made again with care.
+#include "pv_matrix_common.h"
 
 #define LP_MAX_TOP 32
 #define LP_ROOM 512                         // tokens above the bound that LDS has room for
@@ -35,23 +36,12 @@ template <> __device__ inline float lp_one<float>(const char *p, int64_t i) { re
 template <> __device__ inline float lp_one<__bf16>(const char *p, int64_t i) { return pv_bf16_to_f32(((const uint16_t *)p)[i]); }
 template <> __device__ inline float lp_one<_Float16>(const char *p, int64_t i) { return (float)((const _Float16 *)p)[i]; }
 
+// Numbers as they lie in memory, dwords w of them: number i
 typedef __attribute__((ext_vector_type(2))) _Float16 lp_h2;
-template <typename T> __device__ inline void lp_load(const char *p, float *v);           // 16 bytes
-template <> __device__ inline void lp_load<float>(const char *p, float *v) { const float4 a = *(const float4 *)p; v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; }
-template <> __device__ inline void lp_load<__bf16>(const char *p, float *v)
-{
-    const uint4 a = *(const uint4 *)p;
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-}
-template <> __device__ inline void lp_load<_Float16>(const char *p, float *v)
-{
-    const uint4 a = *(const uint4 *)p;
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { const lp_h2 h = __builtin_bit_cast(lp_h2, w[i]); v[2 * i] = (float)h.x; v[2 * i + 1] = (float)h.y; }
-}
+template <typename T> __device__ inline float lp_get(const uint32_t *w, int i);
+template <> __device__ inline float lp_get<float>(const uint32_t *w, int i) { return __uint_as_float(w[i]); }
+template <> __device__ inline float lp_get<__bf16>(const uint32_t *w, int i) { return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16); }
+template <> __device__ inline float lp_get<_Float16>(const uint32_t *w, int i) { const lp_h2 h = __builtin_bit_cast(lp_h2, w[i >> 1]); return (float)(i & 1 ? h.y : h.x); }
 
 // Maximum, sum of 2^y, sum of 2^y y, y = (x - maximum) log2(e), of two sets
 struct lp_sums { float m, s, w; };
@@ -100,77 +90,122 @@ __device__ inline uint64_t lp_wave_best(uint64_t k)
     return k;
 }
 
-// NT threads, E numbers of a row each
-template <typename T, int NT, int E, bool ALIGNED>
-__global__ void __launch_bounds__(NT)
+// The best `top` of n <= 64 keys in LDS, in order: a lane a key, counting the better ones
+__device__ inline void lp_rank(const uint64_t *keys, int n, int top, uint64_t *best)
+{
+    const int lane = threadIdx.x & 63;
+    const uint64_t k = lane < n ? keys[lane] : 0;
+    const uint32_t lo = (uint32_t)k, hi = (uint32_t)(k >> 32);
+    int better = 0;
+    for (int j = 0; j < n; ++j) {
+        const uint64_t o = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, j) << 32 | (uint32_t)__builtin_amdgcn_readlane(lo, j);
+        better += o > k;
+    }
+    if (lane < n && better < top) best[better] = k;
+}
+
+// NT threads, E numbers of a row each, from the row's first address that is a multiple of 16 bytes on; the few numbers ahead of that belong to the first segment's first threads.
+template <typename T, int NT, int E>
+__global__ void __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(8, 8)))
 k_logprobs(const lp_args a)
 {
-    constexpr int V = ALIGNED ? 16 / (int)sizeof(T) : 1, U = E / V, NW = NT / 64;
+    constexpr int V = 16 / (int)sizeof(T), U = E / V, NW = NT / 64, D = E * (int)sizeof(T) / 4;
     __shared__ lp_sums sh_s[NW];
-    __shared__ uint32_t sh_max[NT];
+    __shared__ uint32_t sh_max[NT], sh_bound;
     __shared__ uint64_t sh_key[LP_ROOM], sh_best[LP_MAX_TOP];
     __shared__ int sh_n;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t row = blockIdx.x / a.segs;
-    const int seg = (int)(blockIdx.x - row * a.segs), base = seg * (NT * E);
+    const int seg = (int)(blockIdx.x - row * a.segs);
     const char *src = a.logits + row * a.row_bytes;
-    float x[E];
+    const int head = min((int)(((16u - ((uint32_t)(uintptr_t)src & 15u)) & 15u) / (uint32_t)sizeof(T)), a.vocab), base = head + seg * (NT * E);
+    uint32_t x[D];
     auto index = [&](int i) { return base + ((i / V) * NT + tid) * V + i % V; };
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int i0 = base + (u * NT + tid) * V;
-        if constexpr (V > 1) {
-            if (i0 + V <= a.vocab) { lp_load<T>(src + (int64_t)i0 * sizeof(T), x + u * V); continue; }
+        if (i0 + V <= a.vocab) {
+            const u32x4 v = __builtin_nontemporal_load((const u32x4 *)(src + (int64_t)i0 * sizeof(T)));
+            x[4 * u] = v.x; x[4 * u + 1] = v.y; x[4 * u + 2] = v.z; x[4 * u + 3] = v.w;
+        } else {
+            const uint32_t none = sizeof(T) == 4 ? 0xff800000u : __is_same(T, __bf16) ? 0xff80ff80u : 0xfc00fc00u;      // -infinity
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                x[4 * u + d] = none;
+                if constexpr (sizeof(T) == 4) { if (i0 + d < a.vocab) x[4 * u + d] = ((const uint32_t *)src)[i0 + d]; }
+                else {
+                    if (i0 + 2 * d < a.vocab) x[4 * u + d] = (none & 0xffff0000u) | ((const uint16_t *)src)[i0 + 2 * d];
+                    if (i0 + 2 * d + 1 < a.vocab) x[4 * u + d] = (x[4 * u + d] & 0xffffu) | (uint32_t)((const uint16_t *)src)[i0 + 2 * d + 1] << 16;
+                }
+            }
         }
-#pragma unroll
-        for (int e = 0; e < V; ++e) x[u * V + e] = i0 + e < a.vocab ? lp_one<T>(src, i0 + e) : -INFINITY;
     }
-    lp_sums t = {-INFINITY, 0.f, 0.f};
+    const bool first = seg == 0 && tid < head;
+    const float x0 = first ? lp_clean(lp_one<T>(src, tid)) : -INFINITY;
+    lp_sums t = {x0, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < E; ++i) { x[i] = lp_clean(x[i]); t.m = fmaxf(t.m, x[i]); }
-    const float ref = t.m == -INFINITY ? 0.f : t.m;
+    for (int i = 0; i < E; ++i) t.m = fmaxf(t.m, lp_get<T>(x, i));          // (of a number and NaN the number)
+#pragma unroll
+    for (int d = 0; d < D; ++d) if (sizeof(T) == 2) asm volatile("" : "+v"(x[d]));     // (taken apart anew each time: 32 bits of each number would be twice the registers)
+    const float ref = t.m == -INFINITY ? 0.f : t.m, c = -ref * 1.44269504088896340736f;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-        const float y = (x[i] - ref) * 1.44269504088896340736f, e = __builtin_amdgcn_exp2f(y);
+        const float y = fmaf(lp_get<T>(x, i), 1.44269504088896340736f, c), e = __builtin_amdgcn_exp2f(y);
         t.s += e;
-        t.w = fmaf(e, fmaxf(y, -256.f), t.w);                // (2^-256 is 0: keeps 0 * -infinity out)
+        t.w = fmaf(e, y, t.w);
+    }
+    if (__any(!(t.s < INFINITY && t.w == t.w))) {             // -infinity (its exponential, 0, times it is no number), NaN, +infinity, products over the largest number
+        t.s = t.m == INFINITY ? __uint_as_float(0x7fc00000u) : 0.f; t.w = t.s;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            const float y = fmaxf((lp_clean(lp_get<T>(x, i)) - ref) * 1.44269504088896340736f, -256.f), e = __builtin_amdgcn_exp2f(y);      // (2^-256 is 0)
+            t.s += e;
+            t.w = fmaf(e, y, t.w);
+            asm volatile("" : "+v"(t.s), "+v"(t.w));          // (one after the other: no registers for more)
+        }
+    }
+    {
+        const float y = fmaxf((x0 - ref) * 1.44269504088896340736f, -256.f), e = __builtin_amdgcn_exp2f(y);
+        t.s += e; t.w = fmaf(e, y, t.w);
     }
     const float mine = t.m;
     lp_over_wave(t);
     if (lane == 0) sh_s[wave] = t;
     if (a.top > 0) {
-        sh_max[tid] = index(0) < a.vocab ? lp_order(mine) : 0u;          // (a thread behind the row's end has no token)
+        sh_max[tid] = first || index(0) < a.vocab ? lp_order(mine + 0.f) : 0u;      // (a thread behind the row's end has no token)
         if (tid == 0) sh_n = 0;
+        if (tid < LP_MAX_TOP) sh_best[tid] = 0;
     }
     __syncthreads();
-    t = sh_s[0];
-#pragma unroll
-    for (int w = 1; w < NW; ++w) t.m = fmaxf(t.m, sh_s[w].m);
-    {
-        const float M = t.m;
-        t = {M, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < NW; ++w) { lp_sums o = sh_s[w]; lp_under(o, M); t.s += o.s; t.w += o.w; }
-    }
     if (a.top > 0) {
-        uint32_t g = 0;
+        if (wave == 0) {
+            uint32_t g = 0;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) { const uint32_t o = sh_max[w * 64 + lane]; g = o > g ? o : g; }
-        uint32_t bound = 0;                                   // the largest number that `top` of the 64 maxima reach
-        for (int b = 31; b >= 0; --b) { const uint32_t c = bound | 1u << b; if (__popcll(__ballot(g >= c)) >= a.top) bound = c; }
-        if (lp_order(mine) >= bound) {
+            for (int w = 0; w < NW; ++w) { const uint32_t o = sh_max[w * 64 + lane]; g = o > g ? o : g; }
+            uint32_t bound = 0;                               // the largest number, to 20 bits, that `top` of the 64 maxima reach
+#pragma unroll 4
+            for (int b = 31; b >= 12; --b) { const uint32_t n = bound | 1u << b; if (__popcll(__ballot(g >= n)) >= a.top) bound = n; }
+            if (lane == 0) sh_bound = bound;
+        }
+        __syncthreads();
+        const uint32_t bound = sh_bound;
+        auto keep = [&](uint64_t k) { const int at = atomicAdd(&sh_n, 1); if (at < LP_ROOM) sh_key[at] = k; };
+        if (lp_order(mine + 0.f) >= bound) {
+            if (first && lp_order(x0) >= bound) keep(lp_key(x0, tid));
 #pragma unroll
-            for (int i = 0; i < E; ++i)
-                if (lp_order(x[i]) >= bound && index(i) < a.vocab) { const int at = atomicAdd(&sh_n, 1); if (at < LP_ROOM) sh_key[at] = lp_key(x[i], index(i)); }
+            for (int i = 0; i < E; ++i) {
+                const float v = lp_clean(lp_get<T>(x, i));
+                if (lp_order(v) >= bound && index(i) < a.vocab) keep(lp_key(v, index(i)));
+            }
         }
         __syncthreads();
         const int n = sh_n;
-        if (tid < LP_MAX_TOP) sh_best[tid] = 0;
-        __syncthreads();
-        if (n <= LP_ROOM) {
+        if (n <= 64) { if (wave == 0) lp_rank(sh_key, n, a.top, sh_best); }
+        else if (n <= LP_ROOM) {
             for (int i = tid; i < n; i += NT) {
                 const uint64_t k = sh_key[i];
                 int better = 0;
+#pragma unroll 4
                 for (int j = 0; j < n; ++j) better += sh_key[j] > k;
                 if (better < a.top) sh_best[better] = k;
             }
@@ -179,7 +214,7 @@ k_logprobs(const lp_args a)
             for (int r = 0; r < a.top; ++r) {
                 uint64_t k = 0;
                 // (read again: in a loop over registers the keys would have to be kept as well)
-                for (int i = base + tid; i < min(base + NT * E, a.vocab); i += NT) { const uint64_t c = lp_key(lp_clean(lp_one<T>(src, i)), i); if (c < last && c > k) k = c; }
+                for (int i = (seg == 0 ? 0 : base) + tid; i < min(base + NT * E, a.vocab); i += NT) { const uint64_t o = lp_key(lp_clean(lp_one<T>(src, i)), i); if (o < last && o > k) k = o; }
                 k = lp_wave_best(k);
                 if (lane == 0) sh_key[wave] = k;
                 __syncthreads();
@@ -190,6 +225,14 @@ k_logprobs(const lp_args a)
             }
         }
         __syncthreads();
+    }
+    t = sh_s[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) t.m = fmaxf(t.m, sh_s[w].m);
+    {
+        const float M = t.m;
+        t = {M, 0.f, 0.f};
+        for (int w = 0; w < NW; ++w) { lp_sums o = sh_s[w]; lp_under(o, M); t.s += o.s; t.w += o.w; }
     }
     if (a.segs == 1) { lp_finish<T>(a, row, t, tid, NT, sh_best); return; }
     if (tid == 0) *(float4 *)(a.part + (row * a.segs + seg) * 4) = make_float4(t.m, t.s, t.w, 0.f);
@@ -250,12 +293,12 @@ extern "C" int pv_token_logprobs_bytes(int64_t rows, int32_t vocab, int32_t top,
     return PV_OK;
 }
 
-template <typename T, bool ALIGNED>
+template <typename T>
 static int launch(const lp_args &a, const lp_plan &p, hipStream_t s)
 {
     const unsigned grid = (unsigned)(a.rows * a.segs);
-    if (p.large) k_logprobs<T, 1024, 32, ALIGNED><<<grid, 1024, 0, s>>>(a);
-    else k_logprobs<T, 256, 16, ALIGNED><<<grid, 256, 0, s>>>(a);
+    if (p.large) k_logprobs<T, 1024, 32><<<grid, 1024, 0, s>>>(a);
+    else k_logprobs<T, 256, 16><<<grid, 256, 0, s>>>(a);
     PV_HIP(hipGetLastError());
     if (a.segs > 1) { k_logprobs_join<T><<<(unsigned)a.rows, 64, 0, s>>>(a); PV_HIP(hipGetLastError()); }
     return PV_OK;
@@ -283,9 +326,6 @@ extern "C" int pv_token_logprobs(const void *logits, int64_t row_stride, int32_t
     a.logits = (const char *)logits; a.row_bytes = row_stride * size; a.rows = rows; a.vocab = vocab; a.segs = p.segs;
     a.tokens = tokens; a.n_tokens = n_tokens; a.top = top; a.logprobs = logprobs; a.entropy = entropy; a.lse = lse; a.top_ids = top_ids; a.top_logprobs = top_logprobs;
     a.part = (float *)workspace; a.keys = (uint64_t *)((char *)workspace + (size_t)rows * p.segs * 16);
-    const bool aligned = !(((uintptr_t)logits | (uintptr_t)a.row_bytes) & 15);
     hipStream_t s = (hipStream_t)hip_stream;
-    if (dtype == PV_F32) return aligned ? launch<float, true>(a, p, s) : launch<float, false>(a, p, s);
-    if (dtype == PV_BF16) return aligned ? launch<__bf16, true>(a, p, s) : launch<__bf16, false>(a, p, s);
-    return aligned ? launch<_Float16, true>(a, p, s) : launch<_Float16, false>(a, p, s);
+    return dtype == PV_F32 ? launch<float>(a, p, s) : dtype == PV_BF16 ? launch<__bf16>(a, p, s) : launch<_Float16>(a, p, s);
 }
