@@ -4,7 +4,7 @@
 //
 // A workgroup reads a segment of a row once and keeps it in registers as it comes: every thread takes its own maximum, then sums, and the threads are joined by their maxima.  The
 // most probable tokens from the same registers: the threads' maxima, joined to 64 of them, are 64 different tokens, so that the k-th largest of these is a bound that k tokens reach and few others
-// do (k = 20: 24 are expected); those are written to LDS and each counts the better ones.  What keys are compared by: the value, then the lower index first; all different, so the result is
+// do (k = 20: 24 are expected); the threads that have them hand them over in LDS and each is compared with all.  What keys are compared by: the value, then the lower index first; all different, so the result is
 // the same whatever order they come in.  Where the bound lets too many through (rows with many equal values, masked rows), k rounds of a plain arg-max.
 // Segments of a row are joined by a second kernel.  Bound by the read of the logits, and nearly as much by the exponentials: some nine instruction slots a number, so nothing else is done to
 // each; where sums come out as no numbers (masked logits, NaN), they are made again with care.
@@ -13,6 +13,7 @@
 #define LP_MAX_TOP 32
 #define LP_ROOM 512                         // tokens above the bound that LDS has room for
 #define LP_MAX_SEGS 64
+#define LP_FEW 64                           // threads with such tokens that LDS has room for
 
 struct lp_args {
     const char *logits; int64_t row_bytes;
@@ -60,9 +61,16 @@ __device__ inline void lp_over_wave(lp_sums &a)
     a.s = over_wave(a.s, op_add); a.w = over_wave(a.w, op_add);
 }
 
-// What a row's sums say: written by all threads of the workgroup
+// A token's logit (no token: NaN)
+template <typename T> __device__ inline float lp_logit(const lp_args &a, int64_t row, int i)
+{
+    const int tok = a.tokens[row * a.n_tokens + i];
+    return tok >= 0 && tok < a.vocab ? lp_clean(lp_one<T>(a.logits + row * a.row_bytes, tok)) : __uint_as_float(0x7fc00000u);
+}
+
+// What a row's sums say: written by all threads of the workgroup.  x0: the logit of token tid, asked for early.
 template <typename T>
-__device__ inline void lp_finish(const lp_args &a, int64_t row, const lp_sums &t, int tid, int nt, const uint64_t *best)
+__device__ inline void lp_finish(const lp_args &a, int64_t row, const lp_sums &t, int tid, int nt, const uint64_t *best, float x0)
 {
     const float lz = __log2f(t.s) * 0.69314718055994530942f, lse = t.s == 0.f ? -INFINITY : t.m + lz;
     // under -infinity alone no token has a probability
@@ -72,8 +80,8 @@ __device__ inline void lp_finish(const lp_args &a, int64_t row, const lp_sums &t
         if (a.entropy != nullptr) a.entropy[row] = t.s == 0.f ? 0.f : lz - 0.69314718055994530942f * t.w / t.s;
     }
     for (int i = tid; i < a.n_tokens; i += nt) {
-        const int tok = a.tokens[row * a.n_tokens + i];
-        a.logprobs[row * a.n_tokens + i] = tok >= 0 && tok < a.vocab ? logp(lp_clean(lp_one<T>(a.logits + row * a.row_bytes, tok))) : __uint_as_float(0x7fc00000u);
+        const float x = i == tid ? x0 : lp_logit<T>(a, row, i);
+        a.logprobs[row * a.n_tokens + i] = x == x ? logp(x) : x;
     }
     for (int i = tid; i < a.top; i += nt) {
         const uint64_t k = best[i];
@@ -90,58 +98,64 @@ __device__ inline uint64_t lp_wave_best(uint64_t k)
     return k;
 }
 
-// The best `top` of n <= 64 keys in LDS, in order: a lane a key, counting the better ones
-__device__ inline void lp_rank(const uint64_t *keys, int n, int top, uint64_t *best)
+// The best `top` of n <= 64 keys in LDS, in order: the waves take keys in turn, their lanes compare them with all
+__device__ inline void lp_rank(const uint64_t *keys, int n, int top, uint64_t *best, int wave, int waves)
 {
     const int lane = threadIdx.x & 63;
-    const uint64_t k = lane < n ? keys[lane] : 0;
-    const uint32_t lo = (uint32_t)k, hi = (uint32_t)(k >> 32);
-    int better = 0;
-    for (int j = 0; j < n; ++j) {
-        const uint64_t o = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, j) << 32 | (uint32_t)__builtin_amdgcn_readlane(lo, j);
-        better += o > k;
+    const uint64_t other = lane < n ? keys[lane] : 0;
+    for (int i = wave; i < n; i += waves) {
+        const uint64_t k = keys[i];
+        const int better = __popcll(__ballot(other > k));
+        if (better < top && lane == 0) best[better] = k;
     }
-    if (lane < n && better < top) best[better] = k;
 }
 
-// NT threads, E numbers of a row each, from the row's first address that is a multiple of 16 bytes on; the few numbers ahead of that belong to the first segment's first threads.
+// NT threads, E numbers of a row each, from the row's first address that is a multiple of 16 bytes on; the few numbers ahead of that and behind the last 16 bytes
+// go to single threads of the first and the last segment.
 template <typename T, int NT, int E>
-__global__ void __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(8, 8)))
+__global__ void __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 4 ? 4 : 8)))
 k_logprobs(const lp_args a)
 {
     constexpr int V = 16 / (int)sizeof(T), U = E / V, NW = NT / 64, D = E * (int)sizeof(T) / 4;
     __shared__ lp_sums sh_s[NW];
     __shared__ uint32_t sh_max[NT], sh_bound;
     __shared__ uint64_t sh_key[LP_ROOM], sh_best[LP_MAX_TOP];
-    __shared__ int sh_n;
+    __shared__ int sh_n, sh_few, sh_who[LP_FEW];
+    __shared__ __align__(16) uint32_t sh_x[LP_FEW][D];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t row = blockIdx.x / a.segs;
-    const int seg = (int)(blockIdx.x - row * a.segs);
-    const char *src = a.logits + row * a.row_bytes;
-    const int head = min((int)(((16u - ((uint32_t)(uintptr_t)src & 15u)) & 15u) / (uint32_t)sizeof(T)), a.vocab), base = head + seg * (NT * E);
     uint32_t x[D];
-    auto index = [&](int i) { return base + ((i / V) * NT + tid) * V + i % V; };
+    // a segment's numbers on their way into the registers
+    auto place = [&](int64_t item, int64_t &row, int &seg, const char *&src, int &head) {
+        row = item / a.segs; seg = (int)(item - row * a.segs);
+        src = a.logits + row * a.row_bytes;
+        head = min((int)(((16u - ((uint32_t)(uintptr_t)src & 15u)) & 15u) / (uint32_t)sizeof(T)), a.vocab);
+    };
+    auto load = [&](int64_t item) {
+        int64_t row; int seg, head; const char *src;
+        place(item, row, seg, src, head);
+        const int base = head + seg * (NT * E);
+        constexpr uint32_t inf = sizeof(T) == 4 ? 0xff800000u : __is_same(T, __bf16) ? 0xff80ff80u : 0xfc00fc00u;      // -infinity
+        const u32x4 none = {inf, inf, inf, inf};
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int i0 = base + (u * NT + tid) * V;
-        if (i0 + V <= a.vocab) {
-            const u32x4 v = __builtin_nontemporal_load((const u32x4 *)(src + (int64_t)i0 * sizeof(T)));
+        for (int u = 0; u < U; ++u) {
+            const int i0 = base + (u * NT + tid) * V;
+            u32x4 v = none;
+            if (i0 + V <= a.vocab) v = __builtin_nontemporal_load((const u32x4 *)(src + (int64_t)i0 * sizeof(T)));
             x[4 * u] = v.x; x[4 * u + 1] = v.y; x[4 * u + 2] = v.z; x[4 * u + 3] = v.w;
-        } else {
-            const uint32_t none = sizeof(T) == 4 ? 0xff800000u : __is_same(T, __bf16) ? 0xff80ff80u : 0xfc00fc00u;      // -infinity
-#pragma unroll
-            for (int d = 0; d < 4; ++d) {
-                x[4 * u + d] = none;
-                if constexpr (sizeof(T) == 4) { if (i0 + d < a.vocab) x[4 * u + d] = ((const uint32_t *)src)[i0 + d]; }
-                else {
-                    if (i0 + 2 * d < a.vocab) x[4 * u + d] = (none & 0xffff0000u) | ((const uint16_t *)src)[i0 + 2 * d];
-                    if (i0 + 2 * d + 1 < a.vocab) x[4 * u + d] = (x[4 * u + d] & 0xffffu) | (uint32_t)((const uint16_t *)src)[i0 + 2 * d + 1] << 16;
-                }
-            }
         }
-    }
-    const bool first = seg == 0 && tid < head;
-    const float x0 = first ? lp_clean(lp_one<T>(src, tid)) : -INFINITY;
+    };
+    const int64_t item = blockIdx.x;
+    load(item);
+    int64_t row; int seg, head; const char *src;
+    place(item, row, seg, src, head);
+    const int base = head + seg * (NT * E);
+    auto index = [&](int i) { return base + ((i / V) * NT + tid) * V + i % V; };
+    float asked = 0.f;
+    if (a.segs == 1 && tid < a.n_tokens) asked = lp_logit<T>(a, row, tid);
+    // those that no 16 bytes hold: ahead of the row's first, behind its last
+    const int behind = (a.vocab - head) % V, alone = tid < 8 ? (seg == 0 && tid < head ? tid : -1) : tid < 8 + behind && seg == (a.vocab - behind - head) / (NT * E) ? a.vocab - behind + tid - 8 : -1;
+    const bool first = alone >= 0;
+    const float x0 = first ? lp_clean(lp_one<T>(src, alone)) : -INFINITY;
     lp_sums t = {x0, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < E; ++i) t.m = fmaxf(t.m, lp_get<T>(x, i));          // (of a number and NaN the number)
@@ -172,8 +186,8 @@ k_logprobs(const lp_args a)
     lp_over_wave(t);
     if (lane == 0) sh_s[wave] = t;
     if (a.top > 0) {
-        sh_max[tid] = first || index(0) < a.vocab ? lp_order(mine + 0.f) : 0u;      // (a thread behind the row's end has no token)
-        if (tid == 0) sh_n = 0;
+        sh_max[tid] = first || index(V - 1) < a.vocab ? lp_order(mine + 0.f) : 0u;      // (a thread behind the row's end has no token)
+        if (tid == 0) { sh_n = 0; sh_few = 0; }
         if (tid < LP_MAX_TOP) sh_best[tid] = 0;
     }
     __syncthreads();
@@ -182,25 +196,42 @@ k_logprobs(const lp_args a)
             uint32_t g = 0;
 #pragma unroll
             for (int w = 0; w < NW; ++w) { const uint32_t o = sh_max[w * 64 + lane]; g = o > g ? o : g; }
-            uint32_t bound = 0;                               // the largest number, to 20 bits, that `top` of the 64 maxima reach
-#pragma unroll 4
-            for (int b = 31; b >= 12; --b) { const uint32_t n = bound | 1u << b; if (__popcll(__ballot(g >= n)) >= a.top) bound = n; }
+            uint32_t bound = 0;                               // a number that `top` of the 64 maxima reach: the largest to 20 bits, or one that no more reach
+            for (int b = 31; b >= 12; --b) {
+                const uint32_t n = bound | 1u << b;
+                const int reach = __popcll(__ballot(g >= n));
+                if (reach >= a.top) bound = n;
+                if (reach == a.top) break;
+            }
             if (lane == 0) sh_bound = bound;
         }
         __syncthreads();
         const uint32_t bound = sh_bound;
         auto keep = [&](uint64_t k) { const int at = atomicAdd(&sh_n, 1); if (at < LP_ROOM) sh_key[at] = k; };
-        if (lp_order(mine + 0.f) >= bound) {
-            if (first && lp_order(x0) >= bound) keep(lp_key(x0, tid));
+        const int begin = seg == 0 ? 0 : base, end = min(base + NT * E, a.vocab);
+        if (bound <= 0x007fffffu) {                           // every token: to be kept, or too many
+            if (end - begin > LP_ROOM) sh_n = LP_ROOM + 1;
+            else for (int i = begin + tid; i < end; i += NT) keep(lp_key(lp_clean(lp_one<T>(src, i)), i));
+        } else if (lp_order(mine + 0.f) >= bound) {           // few threads have any: those hand their numbers to the first wave
+            if (first && lp_order(x0) >= bound) keep(lp_key(x0, alone));
+            const int at = atomicAdd(&sh_few, 1);
+            if (at < LP_FEW) {
+                sh_who[at] = tid;
 #pragma unroll
-            for (int i = 0; i < E; ++i) {
-                const float v = lp_clean(lp_get<T>(x, i));
-                if (lp_order(v) >= bound && index(i) < a.vocab) keep(lp_key(v, index(i)));
-            }
+                for (int d = 0; d < D; d += 4) *(uint4 *)&sh_x[at][d] = make_uint4(x[d], x[d + 1], x[d + 2], x[d + 3]);
+            } else sh_n = LP_ROOM + 1;
+        }
+        __syncthreads();
+        const int few = sh_few <= LP_FEW ? sh_few : 0;        // (else too many)
+        const float least = lp_value(bound);                  // (neither NaN reaches it nor what fills up a row)
+        for (int i = tid; i < few * E; i += NT) {
+            const int who = i / E, e = i - who * E, at = base + ((e / V) * NT + sh_who[who]) * V + e % V;
+            const float v = lp_get<T>(sh_x[who], e);
+            if (v >= least) keep(lp_key(v + 0.f, at));
         }
         __syncthreads();
         const int n = sh_n;
-        if (n <= 64) { if (wave == 0) lp_rank(sh_key, n, a.top, sh_best); }
+        if (n <= 64) lp_rank(sh_key, n, a.top, sh_best, wave, NW);
         else if (n <= LP_ROOM) {
             for (int i = tid; i < n; i += NT) {
                 const uint64_t k = sh_key[i];
@@ -214,7 +245,7 @@ k_logprobs(const lp_args a)
             for (int r = 0; r < a.top; ++r) {
                 uint64_t k = 0;
                 // (read again: in a loop over registers the keys would have to be kept as well)
-                for (int i = (seg == 0 ? 0 : base) + tid; i < min(base + NT * E, a.vocab); i += NT) { const uint64_t o = lp_key(lp_clean(lp_one<T>(src, i)), i); if (o < last && o > k) k = o; }
+                for (int i = begin + tid; i < end; i += NT) { const uint64_t o = lp_key(lp_clean(lp_one<T>(src, i)), i); if (o < last && o > k) k = o; }
                 k = lp_wave_best(k);
                 if (lane == 0) sh_key[wave] = k;
                 __syncthreads();
@@ -234,32 +265,60 @@ k_logprobs(const lp_args a)
         t = {M, 0.f, 0.f};
         for (int w = 0; w < NW; ++w) { lp_sums o = sh_s[w]; lp_under(o, M); t.s += o.s; t.w += o.w; }
     }
-    if (a.segs == 1) { lp_finish<T>(a, row, t, tid, NT, sh_best); return; }
-    if (tid == 0) *(float4 *)(a.part + (row * a.segs + seg) * 4) = make_float4(t.m, t.s, t.w, 0.f);
-    for (int i = tid; i < a.top; i += NT) a.keys[(row * a.segs + seg) * a.top + i] = sh_best[i];
+    if (a.segs == 1) lp_finish<T>(a, row, t, tid, NT, sh_best, asked);
+    else {
+        if (tid == 0) *(float4 *)(a.part + (row * a.segs + seg) * 4) = make_float4(t.m, t.s, t.w, 0.f);
+        for (int i = tid; i < a.top; i += NT) a.keys[(row * a.segs + seg) * a.top + i] = sh_best[i];
+    }
 }
 
-// The segments of a row joined: a wave a row, a lane a segment (its best tokens come in order)
+// The segments of a row joined: a workgroup a row, a lane a segment for its sums and the bound that its best tokens give
 template <typename T>
-__global__ void __launch_bounds__(64)
+__global__ void __launch_bounds__(256)
 k_logprobs_join(const lp_args a)
 {
-    __shared__ uint64_t sh_key[LP_MAX_SEGS * LP_MAX_TOP], sh_best[LP_MAX_TOP];
-    const int lane = threadIdx.x;
+    constexpr int MOST = LP_MAX_SEGS * LP_MAX_TOP, FL = MOST / 256;
+    __shared__ uint64_t sh_few[MOST], sh_best[LP_MAX_TOP];
+    __shared__ int sh_n;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, total = a.segs * a.top;
     const int64_t row = blockIdx.x;
+    const uint64_t *keys = a.keys + row * total;
     lp_sums t = {-INFINITY, 0.f, 0.f};
+    uint64_t k[FL], g = 0;
+    // the d-th best of each segment: as many of them as reach a bound bring d tokens each
+    const int d = a.top > 0 ? (a.top + a.segs - 1) / a.segs : 1, want = (a.top + d - 1) / d;
     if (lane < a.segs) { const float4 p = *(const float4 *)(a.part + (row * a.segs + lane) * 4); t = {p.x, p.y, p.z}; }
-    for (int i = lane; i < a.segs * a.top; i += 64) sh_key[i] = a.keys[row * a.segs * a.top + i];
+    if (a.top > 0 && lane < a.segs) g = keys[lane * a.top + d - 1];
+#pragma unroll
+    for (int i = 0; i < FL; ++i) { k[i] = 0; if (i * 256 < total && i * 256 + tid < total) k[i] = keys[i * 256 + tid]; }
+    const float asked = tid < a.n_tokens ? lp_logit<T>(a, row, tid) : 0.f;
+    if (tid == 0) sh_n = 0;
+    if (tid < LP_MAX_TOP) sh_best[tid] = 0;
+    __syncthreads();
+    if (a.top > 0) {
+        uint32_t bound = 0;
+        for (int b = 31; b >= 0; --b) {
+            const uint32_t n = bound | 1u << b;
+            const int reach = __popcll(__ballot((uint32_t)(g >> 32) >= n));
+            if (reach >= want) bound = n;
+            if (reach == want) break;
+        }
+#pragma unroll
+        for (int i = 0; i < FL; ++i) if (k[i] != 0 && (uint32_t)(k[i] >> 32) >= bound) sh_few[atomicAdd(&sh_n, 1)] = k[i];
+        __syncthreads();
+        const int n = sh_n;
+        if (n <= 64) lp_rank(sh_few, n, a.top, sh_best, wave, 4);
+        else for (int i = tid; i < n; i += 256) {
+            const uint64_t mine = sh_few[i];
+            int better = 0;
+#pragma unroll 4
+            for (int j = 0; j < n; ++j) better += sh_few[j] > mine;
+            if (better < a.top) sh_best[better] = mine;
+        }
+    }
     lp_over_wave(t);
     __syncthreads();
-    int at = 0;
-    for (int r = 0; r < a.top; ++r) {
-        const uint64_t head = lane < a.segs && at < a.top ? sh_key[lane * a.top + at] : 0, best = lp_wave_best(head);
-        if (head == best && best != 0) ++at;                  // (keys are all different)
-        if (lane == 0) sh_best[r] = best;
-    }
-    __syncthreads();
-    lp_finish<T>(a, row, t, lane, 64, sh_best);
+    lp_finish<T>(a, row, t, tid, 256, sh_best, asked);
 }
 
 // ------------------------------- host side ----------------------------------------
@@ -300,7 +359,7 @@ static int launch(const lp_args &a, const lp_plan &p, hipStream_t s)
     if (p.large) k_logprobs<T, 1024, 32><<<grid, 1024, 0, s>>>(a);
     else k_logprobs<T, 256, 16><<<grid, 256, 0, s>>>(a);
     PV_HIP(hipGetLastError());
-    if (a.segs > 1) { k_logprobs_join<T><<<(unsigned)a.rows, 64, 0, s>>>(a); PV_HIP(hipGetLastError()); }
+    if (a.segs > 1) { k_logprobs_join<T><<<(unsigned)a.rows, 256, 0, s>>>(a); PV_HIP(hipGetLastError()); }
     return PV_OK;
 }
 
