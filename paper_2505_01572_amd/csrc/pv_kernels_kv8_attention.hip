@@ -365,18 +365,24 @@ k_kv8_attn(const kv8_attn_args a)
     const bool whole = nk <= a.chunk;
     const int sure = a.mask != nullptr ? len : len + m0 / a.group + 1;     // keys before this one are seen by every row
 
-    // the four groups of 16 keys from p0 on: their pages (-1: none), known two turns ahead, and, in lanes 16 i .., group i's scales' bytes
+    // the four groups of 16 keys from p0 on: their table entries, known two turns ahead, and, in lanes 16 i .., group i's scales' bytes
     const uint64_t block = (uint64_t)HD << shift;                        // bytes of a head's keys in a page
-    int page[4];
+    int page[4] = {-1, -1, -1, -1}, ahead[4];
     uint32_t bytes = 0;
-    auto pages = [&](int p0) {
+    auto pages = [&](int p0, int (&to)[4]) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) page[i] = kv8_entry(sq, (p0 + 16 * i) >> shift);
+        for (int i = 0; i < 4; ++i) to[i] = kv8_entry(sq, (p0 + 16 * i) >> shift);
     };
     auto exists = [&](int p0, int i) { return (int)(p0 + 16 * i < k1) & (int)kv8_is_page(sq, page[i]); };       // (k1 does not lie behind the table's end)
+    // Every load is made, without a branch, through a descriptor of no bytes where there is no such group: it reads nothing then and gives zeros.  (The compiler counts the loads behind the one that it
+    // waits for and takes the least of all ways to a place: with loads that may not be there it waited for V before the scores: 32 sequences of 1..8192 keys 52.7 -> 50.5 us)
     uint4 kt[4][KB], vt[4][KB];
-    const uint8_t *from[4];
+    __amdgpu_buffer_rsrc_t from[4];
     int bad = 0;
+    auto load_16 = [&](int i, uint32_t off, int b) {
+        const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(from[i], off + lane * 16 + b * 1024, 0, 2);      // (2: each code is read once, and past the caches)
+        return make_uint4(v.x, v.y, v.z, v.w);
+    };
     auto load_k = [&](int p0) {
         bad = 0;
         int at[4];
@@ -386,20 +392,21 @@ k_kv8_attn(const kv8_attn_args a)
         bytes = *(const uint16_t *)(sq.pool.scales + kv8_scale(sq.pool, mine, kvh, 0, sub));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            from[i] = uniform_ptr(sq.pool.codes + ((uint64_t)(uint32_t)at[i] * sq.pool.n_heads + kvh) * 2 * block + (uint32_t)(((p0 + 16 * i) & ((1 << shift) - 1)) >> 4) * (16 * HD));
+            const uint8_t *base = uniform_ptr(sq.pool.codes + ((uint64_t)(uint32_t)at[i] * sq.pool.n_heads + kvh) * 2 * block + (uint32_t)(((p0 + 16 * i) & ((1 << shift) - 1)) >> 4) * (16 * HD));
+            from[i] = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (bad >> i) & 1 ? 0 : (int)block + 16 * HD, 0x00027000);
 #pragma unroll
-            for (int b = 0; b < KB; ++b) kt[i][b] = load_once((const uint4 *)from[i] + b * 64 + lane);
+            for (int b = 0; b < KB; ++b) kt[i][b] = load_16(i, 0, b);
         }
     };
     auto load_v = [&]() {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int b = 0; b < KB; ++b) vt[i][b] = load_once((const uint4 *)(from[i] + block) + b * 64 + lane);
+            for (int b = 0; b < KB; ++b) vt[i][b] = load_16(i, (uint32_t)block, b);
     };
 
     int p0 = k0 + 64 * wave;
-    if (p0 < k1) pages(p0);
+    if (p0 < k1) pages(p0, page);
     kv8_row row[RT];
     uint4 q[RT][NQ][KS];
     uint64_t vm[RT];
@@ -412,13 +419,14 @@ k_kv8_attn(const kv8_attn_args a)
         vm[t] = a.mask != nullptr ? a.mask[row[t].row] : 0;
     }
     asm volatile("" ::: "memory");
-    if (p0 < k1) { load_k(p0); load_v(); }
+    load_k(p0);
+    load_v();
     auto sees = [&](int t, int p) { return kv8_sees(a.mask != nullptr, vm[t], p + 4 * g, len, len + row[t].j + 1, nk); };
     bool spoilt = false;                    // NaN among values that not every row sees
     int only = -1;
-    if (p0 < k1) pages(p0 + 256);
+    ahead[0] = ahead[1] = ahead[2] = ahead[3] = -1;
+    if (p0 < k1) pages(p0 + 256, ahead);
     while (p0 < k1) {
-        const bool more = p0 + 256 < k1;
         const int miss = bad;
         float fk[4];
         int ev[4], dv[4];
@@ -453,8 +461,13 @@ k_kv8_attn(const kv8_attn_args a)
         }
         auto see = [&](int t) { return sees(t, p0) & there; };
         uint2 P[RT][4], PL[RT][4];
+        // the next 64 keys, or these again
         const bool through = only < 0 || only == 3;
-        if (through && more) { load_k(p0 + 256); pages(p0 + 512); }
+        const int p1 = through ? p0 + 256 : p0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) page[i] = through ? ahead[i] : page[i];
+        load_k(p1);
+        pages(p1 + 256, ahead);
         kv8_softmax<HD, RT, IO>(A, S, a.scale2, fk, edge, see, dv, P, PL);
         if (last_keys) {
             bool nans = false;
@@ -481,15 +494,14 @@ k_kv8_attn(const kv8_attn_args a)
             const uint2 x = part(2 * u), y = part(2 * u + 1);
             return make_uint4(x.x, x.y, y.x, y.y);
         });
-        if (!through) { ++only; continue; }
-        only = -1;
-        p0 += 256;
-        if (more) load_v();
+        only = through ? -1 : only + 1;
+        p0 = p1;
+        load_v();
     }
     if (spoilt) {
         for (p0 = k0 + 64 * wave; p0 < k1; p0 += 256) {
             if (p0 + 64 <= sure && p0 + 64 <= nk) continue;
-            pages(p0);
+            pages(p0, page);
             kv8_put_nans<HD, RT>(A, [&](int t) { return sees(t, p0); }, [&](int i, int b) {
                 if (!exists(p0, i)) return make_uint4(0u, 0u, 0u, 0u);
                 const uint4 c = ((const uint4 *)(sq.pool.codes + (((uint64_t)(uint32_t)page[i] * sq.pool.n_heads + kvh) * 2 + 1) * block + (uint32_t)(((p0 + 16 * i) & ((1 << shift) - 1)) >> 4) * (16 * HD)))[b * 64 + lane];
@@ -574,17 +586,18 @@ k_kv8_attn_wide(const kv8_attn_args a)
     const uint64_t block = (uint64_t)HD << shift;
     auto page_of = [&](int s) { const int p = k0 + 64 * s + 16 * wave; return kv8_entry(sq, p >> shift); };
     auto codes_of = [&](int page, int p) { return sq.pool.codes + ((uint64_t)(uint32_t)page * sq.pool.n_heads + kvh) * 2 * block + (uint32_t)((p & ((1 << shift) - 1)) >> 4) * (16 * HD); };
-    uint4 kt[KB], vt[KB];
+    u32x4 kt[KB], vt[KB];
     uint32_t bytes = 0;
     int page = -1;                           // of the group that the registers hold
+    // (no branch around the loads, and their registers stay whole: the compiler waits for a load where it moves a part of it)
     auto load = [&](int s, int pg) {
         const int p = k0 + 64 * s + 16 * wave;
         page = p < k1 && kv8_is_page(sq, pg) ? pg : -1;
-        if (page < 0) return;
-        const uint8_t *at = codes_of(pg, p);
-        bytes = *(const uint16_t *)(sq.pool.scales + kv8_scale(sq.pool, pg, kvh, 0, (p & ((1 << shift) - 1)) >> 4));
+        const int there = max(page, 0);
+        const uint8_t *at = kv8_global(uniform_ptr(codes_of(there, p)));
+        bytes = *(const uint16_t *)(sq.pool.scales + kv8_scale(sq.pool, there, kvh, 0, (p & ((1 << shift) - 1)) >> 4));
 #pragma unroll
-        for (int b = 0; b < KB; ++b) { kt[b] = ((const uint4 *)at)[b * 64 + lane]; vt[b] = ((const uint4 *)(at + block))[b * 64 + lane]; }
+        for (int b = 0; b < KB; ++b) { kt[b] = ((const u32x4 *)at)[b * 64 + lane]; vt[b] = ((const u32x4 *)(at + block))[b * 64 + lane]; }
     };
     auto convert = [&](int s, int buf) {
         uint4 *L = wide_lds + buf * W::buffer;
@@ -592,24 +605,23 @@ k_kv8_attn_wide(const kv8_attn_args a)
         uint2 *Lv = (uint2 *)(L + 4 * KS * 64 + (wave >> 1) * ET * 64 + lane) + (wave & 1);
         const int p = k0 + 64 * s + 16 * wave;
         uint32_t what = page < 0 ? 1u << 16 : bytes;
-        if (page < 0) {
-#pragma unroll
-            for (int b = 0; b < KB; ++b) kt[b] = vt[b] = make_uint4(0u, 0u, 0u, 0u);
-        } else if (p + 16 > sure || p + 16 > nk) {
-            const uint32_t there = kv8_there(nk - p, g);
+        const float f = kv8_pow2(kv8_byte(__builtin_amdgcn_readfirstlane(bytes) & 0xff) - 127);
+        const bool whole_group = page >= 0 && p + 16 <= sure && p + 16 <= nk;
+        if (!whole_group) {
+            // codes of pages that do not exist, and values behind the end, count as zero, and values that are NaN are put in at the end
+            const uint32_t k_there = page < 0 ? 0u : ~0u, there = page < 0 ? 0u : kv8_there(nk - p, g);
             bool nans = false;
 #pragma unroll
             for (int b = 0; b < KB; ++b) {
-                vt[b].x &= there; vt[b].y &= there; vt[b].z &= there; vt[b].w &= there;
+                kt[b] &= k_there; vt[b] &= there;
                 nans = nans || (kv8_nans(vt[b].x) | kv8_nans(vt[b].y) | kv8_nans(vt[b].z) | kv8_nans(vt[b].w)) != 0;
             }
             if (__any(nans)) {
                 what |= 1u << 17;
 #pragma unroll
-                for (int b = 0; b < KB; ++b) vt[b] = make_uint4(kv8_without_nans(vt[b].x), kv8_without_nans(vt[b].y), kv8_without_nans(vt[b].z), kv8_without_nans(vt[b].w));
+                for (int b = 0; b < KB; ++b) vt[b] = (u32x4){kv8_without_nans(vt[b].x), kv8_without_nans(vt[b].y), kv8_without_nans(vt[b].z), kv8_without_nans(vt[b].w)};
             }
         }
-        const float f = kv8_pow2(kv8_byte(__builtin_amdgcn_readfirstlane(bytes) & 0xff) - 127);
 #pragma unroll
         for (int b = 0; b < KB; ++b) {
             Lk[(2 * b) * 64] = kv8_key<HALF>(kt[b].x, kt[b].y, f);
@@ -648,12 +660,19 @@ k_kv8_attn_wide(const kv8_attn_args a)
     }
     for (int s = 0; s < steps;) {
         const int buf = s & 1, p0 = k0 + 64 * s;
+        const uint4 *Lk = wide_lds + buf * W::buffer + lane, *Lv = Lk + 4 * KS * 64;
+        // LDS is asked one group of products ahead (two prompts of 2048 rows 509 -> 485 us); the page three steps ahead is asked for before all else (a wait for LDS waits for scalar loads too)
+        const int after = page_of(s + 3);
+        const int4 ab = about[buf];
+        uint4 k[2][KS], v[2][2];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) k[0][ks] = Lk[ks * 64];
+        __builtin_amdgcn_sched_barrier(0);
         if (only < 0 && s + 1 < steps) {
             convert(s + 1, buf ^ 1);
-            if (s + 2 < steps) { load(s + 2, next); next = page_of(s + 3); }
+            if (s + 2 < steps) load(s + 2, next);
         }
-        const uint4 *Lk = wide_lds + buf * W::buffer + lane, *Lv = Lk + 4 * KS * 64;
-        const int4 ab = about[buf];
+        next = after;                                                    // (a group looked at again asks for the same one)
         const uint32_t what[4] = {(uint32_t)__builtin_amdgcn_readfirstlane(ab.x), (uint32_t)__builtin_amdgcn_readfirstlane(ab.y), (uint32_t)__builtin_amdgcn_readfirstlane(ab.z), (uint32_t)__builtin_amdgcn_readfirstlane(ab.w)};
         int miss = 0, ev[4], dv[4];
         float fk[4];
@@ -667,15 +686,19 @@ k_kv8_attn_wide(const kv8_attn_args a)
         f32x4 S[RT][4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
+            if (i < 3) {
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) k[(i + 1) & 1][ks] = Lk[((i + 1) * KS + ks) * 64];
+            } else { v[0][0] = Lv[0]; v[0][1] = Lv[64]; }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int t = 0; t < RT; ++t) S[t][i] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                const uint4 k = Lk[(i * KS + ks) * 64];
 #pragma unroll
                 for (int t = 0; t < RT; ++t)
 #pragma unroll
-                    for (int n = 0; n < NQ; ++n) S[t][i] = kv8_score<HALF>(k, q[t][n][ks], S[t][i]);
+                    for (int n = 0; n < NQ; ++n) S[t][i] = kv8_score<HALF>(k[i & 1][ks], q[t][n][ks], S[t][i]);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -690,7 +713,14 @@ k_kv8_attn_wide(const kv8_attn_args a)
         auto see = [&](int t) { return sees(t, p0) & there; };
         uint2 P[RT][4], PL[RT][4];
         kv8_softmax<HD, RT, IO>(A, S, a.scale2, fk, edge, see, dv, P, PL);
-        kv8_output<HD, RT, IO>(A, P, PL, [&](int u, int e) { return Lv[(u * ET + e) * 64]; });
+        kv8_output<HD, RT, IO>(A, P, PL, [&](int u, int e) {
+            const int n = u * ET + e, i = n >> 1;
+            if (!(n & 1) && i + 1 < ET) {
+                v[(i + 1) & 1][0] = Lv[(n + 2) * 64]; v[(i + 1) & 1][1] = Lv[(n + 3) * 64];
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            return v[i & 1][n & 1];
+        });
         if (only >= 0 && only < 3) { ++only; continue; }                 // (all waves alike: the exponents are the same for them)
         only = -1;
         ++s;
