@@ -181,17 +181,23 @@ template <int HD, int RT> __device__ inline void kv8_unit_is(kv8_acc<HD, RT> &A,
 // V's exponents of four groups against the accumulators' unit, which grows with them: dv.  Where they are too far apart, `only` one group is looked at at a time, from 0 to 3 (-1: all).
 template <int HD, int RT> __device__ inline void kv8_units(kv8_acc<HD, RT> &A, const int (&ev)[4], int (&dv)[4], int &only)
 {
-    const int top = max(max(max(ev[0], ev[1]), max(ev[2], ev[3])), A.E);
-    if (only < 0) {
-        bool far = false;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) far = far || (ev[i] != KV8_NO_SCALE && ev[i] - top < -14);
-        if (far) only = 0;
+    const int e0 = ev[0], e1 = ev[1], e2 = ev[2], e3 = ev[3], top = max(max(max(e0, e1), max(e2, e3)), A.E);
+    int E = top, lowest = -1000000;
+    bool one = false;
+    if (!(only < 0 && min(min(e0, e1), min(e2, e3)) - top >= -14)) {     // (seldom; few scalar instructions else, which take a wave's turns as others do)
+        auto far = [&](int e) { return (int)(e != KV8_NO_SCALE) & (int)(e - top < -14); };
+        if (only < 0 && (far(e0) | far(e1) | far(e2) | far(e3))) only = 0;
+        one = only >= 0;
+        const int mine = only == 0 ? e0 : only == 1 ? e1 : only == 2 ? e2 : e3;
+        if (one) E = mine == KV8_NO_SCALE ? A.E : max(mine, A.E - 100);
+        lowest = -100;
     }
-    const int mine = only == 0 ? ev[0] : only == 1 ? ev[1] : only == 2 ? ev[2] : ev[3], E = only < 0 ? top : mine == KV8_NO_SCALE ? A.E : max(mine, A.E - 100);
     if (E != A.E) kv8_unit_is(A, E);
+    dv[0] = max(e0 - E, lowest); dv[1] = max(e1 - E, lowest); dv[2] = max(e2 - E, lowest); dv[3] = max(e3 - E, lowest);
+    if (one) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) dv[i] = ev[i] == KV8_NO_SCALE || (only >= 0 && i != only) ? 0 : max(ev[i] - E, -100);
+        for (int i = 0; i < 4; ++i) dv[i] = i != only ? 0 : dv[i];
+    }
 }
 
 // Which of 64 keys a row sees: those before `end`, without a mask; with one, those before len, and from there on those that the mask names, before nk.  Bit i: key p + i.
@@ -363,10 +369,11 @@ k_kv8_attn(const kv8_attn_args a)
     const int k0 = split * a.chunk, k1 = min(k0 + a.chunk, nk);
     if (k0 >= nk && split > 0) return;      // (a sequence without keys: split 0 writes its rows)
     const bool whole = nk <= a.chunk;
-    const int sure = a.mask != nullptr ? len : len + m0 / a.group + 1;     // keys before this one are seen by every row
+    const int sure = min(nk, a.mask != nullptr ? len : len + m0 / a.group + 1);     // keys before this one are seen by every row
 
     // the four groups of 16 keys from p0 on: their table entries, known two turns ahead, and, in lanes 16 i .., group i's scales' bytes
-    const uint64_t block = (uint64_t)HD << shift;                        // bytes of a head's keys in a page
+    const uint32_t block = (uint32_t)HD << shift, page_codes = 2 * block * sq.pool.n_heads, page_scales = sq.pool.n_heads << (shift - 3), in_page = (1u << shift) - 1;    // bytes of a head's keys in a page, ...
+    const uint8_t *codes = sq.pool.codes + (size_t)kvh * 2 * block, *scales = sq.pool.scales + (kvh << (shift - 3));
     int page[4] = {-1, -1, -1, -1}, ahead[4];
     uint32_t bytes = 0;
     auto pages = [&](int p0, int (&to)[4]) {
@@ -388,12 +395,12 @@ k_kv8_attn(const kv8_attn_args a)
         int at[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) { const int ok = exists(p0, i); bad |= (ok ^ 1) << i; at[i] = ok ? page[i] : 0; }
-        const int mine = g == 0 ? at[0] : g == 1 ? at[1] : g == 2 ? at[2] : at[3], sub = ((p0 + 16 * g) & ((1 << shift) - 1)) >> 4;
-        bytes = *(const uint16_t *)(sq.pool.scales + kv8_scale(sq.pool, mine, kvh, 0, sub));
+        const int mine = g == 0 ? at[0] : g == 1 ? at[1] : g == 2 ? at[2] : at[3];
+        bytes = *(const uint16_t *)(scales + ((uint64_t)(uint32_t)mine * page_scales + (((p0 + 16 * g) & in_page) >> 3)));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint8_t *base = uniform_ptr(sq.pool.codes + ((uint64_t)(uint32_t)at[i] * sq.pool.n_heads + kvh) * 2 * block + (uint32_t)(((p0 + 16 * i) & ((1 << shift) - 1)) >> 4) * (16 * HD));
-            from[i] = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (bad >> i) & 1 ? 0 : (int)block + 16 * HD, 0x00027000);
+            const uint8_t *base = uniform_ptr(codes + ((uint64_t)(uint32_t)at[i] * page_codes + ((p0 + 16 * i) & in_page) * HD));
+            from[i] = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (bad >> i) & 1 ? 0 : (int)(block + 16 * HD), 0x00027000);
 #pragma unroll
             for (int b = 0; b < KB; ++b) kt[i][b] = load_16(i, 0, b);
         }
@@ -402,7 +409,7 @@ k_kv8_attn(const kv8_attn_args a)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int b = 0; b < KB; ++b) vt[i][b] = load_16(i, (uint32_t)block, b);
+            for (int b = 0; b < KB; ++b) vt[i][b] = load_16(i, block, b);
     };
 
     int p0 = k0 + 64 * wave;
@@ -430,11 +437,11 @@ k_kv8_attn(const kv8_attn_args a)
         const int miss = bad;
         float fk[4];
         int ev[4], dv[4];
+        const int fk_bits = kv8_byte(bytes & 0xffu) << 23, e_v = (miss >> g) & 1 ? KV8_NO_SCALE : kv8_byte(bytes >> 8) - 127;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t b = __builtin_amdgcn_readlane(bytes, 16 * i);
-            fk[i] = kv8_pow2(kv8_byte(b & 0xffu) - 127);
-            ev[i] = ((miss >> i) & 1) ? KV8_NO_SCALE : kv8_byte(b >> 8) - 127;
+            fk[i] = __uint_as_float(__builtin_amdgcn_readlane(fk_bits, 16 * i));
+            ev[i] = __builtin_amdgcn_readlane(e_v, 16 * i);
         }
         f32x4 S[RT][4];
 #pragma unroll
@@ -453,7 +460,7 @@ k_kv8_attn(const kv8_attn_args a)
         }
         kv8_units(A, ev, dv, only);
         const int without = miss | (only < 0 ? 0 : 15 & ~(1 << only));    // groups that are not looked at
-        const bool last_keys = p0 + 64 > sure || p0 + 64 > nk || miss != 0, edge = last_keys || without != 0;
+        const bool last_keys = p0 + 64 > sure || miss != 0, edge = last_keys || without != 0;
         uint64_t there = ~0ull;
         if (without) {
 #pragma unroll
@@ -500,11 +507,11 @@ k_kv8_attn(const kv8_attn_args a)
     }
     if (spoilt) {
         for (p0 = k0 + 64 * wave; p0 < k1; p0 += 256) {
-            if (p0 + 64 <= sure && p0 + 64 <= nk) continue;
+            if (p0 + 64 <= sure) continue;
             pages(p0, page);
             kv8_put_nans<HD, RT>(A, [&](int t) { return sees(t, p0); }, [&](int i, int b) {
                 if (!exists(p0, i)) return make_uint4(0u, 0u, 0u, 0u);
-                const uint4 c = ((const uint4 *)(sq.pool.codes + (((uint64_t)(uint32_t)page[i] * sq.pool.n_heads + kvh) * 2 + 1) * block + (uint32_t)(((p0 + 16 * i) & ((1 << shift) - 1)) >> 4) * (16 * HD)))[b * 64 + lane];
+                const uint4 c = ((const uint4 *)(codes + ((uint64_t)(uint32_t)page[i] * page_codes + block + ((p0 + 16 * i) & in_page) * HD)))[b * 64 + lane];
                 const uint32_t there = kv8_there(nk - (p0 + 16 * i), g);
                 return make_uint4(c.x & there, c.y & there, c.z & there, c.w & there);
             });
@@ -579,13 +586,14 @@ k_kv8_attn_wide(const kv8_attn_args a)
     const int k0 = split * a.chunk, k1 = min(k0 + a.chunk, nk);
     if (k0 >= nk && split > 0) return;
     const bool whole = nk <= a.chunk;
-    const int sure = a.mask != nullptr ? len : len + m0 / a.group + 1;     // keys before this one are seen by every row
+    const int sure = min(nk, a.mask != nullptr ? len : len + m0 / a.group + 1);     // keys before this one are seen by every row
     const int steps = (k1 - k0 + 63) >> 6;
 
     // this wave's group of 16 keys of step s
-    const uint64_t block = (uint64_t)HD << shift;
+    const uint32_t block = (uint32_t)HD << shift, page_codes = 2 * block * sq.pool.n_heads, page_scales = sq.pool.n_heads << (shift - 3), in_page = (1u << shift) - 1;
+    const uint8_t *codes = sq.pool.codes + (size_t)kvh * 2 * block, *scales = sq.pool.scales + (kvh << (shift - 3));
     auto page_of = [&](int s) { const int p = k0 + 64 * s + 16 * wave; return kv8_entry(sq, p >> shift); };
-    auto codes_of = [&](int page, int p) { return sq.pool.codes + ((uint64_t)(uint32_t)page * sq.pool.n_heads + kvh) * 2 * block + (uint32_t)((p & ((1 << shift) - 1)) >> 4) * (16 * HD); };
+    auto codes_of = [&](int page, int p) { return codes + ((uint64_t)(uint32_t)page * page_codes + (p & in_page) * HD); };
     u32x4 kt[KB], vt[KB];
     uint32_t bytes = 0;
     int page = -1;                           // of the group that the registers hold
@@ -595,7 +603,7 @@ k_kv8_attn_wide(const kv8_attn_args a)
         page = p < k1 && kv8_is_page(sq, pg) ? pg : -1;
         const int there = max(page, 0);
         const uint8_t *at = kv8_global(uniform_ptr(codes_of(there, p)));
-        bytes = *(const uint16_t *)(sq.pool.scales + kv8_scale(sq.pool, there, kvh, 0, (p & ((1 << shift) - 1)) >> 4));
+        bytes = *(const uint16_t *)(scales + ((uint64_t)(uint32_t)there * page_scales + ((p & in_page) >> 3)));
 #pragma unroll
         for (int b = 0; b < KB; ++b) { kt[b] = ((const u32x4 *)at)[b * 64 + lane]; vt[b] = ((const u32x4 *)(at + block))[b * 64 + lane]; }
     };
@@ -604,9 +612,10 @@ k_kv8_attn_wide(const kv8_attn_args a)
         uint4 *Lk = L + wave * KS * 64 + lane;
         uint2 *Lv = (uint2 *)(L + 4 * KS * 64 + (wave >> 1) * ET * 64 + lane) + (wave & 1);
         const int p = k0 + 64 * s + 16 * wave;
-        uint32_t what = page < 0 ? 1u << 16 : bytes;
-        const float f = kv8_pow2(kv8_byte(__builtin_amdgcn_readfirstlane(bytes) & 0xff) - 127);
-        const bool whole_group = page >= 0 && p + 16 <= sure && p + 16 <= nk;
+        const uint32_t byte_k = kv8_byte(bytes & 0xffu), byte_v = kv8_byte(bytes >> 8);
+        uint32_t what = page < 0 ? 1u << 16 : byte_k | byte_v << 8;
+        const float f = __uint_as_float(byte_k << 23);
+        const bool whole_group = page >= 0 && p + 16 <= sure;
         if (!whole_group) {
             // codes of pages that do not exist, and values behind the end, count as zero, and values that are NaN are put in at the end
             const uint32_t k_there = page < 0 ? 0u : ~0u, there = page < 0 ? 0u : kv8_there(nk - p, g);
@@ -649,7 +658,7 @@ k_kv8_attn_wide(const kv8_attn_args a)
         vm[t] = a.mask != nullptr ? a.mask[row[t].row] : 0;
     }
     auto sees = [&](int t, int p) { return kv8_sees(a.mask != nullptr, vm[t], p + 4 * g, len, len + row[t].j + 1, nk); };
-    bool spoilt = false;
+    uint32_t matter = 0;
     int only = -1;
     int next = 0;
     if (steps > 0) {
@@ -674,14 +683,15 @@ k_kv8_attn_wide(const kv8_attn_args a)
         }
         next = after;                                                    // (a group looked at again asks for the same one)
         const uint32_t what[4] = {(uint32_t)__builtin_amdgcn_readfirstlane(ab.x), (uint32_t)__builtin_amdgcn_readfirstlane(ab.y), (uint32_t)__builtin_amdgcn_readfirstlane(ab.z), (uint32_t)__builtin_amdgcn_readfirstlane(ab.w)};
+        const uint32_t any = what[0] | what[1] | what[2] | what[3];
+        matter |= any;
         int miss = 0, ev[4], dv[4];
         float fk[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (what[i] & 0x10000u) miss |= 1 << i;
-            spoilt = spoilt || (what[i] & 0x20000u);
-            fk[i] = kv8_pow2(kv8_byte(what[i] & 0xffu) - 127);
-            ev[i] = (what[i] & 0x10000u) ? KV8_NO_SCALE : kv8_byte((what[i] >> 8) & 0xffu) - 127;
+        for (int i = 0; i < 4; ++i) { fk[i] = __uint_as_float((what[i] & 0xffu) << 23); ev[i] = (int)((what[i] >> 8) & 0xffu) - 127; }
+        if (any & 0x10000u) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) if (what[i] & 0x10000u) { miss |= 1 << i; ev[i] = KV8_NO_SCALE; }
         }
         f32x4 S[RT][4];
 #pragma unroll
@@ -704,7 +714,7 @@ k_kv8_attn_wide(const kv8_attn_args a)
         }
         kv8_units(A, ev, dv, only);
         const int without = miss | (only < 0 ? 0 : 15 & ~(1 << only));    // groups that are not looked at
-        const bool last_keys = p0 + 64 > sure || p0 + 64 > nk || miss != 0, edge = last_keys || without != 0;
+        const bool last_keys = p0 + 64 > sure || miss != 0, edge = last_keys || without != 0;
         uint64_t there = ~0ull;
         if (without) {
 #pragma unroll
@@ -726,9 +736,9 @@ k_kv8_attn_wide(const kv8_attn_args a)
         ++s;
         sync();
     }
-    if (spoilt) {
+    if (matter & 0x20000u) {
         for (int p0 = k0; p0 < k1; p0 += 64) {
-            if (p0 + 64 <= sure && p0 + 64 <= nk) continue;
+            if (p0 + 64 <= sure) continue;
             kv8_put_nans<HD, RT>(A, [&](int t) { return sees(t, p0); }, [&](int i, int b) {
                 const int p = p0 + 16 * i, pg = p < k1 ? kv8_page(sq, p >> shift) : -1;
                 if (pg < 0) return make_uint4(0u, 0u, 0u, 0u);

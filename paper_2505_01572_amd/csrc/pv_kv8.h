@@ -108,7 +108,7 @@ __device__ inline int kv8_page(const kv8_seq &s, int logical)
 __device__ inline int kv8_entry(const kv8_seq &s, int logical)
 {
     typedef const __attribute__((address_space(4))) int32_t *table;
-    const int l = __builtin_amdgcn_readfirstlane(min(max(logical, 0), s.table_pages - 1));
+    const uint32_t l = __builtin_amdgcn_readfirstlane(min((uint32_t)logical, (uint32_t)s.table_pages - 1));
     return ((table)(uintptr_t)uniform_ptr(s.table))[l];
 }
 __device__ inline bool kv8_is_page(const kv8_seq &s, int entry) { return (uint32_t)entry < (uint32_t)s.pool.n_pages; }
