@@ -306,7 +306,7 @@ int pv_cache_use_graphs(pv_cache *c, int32_t enable);
  *   codes  [n_pages][n_kv_heads][2 (K, V)][page_tokens / 16][16 * head_dim] bytes, 16-byte aligned; inside a block
  *          K [head_dim / 16][token][16 features],  V [head_dim / 64][token / 4][feature % 16][feature / 16 % 4][token % 4]
  *   scales [n_pages][n_kv_heads][page_tokens / 16][2 (K, V)] bytes, 2-byte aligned
- * head_dim is 64 or 128, page_tokens a power of two from 16 to 65536.  Neither array has to be cleared before use. */
+ * head_dim is 64 or 128, page_tokens a power of two from 16 to 65536, a page's codes less than 2^32 bytes.  Neither array has to be cleared before use. */
 typedef struct {
     void *codes, *scales;
     int32_t n_pages, n_kv_heads, head_dim, page_tokens;

@@ -334,6 +334,7 @@ static int check_kv_bits(const pv_model *m, int kv_bits)
     if (kv_bits != 0 && kv_bits != 8) { pv_set_error("kv_bits must be 0 (the model's storage type) or 8, got %d", kv_bits); return PV_EINVAL; }
     if (kv_bits == 8 && m->path < PV_PATH_MATRIX) { pv_set_error("8-bit keys and values need the matrix path (bf16 models)"); return PV_EINVAL; }
     if (kv_bits == 8 && m->cfg.head_dim != 64 && m->cfg.head_dim != 128) { pv_set_error("8-bit keys and values: head_dim must be 64 or 128, got %d", m->cfg.head_dim); return PV_EINVAL; }
+    if (kv_bits == 8 && (int64_t)m->cfg.n_kv_heads * m->cfg.page_tokens * m->cfg.head_dim >= 1ll << 31) { pv_set_error("8-bit keys and values: a page of 2^32 bytes or more"); return PV_ERANGE; }
     if (kv_bits == 8 && m->cfg.page_tokens > 65536) { pv_set_error("8-bit keys and values: at most 65536 tokens a page"); return PV_EINVAL; }
     return PV_OK;
 }

@@ -24,7 +24,7 @@ __device__ inline void kv8_each_block(const kv8_seqs &seqs, const kv8_pool &pool
         if (local < 0 || local >= q.rows) { ++i; continue; }
         const int stop = min(end, q.row0 + q.rows);
         for (; i < stop;) {
-            const int pos = q.len + (i - q.row0), off = pos & 15;
+            const int pos = (int)((uint32_t)q.len + (uint32_t)(i - q.row0)), off = pos & 15;       // (past 2^31: negative, of no page)
             if (off != 0 && i != q.row0) { i += 16 - off; continue; }
             const int n = min(16 - off, q.row0 + q.rows - i);
             work(q, i, pos, off, n);
@@ -217,6 +217,7 @@ int pv_kv8_check_pool(const pv_kv8_pool *p)
     if (p->n_pages < 1 || p->n_pages >= (1 << 26)) { pv_set_error("8-bit cache: n_pages %d outside [1, 2^26)", p->n_pages); return PV_ERANGE; }
     if (p->n_kv_heads < 1 || p->n_kv_heads > 16384) { pv_set_error("8-bit cache: n_kv_heads %d outside [1, 16384]", p->n_kv_heads); return PV_ERANGE; }
     if (p->page_tokens < 16 || p->page_tokens > 65536 || (p->page_tokens & (p->page_tokens - 1))) { pv_set_error("8-bit cache: page_tokens must be a power of two from 16 to 65536, got %d", p->page_tokens); return PV_EINVAL; }
+    if ((int64_t)p->n_kv_heads * p->page_tokens * p->head_dim >= 1ll << 31) { pv_set_error("8-bit cache: a page of %d heads x %d tokens: 2^32 bytes of codes or more", p->n_kv_heads, p->page_tokens); return PV_ERANGE; }
     if (((uintptr_t)p->codes & 15) || ((uintptr_t)p->scales & 1)) { pv_set_error("8-bit cache: codes must be 16-byte and scales 2-byte aligned"); return PV_EINVAL; }
     return PV_OK;
 }

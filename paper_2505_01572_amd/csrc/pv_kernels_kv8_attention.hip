@@ -357,13 +357,13 @@ __device__ inline void kv8_finish4(const kv8_attn_args &a, const kv8_row &w, int
     }
 }
 
-// Few rows: one workgroup is a kv head, a tile of 16 RT packed rows of a sequence, a chunk of its keys; the waves take 64 keys in turn, straight from memory to registers, and are joined
+// Few rows: one workgroup is a kv head, a tile of 16 packed rows of a sequence, a chunk of its keys; the waves take 64 keys in turn, straight from memory to registers, and are joined
 // through LDS at the end.  Bound by the read of the codes: the next 64 keys' K is asked for when this one's scores are there, V when its products are.
-template <int HD, int RT, int IO>
+template <int HD, int IO>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 k_kv8_attn(const kv8_attn_args a)
 {
-    constexpr int KB = HD / 64, KS = HD / 32, NQ = kv8_types<IO>::NQ, TR = 16 * RT, OS = 68;
+    constexpr int KB = HD / 64, KS = HD / 32, NQ = kv8_types<IO>::NQ, RT = 1, TR = 16, OS = 68;
     constexpr bool HALF = kv8_types<IO>::half;
     __shared__ float2 sh_ml[4][TR];
     __shared__ float sh_o[4][TR][OS];
@@ -374,7 +374,7 @@ k_kv8_attn(const kv8_attn_args a)
     if (!kv8_unit<HD, TR>(a.seqs, a.pool, blockIdx.x / a.pool.n_heads, a.group, sq, tile)) return;
     const int m0 = tile * TR, nrows = sq.rows * a.group, shift = sq.pool.page_shift;
     const int last = (min(m0 + TR, nrows) - 1) / a.group;
-    const int nk = __builtin_amdgcn_readfirstlane(kv8_keys(sq, shift, last, a.mask != nullptr)), len = __builtin_amdgcn_readfirstlane(sq.len);
+    const int nk = __builtin_amdgcn_readfirstlane(kv8_keys(sq, shift, last, a.mask != nullptr)), len = __builtin_amdgcn_readfirstlane(min(sq.len, 1 << 30));     // (no table goes further)
     const int k0 = split * a.chunk, k1 = min(k0 + a.chunk, nk);
     if (k0 >= nk && split > 0) return;      // (a sequence without keys: split 0 writes its rows)
     const bool whole = nk <= a.chunk;
@@ -591,7 +591,7 @@ k_kv8_attn_wide(const kv8_attn_args a)
     if (!kv8_unit<HD, TR>(a.seqs, a.pool, units - 1 - blockIdx.x / a.pool.n_heads, a.group, sq, tile)) return;
     const int m0 = tile * TR, nrows = sq.rows * a.group, shift = sq.pool.page_shift;
     const int last = (min(m0 + TR, nrows) - 1) / a.group;
-    const int nk = __builtin_amdgcn_readfirstlane(kv8_keys(sq, shift, last, a.mask != nullptr)), len = __builtin_amdgcn_readfirstlane(sq.len);
+    const int nk = __builtin_amdgcn_readfirstlane(kv8_keys(sq, shift, last, a.mask != nullptr)), len = __builtin_amdgcn_readfirstlane(min(sq.len, 1 << 30));     // (no table goes further)
     const int k0 = split * a.chunk, k1 = min(k0 + a.chunk, nk);
     if (k0 >= nk && split > 0) return;
     const bool whole = nk <= a.chunk;
@@ -906,7 +906,7 @@ template <int HD, int IO>
 static int launch(const kv8_attn_args &a, const kv8_plan &p, hipStream_t s)
 {
     const dim3 grid(p.units * a.pool.n_heads, p.nsplit);
-    if (p.tr == 16) k_kv8_attn<HD, 1, IO><<<grid, 256, 0, s>>>(a);
+    if (p.tr == 16) k_kv8_attn<HD, IO><<<grid, 256, 0, s>>>(a);
     else {
         if (kv8_wide<HD, 1>::lds > 65536) { const int rc = allow_lds<HD, IO>(); if (rc != PV_OK) return rc; }
         if (p.tr == 64) k_kv8_attn_wide<HD, 1, IO><<<grid, 256, kv8_wide<HD, 1>::lds, s>>>(a);

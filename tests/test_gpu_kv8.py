@@ -210,6 +210,32 @@ def test_pages_and_lengths_that_do_not_exist(pv):
     check_attention(s, q, out, lse, prefix=prefix, tables=t, untouched=7.0)
 
 
+@pytest.mark.parametrize("rows", [1, 9, 40])
+def test_lengths_up_to_the_largest(pv, rows):
+    """Rows behind a table's end are no tokens, wherever they begin; all that exist are seen.  Tables without pages: nothing is."""
+    s = Setup(pv, [64 - rows], [rows], heads=2, hd=128)
+    s.fill_prefix()
+    s.pool.append(s.seqs(), s.draw(s.n, "bf16").cuda(), s.draw(s.n, "bf16").cuda())
+    before = s.pool.codes.clone()
+    q = torch.from_numpy(s.r.normal(size=(rows, 8, 128))).to(torch.bfloat16).cuda()
+    masks = dev(s.r.integers(0, 2 ** 63, rows), torch.int64)
+    for mask in (None, masks):
+        want = s.pool.attention(s.seqs(prefix=[64]), q, mask=mask, return_lse=True)
+        assert torch.isfinite(want[1]).all()
+        for far in (2 ** 30, 2 ** 31 - 1 - rows, 2 ** 31 - 2, 2 ** 31 - 1):
+            got = s.pool.attention(s.seqs(prefix=[far]), q, mask=mask, return_lse=True)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), far
+            s.pool.append(s.seqs(prefix=[far]), s.draw(rows, "bf16").cuda(), s.draw(rows, "bf16").cuda())
+            k, v = s.pool.read(s.seqs(prefix=[far]), rows)
+            assert not k.any() and not v.any()
+    assert torch.equal(s.pool.codes, before)
+    none = s.seqs(tables=np.zeros((1, 0), np.int32))
+    out, lse = s.pool.attention(none, q, return_lse=True)
+    assert not out.any() and torch.isneginf(lse).all()
+    s.pool.append(none, s.draw(rows, "bf16").cuda(), s.draw(rows, "bf16").cuda())
+    assert not s.pool.read(none, rows)[0].any() and torch.equal(s.pool.codes, before)
+
+
 def check_attention(s, q, out, lse, scale=None, masks=None, prefix=None, tables=None, untouched=None):
     scale = 1 / np.sqrt(s.hd) if scale is None else scale
     want, wlse, mag, mine = ref.attention(s.ref, s.start, s.prefix if prefix is None else prefix, s.tables if tables is None else tables, q.double().numpy(), scale, masks)

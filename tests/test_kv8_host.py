@@ -43,7 +43,8 @@ def test_sizes():
 
 
 BAD_POOLS = [(dict(codes=None), -1), (dict(scales=None), -1), (dict(head_dim=32), -1), (dict(head_dim=96), -1), (dict(n_pages=0), -3), (dict(n_pages=1 << 26), -3), (dict(n_kv_heads=0), -3),
-             (dict(page_tokens=8), -1), (dict(page_tokens=48), -1), (dict(page_tokens=1 << 17), -1), (dict(codes=0x1008), -1), (dict(scales=0x2001), -1)]
+             (dict(page_tokens=8), -1), (dict(page_tokens=48), -1), (dict(page_tokens=1 << 17), -1), (dict(codes=0x1008), -1), (dict(scales=0x2001), -1),
+             (dict(n_kv_heads=512, head_dim=64, page_tokens=1 << 16), -3)]
 BAD_SEQS = [(dict(row_start=None), -1), (dict(prefix_len=None), -1), (dict(page_table=None), -1), (dict(n_seq=-1), -3), (dict(n_rows=-1), -3), (dict(table_pages=-1), -3),
             (dict(n_seq=(1 << 20) + 1), -3), (dict(n_rows=(1 << 24) + 1), -3)]
 
