@@ -171,6 +171,8 @@ k_logprobs(const lp_args a)
     if (__any(!(t.s < INFINITY && t.w == t.w))) {             // -infinity (its exponential, 0, times it is no number), NaN, +infinity, products over the largest number
         t.s = t.m == INFINITY ? __uint_as_float(0x7fc00000u) : 0.f; t.w = t.s;
 #pragma unroll
+        for (int d = 0; d < D; ++d) if (sizeof(T) == 2) asm volatile("" : "+v"(x[d]));     // (as above: the loop before would keep all numbers for this one)
+#pragma unroll
         for (int i = 0; i < E; ++i) {
             const float y = fmaxf((lp_clean(lp_get<T>(x, i)) - ref) * 1.44269504088896340736f, -256.f), e = __builtin_amdgcn_exp2f(y);      // (2^-256 is 0)
             t.s += e;
@@ -356,9 +358,9 @@ template <typename T>
 static int launch(const lp_args &a, const lp_plan &p, hipStream_t s)
 {
     const unsigned grid = (unsigned)(a.rows * a.segs);
-    // f16: three workgroups of 512 threads a CU overlap better than two of 1024 (4096 rows of 32000, 20 alternatives 76 -> 59 us); bf16 does not fit the registers so (86 us), f32 has no need (50 of 40)
-    constexpr int NT = __is_same(T, _Float16) ? 512 : 1024;
-    if (p.large) k_logprobs<T, NT, 32768 / NT><<<grid, NT, 0, s>>>(a);
+    // 512 threads: three workgroups or more a CU, of which some load while others compute (4096 bf16 rows of 32000, 20 alternatives: 256 threads 66 us, 512 57, 1024 75, to be read in 40; 2048 f32 rows
+    // 50, 45, 50)
+    if (p.large) k_logprobs<T, 512, 64><<<grid, 512, 0, s>>>(a);
     else k_logprobs<T, 256, 16><<<grid, 256, 0, s>>>(a);
     PV_HIP(hipGetLastError());
     if (a.segs > 1) { k_logprobs_join<T><<<(unsigned)a.rows, 256, 0, s>>>(a); PV_HIP(hipGetLastError()); }
