@@ -164,43 +164,52 @@ struct kv8_read_args {
     int chunk;
 };
 
-// The same walk the other way: a token whose page is not one of the pool reads as zeros.
+// The same walk the other way, a wave a block and head, keys and values asked for together: a token whose page is not one of the pool reads as zeros.  V's bytes change places through LDS.
+// 65000 tokens of eight heads of 128, bf16: 64.6 us with a wave each for keys and values and loads through the caches, 55.9 so (277 MB, 53.7 at a copy's rate)
 template <int HD, typename T>
 __global__ void __launch_bounds__(64)
 k_kv8_read(const kv8_read_args a)
 {
     constexpr int NP = HD / 64, PR = HD / 16;
     __shared__ uint32_t tile[16 * HD / 4];
-    const int lane = threadIdx.x, which = blockIdx.x & 1, head = blockIdx.x >> 1;
-    char *dst = a.dst[which] + (int64_t)head * a.head_bytes[which];
+    const int lane = threadIdx.x, head = blockIdx.x;
     kv8_each_block<HD>(a.seqs, a.pool, blockIdx.y * a.chunk, a.chunk, [&](const kv8_seq &q, int row, int pos, int off, int n) {
         const int page = kv8_page(q, pos >> q.pool.page_shift), sub = (pos & ((1 << q.pool.page_shift) - 1)) >> 4;
-        const uint8_t *codes = q.pool.codes + kv8_block<HD>(q.pool, max(page, 0), head, which, sub);
-        const float f = page < 0 ? 0.f : kv8_pow2(kv8_byte(q.pool.scales[kv8_scale(q.pool, page, head, which, sub)]) - 127);
-        uint4 c[NP];
+        uint4 c[2][NP];
+        float f[2] = {0.f, 0.f};
 #pragma unroll
-        for (int k = 0; k < NP; ++k) c[k] = make_uint4(0u, 0u, 0u, 0u);
-        if (page >= 0 && which == 1) {
-            const int g = lane >> 4, jl = lane & 15;
+        for (int k = 0; k < NP; ++k) c[0][k] = c[1][k] = make_uint4(0u, 0u, 0u, 0u);
+        if (page >= 0) {
+            const uint8_t *keys = q.pool.codes + kv8_block<HD>(q.pool, page, head, 0, sub), *values = q.pool.codes + kv8_block<HD>(q.pool, page, head, 1, sub);
+            const uint32_t bytes = *(const uint16_t *)(q.pool.scales + kv8_scale(q.pool, page, head, 0, sub));
 #pragma unroll
-            for (int h = 0; h < NP; ++h) {
-                const uint4 v = ((const uint4 *)codes)[h * 64 + lane];
-                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                for (int q4 = 0; q4 < 4; ++q4)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) ((uint8_t *)tile)[(4 * g + r) * HD + (4 * h + q4) * 16 + jl] = (uint8_t)(w[q4] >> (8 * r));
+            for (int k = 0; k < NP; ++k) {
+                const int piece = k * 64 + lane, t = piece / PR, p = piece % PR;
+                c[0][k] = load_once((const uint4 *)(keys + (p * 16 + t) * 16)); c[1][k] = load_once((const uint4 *)values + k * 64 + lane);
             }
-            __syncthreads();
+            f[0] = kv8_pow2(kv8_byte(bytes & 0xffu) - 127); f[1] = kv8_pow2(kv8_byte(bytes >> 8) - 127);
         }
+        const int g = lane >> 4, jl = lane & 15;
+#pragma unroll
+        for (int h = 0; h < NP; ++h) {
+            const uint32_t w[4] = {c[1][h].x, c[1][h].y, c[1][h].z, c[1][h].w};
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) ((uint8_t *)tile)[(4 * g + r) * HD + (4 * h + q4) * 16 + jl] = (uint8_t)(w[q4] >> (8 * r));
+        }
+        __syncthreads();
 #pragma unroll
         for (int k = 0; k < NP; ++k) {
             const int piece = k * 64 + lane, t = piece / PR, p = piece % PR;
-            if (page >= 0) c[k] = which == 0 ? *(const uint4 *)(codes + (p * 16 + t) * 16) : *(const uint4 *)&tile[t * (HD / 4) + p * 4];
+            c[1][k] = *(const uint4 *)&tile[t * (HD / 4) + p * 4];
             if (t < off || t >= off + n) continue;
-            float v[16];
-            kv8_value4(c[k].x, f, v); kv8_value4(c[k].y, f, v + 4); kv8_value4(c[k].z, f, v + 8); kv8_value4(c[k].w, f, v + 12);
-            kv8_el<T>::store(dst + (int64_t)(row + t - off) * a.row_bytes[which] + p * 16 * sizeof(T), v);
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                float v[16];
+                kv8_value4(c[w][k].x, f[w], v); kv8_value4(c[w][k].y, f[w], v + 4); kv8_value4(c[w][k].z, f[w], v + 8); kv8_value4(c[w][k].w, f[w], v + 12);
+                kv8_el<T>::store(a.dst[w] + (int64_t)head * a.head_bytes[w] + (int64_t)(row + t - off) * a.row_bytes[w] + p * 16 * sizeof(T), v);
+            }
         }
         __syncthreads();
     });
@@ -298,7 +307,7 @@ extern "C" int pv_kv8_append(const pv_kv8_pool *pool, const pv_kv8_seqs *seqs, c
 template <int HD>
 static int launch_read(const kv8_read_args &a, int dtype, unsigned gy, hipStream_t s)
 {
-    const dim3 grid(2 * a.pool.n_heads, gy);
+    const dim3 grid(a.pool.n_heads, gy);
     if (dtype == PV_F32) k_kv8_read<HD, float><<<grid, 64, 0, s>>>(a);
     else if (dtype == PV_BF16) k_kv8_read<HD, __bf16><<<grid, 64, 0, s>>>(a);
     else k_kv8_read<HD, _Float16><<<grid, 64, 0, s>>>(a);
