@@ -358,7 +358,8 @@ __device__ inline void kv8_finish4(const kv8_attn_args &a, const kv8_row &w, int
 }
 
 // Few rows: one workgroup is a kv head, a tile of 16 packed rows of a sequence, a chunk of its keys; the waves take 64 keys in turn, straight from memory to registers, and are joined
-// through LDS at the end.  Bound by the read of the codes: the next 64 keys' K is asked for when this one's scores are there, V when its products are.
+// through LDS at the end.  Bound by the read of the codes: the next 64 keys' K is asked for when this one's scores are there, V when its products are.  32 sequences of up to 8192 keys, one row of 32
+// heads each: 45.5 us and 4.9 for the chunks' join, 266 MB at 5.8 TB/s (a read stream: 6.55); one sequence of four rows over 65536 keys 25.9 and 4.6, 133 MB at 5.1.
 template <int HD, int IO>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 k_kv8_attn(const kv8_attn_args a)
@@ -567,7 +568,9 @@ k_kv8_attn(const kv8_attn_args a)
 }
 
 // Many rows: a workgroup is a kv head, 64 RT packed rows of a sequence (16 RT a wave), a chunk of its keys.  64 keys at a time go through LDS as 16-bit numbers: each wave asks for a
-// group of 16 two steps ahead and converts it one step ahead, once for all rows, while the products of this step run in the other wave of its SIMD.
+// group of 16 two steps ahead and converts it one step ahead, once for all rows, while the products of this step run in the other wave of its SIMD.  Bound by a wave's instructions: of 64 keys 64 products
+// of 16 turns, and beside them some 340 vector and 150 scalar instructions (exponentials, maxima, the rounding of the weights, the codes' conversion) that overlap with the other wave's products only in part.  Two
+// prompts of 2048 rows on 6100 tokens, 32 heads of 128: 428 us, 783 TFLOP/s (a library's product of 8192^3: 1254).
 template <int HD, int RT>
 struct kv8_wide {
     static constexpr int KS = HD / 32, ET = HD / 16;
@@ -839,16 +842,20 @@ k_kv8_attn_merge(const kv8_attn_args a, int TR)
 
 // ------------------------------- host side ----------------------------------------
 
-// How a call's work is cut.  Rows a tile, by the mean of a sequence's packed rows (what each has is on the device).  Chunks of keys until there are two workgroups a CU, all begun at once, or twice as many
-// where sequences of different lengths come out at different times: 4 rows over 65000 keys 31, 32, 39, 51 us with 256, 512, 1024, 2048 workgroups, 32 sequences of 256 .. 8192 keys 80, 64, 53, 57,
-// two prompts 540, 540, 583, 583 (128 rows a tile).
+// How a call's work is cut.  Rows a tile: 16, straight from memory, where sequences have no more (in the mean: what each has is on the device), and where the whole work is small, so that what the other kernel
+// pays for going through LDS weighs more than codes converted again for every 16 rows, unless more than two tiles read codes that an XCD's L2 does not hold; else 64 or 128.  Eight kv heads of 128, four query heads
+// each, us with 16 and the better of 64 and 128: one sequence of 4000 keys, 8, 64, 256, 512 rows 11.0 and 13.5, 19.4 and 21.6, 42.2 and 49.8, 76.5 and 74.9; of 60000 keys, 8, 16, 64 rows
+// 38.3 and 42.5, 55.8 and 45.9, 150.6 and 105.4; 16 of up to 4000, 8, 32, 256 rows each 31.0 and 38.5, 55.6 and 57.0, 257.9 and 220.6.
+// Chunks of keys until there are two workgroups a CU, all begun at once, or twice as many where sequences of different lengths come out at different times: 4 rows over 65000 keys 29.9, 31.4, 39.0, 50.7 us with 256,
+// 512, 1024, 2048 workgroups, 32 sequences of 256 .. 8192 keys 59.0, 63.0, 50.7, 54.5, two prompts 426, 427, 470, 464.
 struct kv8_plan { int tr, units, nsplit, chunk; };
 
-static kv8_plan plan(int n_seq, int n_rows, int group, int kv_heads, int64_t keys)
+static kv8_plan plan(int n_seq, int n_rows, int group, int kv_heads, int hd, int64_t keys)
 {
     kv8_plan p;
     const int64_t packed = (int64_t)n_rows * group;
-    p.tr = packed <= (int64_t)16 * n_seq ? 16 : packed <= (int64_t)64 * n_seq ? 64 : 128;
+    const bool little = packed * kv_heads <= (1 << 26) / (keys > 0 ? keys : 1) && (packed <= (int64_t)32 * n_seq || keys * 2 * hd <= 2 << 20);
+    p.tr = packed <= (int64_t)16 * n_seq || little ? 16 : packed <= (int64_t)64 * n_seq ? 64 : 128;
     p.units = (int)((packed + (int64_t)n_seq * (p.tr - 1)) / p.tr);
     const int64_t tiles = packed / p.tr > n_seq ? packed / p.tr : n_seq, base = tiles * kv_heads, most = (keys + 255) / 256, want = p.tr == 16 && n_seq > 1 ? 1024 : 512;
     int64_t n = (want + base - 1) / base;
@@ -883,7 +890,7 @@ extern "C" int pv_kv8_attention_bytes(const pv_kv8_pool *pool, const pv_kv8_seqs
     if (rc != PV_OK) return rc;
     if (!bytes) { pv_set_error("null output pointer"); return PV_EINVAL; }
     const int group = n_q_heads / pool->n_kv_heads;
-    *bytes = seqs->n_seq && seqs->n_rows ? part_bytes(plan(seqs->n_seq, seqs->n_rows, group, pool->n_kv_heads, (int64_t)seqs->table_pages * pool->page_tokens), seqs->n_rows, n_q_heads, pool->head_dim) : 0;
+    *bytes = seqs->n_seq && seqs->n_rows ? part_bytes(plan(seqs->n_seq, seqs->n_rows, group, pool->n_kv_heads, pool->head_dim, (int64_t)seqs->table_pages * pool->page_tokens), seqs->n_rows, n_q_heads, pool->head_dim) : 0;
     return PV_OK;
 }
 
@@ -933,7 +940,7 @@ extern "C" int pv_kv8_attention(const pv_kv8_pool *pool, const pv_kv8_seqs *seqs
     if (!(scale - scale == 0.f)) { pv_set_error("scale is not finite"); return PV_EINVAL; }
     if (((uintptr_t)mask & 7) || ((uintptr_t)lse & 3)) { pv_set_error("mask or lse is not aligned"); return PV_EINVAL; }
     const int group = n_q_heads / pool->n_kv_heads;
-    const kv8_plan p = plan(seqs->n_seq, seqs->n_rows, group, pool->n_kv_heads, (int64_t)seqs->table_pages * pool->page_tokens);
+    const kv8_plan p = plan(seqs->n_seq, seqs->n_rows, group, pool->n_kv_heads, pool->head_dim, (int64_t)seqs->table_pages * pool->page_tokens);
     const size_t need = part_bytes(p, seqs->n_rows, n_q_heads, pool->head_dim);
     if (need > workspace_bytes || (need && !workspace)) { pv_set_error("workspace of %zu bytes, %zu are needed", workspace ? workspace_bytes : (size_t)0, need); return PV_ENOMEM; }
     if ((uintptr_t)workspace & 15) { pv_set_error("workspace must be 16-byte aligned"); return PV_EINVAL; }
@@ -958,7 +965,7 @@ int pv_kv8_step_attention(pv_cache *c, const pv_kv8_step &st, hipStream_t s)
     a.seqs = pv_kv8_step_seqs(c, st.layer, st.rows, -1, &a.pool);
     a.group = f.n_q_heads / f.n_kv_heads; a.n_q_heads = f.n_q_heads;
     const int64_t room = (int64_t)c->n_pages * f.page_tokens, keys = st.prompt ? c->len + st.rows : c->attn_keys > 0 && c->attn_keys < room ? c->attn_keys : room;
-    kv8_plan p = plan(a.seqs.n_seq, st.rows, a.group, f.n_kv_heads, keys);
+    kv8_plan p = plan(a.seqs.n_seq, st.rows, a.group, f.n_kv_heads, f.head_dim, keys);
     while (p.nsplit > 1 && part_bytes(p, st.rows, f.n_q_heads, f.head_dim) > st.n_part * sizeof(float)) { p.chunk *= 2; p.nsplit = (int)((keys + p.chunk - 1) / p.chunk); }
     // a recorded step serves all lengths up to its bound
     a.nsplit = p.nsplit; a.chunk = p.chunk;

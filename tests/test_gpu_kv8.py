@@ -28,6 +28,7 @@ def dev(a, dtype=torch.int32):
 
 class Setup:
     """A pool full of bytes that mean nothing, shuffled tables, ragged sequences."""
+    room = 0                                                              # pages that no sequence has, behind those of its table
 
     def __init__(self, pv, prefix, rows, heads=2, hd=64, pt=16, seed=0, fill=0xFF, extra_pages=1, tail_rows=0):
         r = self.r = np.random.default_rng(seed)
@@ -44,7 +45,9 @@ class Setup:
         self.pv = pv
 
     def seqs(self, start=None, prefix=None, tables=None):
-        return self.pv.KV8Seqs(dev(self.start if start is None else start), dev(self.prefix if prefix is None else prefix), dev(self.tables if tables is None else tables))
+        tables = np.asarray(self.tables if tables is None else tables)
+        tables = np.concatenate([tables, np.full((tables.shape[0], self.room), -1, tables.dtype)], axis=1)
+        return self.pv.KV8Seqs(dev(self.start if start is None else start), dev(self.prefix if prefix is None else prefix), dev(tables))
 
     def draw(self, n, dtype, spread=2.0):
         x = torch.from_numpy(self.r.normal(size=(n, self.heads, self.hd)) * 2.0 ** self.r.uniform(-spread, spread, size=(n, self.heads, 1))).to(TYPES[dtype])
@@ -409,3 +412,53 @@ def test_two_streams_at_once(pv):
     torch.cuda.synchronize()
     for (_, _, _, want), outs in zip(sets, got):
         assert all(torch.equal(o, want) for o in outs)
+
+
+@pytest.fixture()
+def long_tables(monkeypatch):
+    """Tables as of 20000 tokens, most of them of no page: what many rows over long contexts are worked through by, at sizes of a test."""
+    monkeypatch.setattr(Setup, "room", 1250)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("prefix,rows,kvh,heads,pt", [([300], [9], 2, 8, 16), ([255], [10], 1, 4, 64), ([1100], [33], 2, 4, 16), ([0], [17], 2, 8, 16), ([0], [130], 1, 4, 16), ([77], [65], 2, 6, 32),
+                                                      ([513], [33], 1, 16, 16), ([0, 40, 0, 511, 1000], [30, 0, 11, 9, 41], 2, 8, 16), ([200, 0, 31], [1, 100, 40], 2, 8, 16), ([90], [5], 1, 70, 16)])
+def test_many_rows_over_long_tables(pv, long_tables, prefix, rows, kvh, heads, pt, dtype, hd):
+    test_attention(pv, prefix, rows, kvh, heads, pt, dtype, hd)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("prefix,rows", [([100], [48]), ([0], [9]), ([300, 0, 17], [64, 5, 20]), ([50], [70])])
+def test_masks_over_long_tables(pv, long_tables, prefix, rows, dtype):
+    test_attention_with_masks(pv, prefix, rows, dtype)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("rows", [10, 70])
+def test_what_a_row_does_not_see_over_long_tables(pv, long_tables, bad, rows):
+    test_what_a_row_does_not_see_has_no_influence(pv, bad, rows)
+
+
+def test_missing_pages_and_strides_over_long_tables(pv, long_tables):
+    test_pages_and_lengths_that_do_not_exist(pv)
+    test_in_place_and_strided_queries(pv)
+
+
+@pytest.mark.parametrize("rows", [1, 10, 40])
+def test_scales_far_apart_for_any_number_of_rows(pv, monkeypatch, rows):
+    """The case of the two rows, with as many as are worked through in other ways."""
+    monkeypatch.setattr(Setup, "room", 1250)
+    s = Setup(pv, [400], [rows], heads=1, hd=64)
+    n = 400 + rows
+    k, v = torch.from_numpy(s.r.normal(size=(n, 1, 64))).float() * 0.1, torch.from_numpy(s.r.normal(size=(n, 1, 64))).float()
+    v[:200] *= 2.0 ** -20
+    v[200:216] *= 2.0 ** 20
+    k[200:216] = -k[0] * 100
+    k[0], v[0] = 3.0, 1e-12
+    s.pool.append(s.seqs([0, n], [0]), k.cuda(), v.cuda())
+    s.ref.append([0, n], [0], s.tables, k.double().numpy(), v.double().numpy())
+    q = (torch.ones(rows, 6, 64) * torch.linspace(1, 0.5, 6).view(1, 6, 1)).to(torch.bfloat16)
+    for scale in (0.02, 0.07, -0.02):
+        out, lse = s.pool.attention(s.seqs(), q.cuda(), scale=scale, return_lse=True)
+        check_attention(s, q, out, lse, scale=scale)

@@ -116,6 +116,36 @@ def test_long_prompts_and_contexts(pvlib):
     same_cache(gc, rc, 0.06)
 
 
+def test_a_prompt_of_many_packed_rows(pvlib):
+    """1500 tokens of 32 query heads on one kv head in one pass."""
+    _, gc, rc = pair(pvlib, WIDE_GROUP, room=1600)
+    prompt = pv_inputs.uniform_tokens(75, 1500, WIDE_GROUP.vocab)
+    gc.prefill(prompt)
+    assert err(gc.debug_logits()[-1:], rc.prefill(prompt, 1500)[None]) < 3e-2
+    step(gc, rc, pv_inputs.uniform_tokens(76, 64, WIDE_GROUP.vocab))
+    gc.rollback(1500)
+    rc.rollback(1500)
+    same_cache(gc, rc)
+
+
+LONG = S("kv8_long", 1, 256, 4, 1, 128, 352, 512, dtype="bf16", seed=9106)
+
+
+def test_steps_over_a_long_context(pvlib):
+    """More keys than an XCD's L2 holds: blocks of one row, of 12 and of 40 and more are worked through in three ways."""
+    _, gc, rc = pair(pvlib, LONG, room=8900)
+    for i in range(8):
+        piece = pv_inputs.uniform_tokens(77 + i, 1050, LONG.vocab)
+        gc.prefill(piece)
+        last = rc.prefill(piece, 1050)
+    assert err(gc.debug_logits()[-1:], last[None]) < 3e-2
+    for gamma in (1, 8, 12, 40, 64):
+        step(gc, rc, pv_inputs.uniform_tokens(90 + gamma, gamma, LONG.vocab))
+        gc.rollback(8400)
+        rc.rollback(8400)
+    same_cache(gc, rc)
+
+
 def test_graphs_static_steps_and_shuffled_pages_change_nothing(pvlib):
     gm, a, _ = pair(pvlib, MHA)
     caches = [a] + [pvlib.Cache(gm, 512, kv_bits=8) for _ in range(3)]
