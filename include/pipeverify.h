@@ -329,7 +329,7 @@ int pv_kv8_bytes(const pv_kv8_pool *pool, size_t *codes_bytes, size_t *scales_by
  * 2^-100 on) that leaves no code above 448; a block that holds earlier tokens (positions below prefix_len) keeps its scale, or, if a new token needs a larger one, has their codes
  * rounded to that.  Codes are rounded to nearest, ties to the even code; what is not finite becomes NaN and has no say in the scale.  k, v: element (row, head, feature) at
  * row * row_stride + head * head_stride + feature, of type dtype (pv_dtype); addresses and strides multiples of 16 bytes.  A page must not be
- * the place of rows of two sequences of a call. */
+ * the place of rows twice in a call, neither of two sequences nor under two entries of a table (what such a page holds then is not defined; nothing outside it is touched). */
 int pv_kv8_append(const pv_kv8_pool *pool, const pv_kv8_seqs *seqs, const void *k, int64_t k_row_stride, int64_t k_head_stride,
                   const void *v, int64_t v_row_stride, int64_t v_head_stride, int32_t dtype, void *hip_stream);
 
