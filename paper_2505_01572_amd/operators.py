@@ -226,10 +226,12 @@ def token_logprobs(logits, tokens=None, top=0, stream=None):
         if len(_logprobs_need) > 256:
             _logprobs_need.clear()
         need = _logprobs_need[key] = b.value
-    lp = logits.new_empty(shape, dtype=torch.float32)
-    stats = logits.new_empty((2, rows), dtype=torch.float32)
+    if len(shape) == 1:                                    # (one allocation for all three)
+        lp, entropy, lse = logits.new_empty((3, rows), dtype=torch.float32).unbind(0)
+    else:
+        lp = logits.new_empty(shape, dtype=torch.float32)
+        entropy, lse = logits.new_empty((2, rows), dtype=torch.float32).unbind(0)
     ids, best = logits.new_empty((rows, top), dtype=torch.int32), logits.new_empty((rows, top), dtype=torch.float32)
-    entropy, lse = stats.unbind(0)
     ws = logits.new_empty(need, dtype=torch.uint8) if need else None
     rc = L.pv_token_logprobs(logits.data_ptr(), row_stride, _DTYPES[logits.dtype], rows, vocab, tp, n, lp.data_ptr(), entropy.data_ptr(), lse.data_ptr(),
                              top, ids.data_ptr(), best.data_ptr(), None if ws is None else ws.data_ptr(), need, _raw_stream(index))

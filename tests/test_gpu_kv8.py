@@ -462,3 +462,33 @@ def test_scales_far_apart_for_any_number_of_rows(pv, monkeypatch, rows):
     for scale in (0.02, 0.07, -0.02):
         out, lse = s.pool.attention(s.seqs(), q.cuda(), scale=scale, return_lse=True)
         check_attention(s, q, out, lse, scale=scale)
+
+
+def test_graphs_and_eager_calls_at_once(pv):
+    """Calls of three kinds, captured apart, replayed on three streams while eager ones run on a fourth: nobody's workspace is another's."""
+    calls = []
+    for n, length, room in ((1, 2000, 0), (40, 2000, 1250), (9, 1500, 0)):
+        s = Setup(pv, [length], [n], heads=2, hd=128, fill=0)
+        s.pool.codes.random_(0, 120)
+        s.pool.scales.fill_(120)
+        s.room = room
+        calls.append((s.pool, s.seqs(), torch.from_numpy(s.r.normal(size=(n, 8, 128))).to(torch.bfloat16).cuda()))
+    want = [pool.attention(seqs, q, return_lse=True) for pool, seqs, q in calls]
+    torch.cuda.synchronize()
+    graphs = []
+    for pool, seqs, q in calls:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            got = pool.attention(seqs, q, return_lse=True)
+        graphs.append((g, got))
+    streams = [torch.cuda.Stream() for _ in graphs]
+    for _ in range(4):
+        for (g, got), x in zip(graphs, streams):
+            got[0].zero_()
+            x.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(x):
+                g.replay()
+        eager = [pool.attention(seqs, q, return_lse=True) for pool, seqs, q in calls]
+        torch.cuda.synchronize()
+        for (_, got), w, e in zip(graphs, want, eager):
+            assert all(torch.equal(i, j) and torch.equal(k, j) for i, j, k in zip(got, w, e)) and torch.isfinite(w[0]).all()

@@ -129,3 +129,18 @@ def test_runs_are_the_same_and_graphs_replay(pv):
         want = pv.token_logprobs(x, tokens, top=10)
         assert all(torch.equal(a, b) for a, b in zip(got, want)), i
     torch.cuda.synchronize()
+
+
+def test_two_streams_at_once(pv):
+    x, y = torch.randn(8, 128256, device="cuda"), torch.randn(300, 32000, device="cuda").to(torch.bfloat16)
+    a, b = torch.arange(8, dtype=torch.int32, device="cuda"), torch.arange(600, dtype=torch.int32, device="cuda").view(300, 2)
+    want = [pv.token_logprobs(x, a, top=5), pv.token_logprobs(y, b, top=20)]
+    streams = [torch.cuda.Stream() for _ in want]
+    for _ in range(4):
+        got = []
+        for s, args in zip(streams, ((x, a, 5), (y, b, 20))):
+            s.wait_stream(torch.cuda.current_stream())
+            got.append(pv.token_logprobs(*args, stream=s))
+        torch.cuda.synchronize()
+        for u, w in zip(got, want):
+            assert all(torch.equal(i, j) for i, j in zip(u, w))
