@@ -226,8 +226,10 @@ def token_logprobs(logits, tokens=None, top=0, stream=None):
         if len(_logprobs_need) > 256:
             _logprobs_need.clear()
         need = _logprobs_need[key] = b.value
-    if len(shape) == 1:                                    # (one allocation for all three)
+    if n == 1:                                             # (one allocation for all three)
         lp, entropy, lse = logits.new_empty((3, rows), dtype=torch.float32).unbind(0)
+        if len(shape) == 2:
+            lp = lp.view(shape)
     else:
         lp = logits.new_empty(shape, dtype=torch.float32)
         entropy, lse = logits.new_empty((2, rows), dtype=torch.float32).unbind(0)
