@@ -849,6 +849,8 @@ k_kv8_attn_merge(const kv8_attn_args a, int TR)
 // 38.3 and 42.5, 55.8 and 45.9, 150.6 and 105.4; 16 of up to 4000, 8, 32, 256 rows each 31.0 and 38.5, 55.6 and 57.0, 257.9 and 220.6.
 // Chunks of keys until there are two workgroups a CU, all begun at once, or twice as many where sequences of different lengths come out at different times: 4 rows over 65000 keys 29.9, 31.4, 39.0, 50.7 us with 256,
 // 512, 1024, 2048 workgroups, 32 sequences of 256 .. 8192 keys 59.0, 63.0, 50.7, 54.5, two prompts 426, 427, 470, 464.
+// Few keys are one workgroup's, which saves the launch that joins: up to 1024, 768 with more than 16 rows a sequence, 2048 where there is a workgroup a CU (in chunks and whole, from a graph, 8 kv heads: one row over 500 keys 9.2
+// and 7.6 us, 760 9.3 and 8.9, 1020 9.1 and 10.1, 1500 9.5 and 12.6, called one by one 13.5 and 9.5, 13.3 and 10.0, 13.3 and 12.6; 16 rows over 760 9.5 and 10.4, 13.2 and 10.3; 32 sequences of up to 1020 17.1 and 11.9, 2040 21.8 and 18.2).
 struct kv8_plan { int tr, units, nsplit, chunk; };
 
 static kv8_plan plan(int n_seq, int n_rows, int group, int kv_heads, int hd, int64_t keys)
@@ -862,6 +864,7 @@ static kv8_plan plan(int n_seq, int n_rows, int group, int kv_heads, int hd, int
     int64_t n = (want + base - 1) / base;
     n = n < most ? n : most;
     n = n < 256 ? n : 256;
+    if (p.tr == 16 && most <= (base >= 256 ? 8 : packed <= (int64_t)16 * n_seq ? 4 : 3)) n = 1;
     n = n > 1 ? n : 1;
     p.chunk = (int)(((keys + n - 1) / n + 255) / 256 * 256);
     p.chunk = p.chunk > 256 ? p.chunk : 256;

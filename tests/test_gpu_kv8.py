@@ -422,7 +422,7 @@ def long_tables(monkeypatch):
 
 @pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
-@pytest.mark.parametrize("prefix,rows,kvh,heads,pt", [([300], [9], 2, 8, 16), ([255], [10], 1, 4, 64), ([1100], [33], 2, 4, 16), ([0], [17], 2, 8, 16), ([0], [130], 1, 4, 16), ([77], [65], 2, 6, 32),
+@pytest.mark.parametrize("prefix,rows,kvh,heads,pt", [([300], [1], 2, 8, 16), ([700], [4], 1, 5, 16), ([0, 40, 0, 511, 1000], [3, 0, 1, 9, 1], 2, 8, 16), ([5] * 70, [1] * 70, 1, 2, 16), ([300], [9], 2, 8, 16), ([255], [10], 1, 4, 64), ([1100], [33], 2, 4, 16), ([0], [17], 2, 8, 16), ([0], [130], 1, 4, 16), ([77], [65], 2, 6, 32),
                                                       ([513], [33], 1, 16, 16), ([0, 40, 0, 511, 1000], [30, 0, 11, 9, 41], 2, 8, 16), ([200, 0, 31], [1, 100, 40], 2, 8, 16), ([90], [5], 1, 70, 16)])
 def test_many_rows_over_long_tables(pv, long_tables, prefix, rows, kvh, heads, pt, dtype, hd):
     test_attention(pv, prefix, rows, kvh, heads, pt, dtype, hd)
