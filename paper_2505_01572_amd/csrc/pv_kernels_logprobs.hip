@@ -325,12 +325,13 @@ k_logprobs_join(const lp_args a)
 
 // ------------------------------- host side ----------------------------------------
 
-// Segments of 4096 numbers, or of 32768: the larger where there are rows enough for the chip and numbers enough in a row, or where more than 64 segments would come out
+// Segments of 4096 numbers, or of 32768: the larger where that is a row, which saves the launch that joins (8 f32 rows of 16384, five alternatives, called one by one 17.7 and 13.9 us, from a graph 8.3 and 8.9; of
+// 32000 17.7 and 13.6, 8.5 and 9.1; 200 rows of 32000 17.9 and 13.8, 12.5 and 10.6), where there are rows enough for the chip, or where more than 64 segments would come out
 struct lp_plan { bool large; int segs; };
 static lp_plan plan(int64_t rows, int vocab)
 {
     lp_plan p;
-    p.large = (rows >= 256 && vocab > 4096) || vocab > 4096 * LP_MAX_SEGS;
+    p.large = vocab > 4096 && (vocab <= 32768 || rows >= 256 || vocab > 4096 * LP_MAX_SEGS);
     const int n = p.large ? 32768 : 4096;
     p.segs = (vocab + n - 1) / n;
     return p;
