@@ -9,11 +9,11 @@
 //   V   f16 without its scale.  P = 2^15 times the weight, f16: 11 significant bits for weights from 2^-29 on, so that many small ones beside one that takes nearly all count fully; one bf16
 //       would add as much error as the rounding of a bf16 output.  For f16 outputs P is a pair of f16, or its rounding would be as large as theirs (in a step, whose keys and values have four bits, one is enough).
 //       V's scales 2^ev go into the weights' exponents, relative to the unit of the accumulators, 2^E, the largest so far; where one is below 2^-14 of that, the
-//       groups of 16 keys are gone through one after the other, each in its own unit.  (Of values whose scales are more than 2^100
-//       below others of their kv head little is left.)
+//       groups of 16 keys are gone through one after the other, each in its own unit, down to 2^-64 of the largest so far (pv_kv8_units.h: what is further below adds nothing).
 #include <atomic>
 #include <stddef.h>
 #include "pv_kv8.h"
+#include "pv_kv8_units.h"
 
 enum { KV8_BF16 = 0, KV8_F16 = 1, KV8_STEP1 = 2, KV8_STEP2 = 3 };       // queries and outputs: a caller's, or a model's step (operand layouts of 1 .. 8 rows and of more)
 template <int IO> struct kv8_types {
@@ -150,8 +150,7 @@ __device__ inline void kv8_store4(const kv8_attn_args &a, int row, int head, int
 }
 
 // Running result for RT tiles of 16 rows: lane (g, jl) has row jl's maximum and its part of 2^15 times the sum, and features 16 e + 4 g .. + 3 of the output times 2^(15 - E)
-template <int HD, int RT> struct kv8_acc { f32x4 O[RT][HD / 16]; float m[RT], l[RT]; int E; };
-#define KV8_NO_SCALE (-1000)                // exponent of a group that does not exist
+template <int HD, int RT> struct kv8_acc { f32x4 O[RT][HD / 16]; float m[RT], l[RT]; int E, top; };       // E, top: kv8_next_unit
 
 template <int HD, int RT> __device__ inline void kv8_begin(kv8_acc<HD, RT> &A)
 {
@@ -161,7 +160,7 @@ template <int HD, int RT> __device__ inline void kv8_begin(kv8_acc<HD, RT> &A)
 #pragma unroll
         for (int e = 0; e < HD / 16; ++e) A.O[t][e] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
-    A.E = KV8_NO_SCALE;
+    A.E = A.top = KV8_NO_SCALE;
 }
 
 // The accumulators in another unit
@@ -178,26 +177,12 @@ template <int HD, int RT> __device__ inline void kv8_unit_is(kv8_acc<HD, RT> &A,
     A.E = E;
 }
 
-// V's exponents of four groups against the accumulators' unit, which grows with them: dv.  Where they are too far apart, `only` one group is looked at at a time, from 0 to 3 (-1: all).
+// The unit for four groups of V's exponents (kv8_next_unit)
 template <int HD, int RT> __device__ inline void kv8_units(kv8_acc<HD, RT> &A, const int (&ev)[4], int (&dv)[4], int &only)
 {
-    const int e0 = ev[0], e1 = ev[1], e2 = ev[2], e3 = ev[3], top = max(max(max(e0, e1), max(e2, e3)), A.E);
-    int E = top, lowest = -1000000;
-    bool one = false;
-    if (!(only < 0 && min(min(e0, e1), min(e2, e3)) - top >= -14)) {     // (seldom; few scalar instructions else, which take a wave's turns as others do)
-        auto far = [&](int e) { return (int)(e != KV8_NO_SCALE) & (int)(e - top < -14); };
-        if (only < 0 && (far(e0) | far(e1) | far(e2) | far(e3))) only = 0;
-        one = only >= 0;
-        const int mine = only == 0 ? e0 : only == 1 ? e1 : only == 2 ? e2 : e3;
-        if (one) E = mine == KV8_NO_SCALE ? A.E : max(mine, A.E - 100);
-        lowest = -100;
-    }
+    int E = A.E;
+    kv8_next_unit(ev, E, A.top, dv, only);
     if (E != A.E) kv8_unit_is(A, E);
-    dv[0] = max(e0 - E, lowest); dv[1] = max(e1 - E, lowest); dv[2] = max(e2 - E, lowest); dv[3] = max(e3 - E, lowest);
-    if (one) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) dv[i] = i != only ? 0 : dv[i];
-    }
 }
 
 // Which of 64 keys a row sees: those before `end`, without a mask; with one, those before len, and from there on those that the mask names, before nk.  Bit i: key p + i.
