@@ -424,7 +424,7 @@ k_kv8_attn(const kv8_attn_args a)
     load_k(p0);
     load_v();
     auto sees = [&](int t, int p) { return kv8_sees(a.mask != nullptr, vm[t], p + 4 * g, len, len + row[t].j + 1, nk); };
-    bool spoilt = false;                    // NaN among values that not every row sees
+    bool spoilt = false;                    // NaN among values that not every row sees, or beside a page that does not exist
     int only = -1;
     ahead[0] = ahead[1] = ahead[2] = ahead[3] = -1;
     if (p0 < k1) pages(p0 + 256, ahead);
@@ -502,8 +502,8 @@ k_kv8_attn(const kv8_attn_args a)
     }
     if (spoilt) {
         for (p0 = k0 + 64 * wave; p0 < k1; p0 += 256) {
-            if (p0 + 64 <= sure) continue;
             pages(p0, page);
+            if (p0 + 64 <= sure && exists(p0, 0) & exists(p0, 1) & exists(p0, 2) & exists(p0, 3)) continue;      // (their NaN went through the products)
             kv8_put_nans<HD, RT>(A, [&](int t) { return sees(t, p0); }, [&](int i, int b) {
                 if (!exists(p0, i)) return make_uint4(0u, 0u, 0u, 0u);
                 const uint4 c = ((const uint4 *)(codes + ((uint64_t)(uint32_t)page[i] * page_codes + block + ((p0 + 16 * i) & in_page) * HD)))[b * 64 + lane];
