@@ -168,7 +168,11 @@ k_logprobs(const lp_args a)
         t.s += e;
         t.w = fmaf(e, y, t.w);
     }
-    if (__any(!(t.s < INFINITY && t.w == t.w))) {             // -infinity (its exponential, 0, times it is no number), NaN, +infinity, products over the largest number
+    {   // What rounding left of c is in every y of the thread, and comes out of its sums
+        const float off = fmaf(ref, 1.44269504088896340736f, c), f = fabsf(off) < 0.5f ? __builtin_amdgcn_exp2f(-off) : INFINITY;
+        t.w = f * fmaf(-off, t.s, t.w); t.s *= f;
+    }
+    if (__any(!(t.s < INFINITY && t.w == t.w))) {             // -infinity (its exponential, 0, times it is no number), NaN, +infinity, products over the largest number, a maximum from some 2^23 on
         t.s = t.m == INFINITY ? __uint_as_float(0x7fc00000u) : 0.f; t.w = t.s;
 #pragma unroll
         for (int d = 0; d < D; ++d) if (sizeof(T) == 2) asm volatile("" : "+v"(x[d]));     // (as above: the loop before would keep all numbers for this one)
