@@ -355,7 +355,7 @@ int pv_kv8_attention(const pv_kv8_pool *pool, const pv_kv8_seqs *seqs, const voi
  * or NULL; top <= 32: top_ids (int32), top_logprobs (float) device [rows][top], most probable first, equal ones by the lower id.  All computed in 32 bits, in nats: lse = log(sum(exp(logit))),
  * log p = logit - lse, entropy = -sum(p log p).  A logit of -infinity (a masked token) has probability 0, and NaN counts as that, as in the arg-max of a step; a row of
  * nothing else has no probabilities: -infinity for each token and in lse, entropy 0.  A row with +infinity has NaN for all of them.  A token id outside [0, vocab) has the log probability NaN.
- * rows <= 2^24, vocab <= 2^21; workspace (rows of more than 32768 logits): at least pv_token_logprobs_bytes, 16-byte aligned, for this call alone until it has run. */
+ * vocab <= 2^21; rows < 2^24, with a vocab of more than 4096 rows * ceil(vocab / 32768) < 2^22; workspace (rows of more than 32768 logits): at least pv_token_logprobs_bytes, 16-byte aligned, for this call alone until it has run. */
 int pv_token_logprobs_bytes(int64_t rows, int32_t vocab, int32_t top, size_t *bytes);
 int pv_token_logprobs(const void *logits, int64_t row_stride, int32_t dtype, int64_t rows, int32_t vocab, const int32_t *tokens, int32_t n_tokens, float *logprobs,
                       float *entropy, float *lse, int32_t top, int32_t *top_ids, float *top_logprobs, void *workspace, size_t workspace_bytes, void *hip_stream);

@@ -343,9 +343,12 @@ static lp_plan plan(int64_t rows, int vocab)
 
 static int check(int64_t rows, int vocab, int top)
 {
-    if (rows < 0 || rows > (1 << 24)) { pv_set_error("rows %lld outside [0, 2^24]", (long long)rows); return PV_ERANGE; }
+    if (rows < 0 || rows > (1 << 24)) { pv_set_error("rows %lld outside [0, 2^24)", (long long)rows); return PV_ERANGE; }
     if (vocab < 1 || vocab > 32768 * LP_MAX_SEGS) { pv_set_error("vocab %d outside [1, %d]", vocab, 32768 * LP_MAX_SEGS); return PV_ERANGE; }
     if (top < 0 || top > LP_MAX_TOP || top > vocab) { pv_set_error("top %d outside [0, min(%d, vocab)]", top, LP_MAX_TOP); return PV_ERANGE; }
+    // a launch has less than 2^32 threads
+    const lp_plan p = plan(rows, vocab);
+    if (rows * p.segs >= (1 << 22) * (p.large ? 1ll : 4ll)) { pv_set_error("%lld rows of %d: more than a launch takes", (long long)rows, vocab); return PV_ERANGE; }
     return PV_OK;
 }
 
@@ -385,7 +388,6 @@ extern "C" int pv_token_logprobs(const void *logits, int64_t row_stride, int32_t
     const int64_t size = dtype == PV_F32 ? 4 : 2;
     if ((uintptr_t)logits % size) { pv_set_error("logits are not aligned to their type"); return PV_EINVAL; }
     const lp_plan p = plan(rows, vocab);
-    if (rows * p.segs >= (1 << 22) * (p.large ? 1ll : 4ll)) { pv_set_error("%lld rows of %d: more than a launch takes", (long long)rows, vocab); return PV_ERANGE; }
     size_t need = 0;
     pv_token_logprobs_bytes(rows, vocab, top, &need);
     if (need > workspace_bytes || (need && !workspace)) { pv_set_error("workspace of %zu bytes, %zu are needed", workspace ? workspace_bytes : (size_t)0, need); return PV_ENOMEM; }
