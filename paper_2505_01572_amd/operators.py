@@ -7,7 +7,7 @@
     got = pv.token_logprobs(logits, tokens, top=5)                    # log probabilities, entropy, alternatives
 
 Argument marshalling only; work is enqueued on `stream` (default: the current stream of the pool's device) and not waited for.  A tensor made on another stream
-is the caller's to order, as everywhere in torch.
+is the caller's to order, as everywhere in torch.  There are no gradients: tensors that require one are refused, unless gradients are switched off (torch.no_grad()).
 """
 import ctypes
 
@@ -41,6 +41,12 @@ class _Elsewhere:
         if self.stream is not None:
             self.stream.__exit__(*a)
         self.device.__exit__(*a)
+
+
+def _no_gradient(where, name, t):
+    """There is no backward pass: a result without a history where torch would give one would be a gradient lost in silence."""
+    if t.requires_grad and torch.is_grad_enabled():
+        _refuse(where, f"{name} requires a gradient, and this operator has none: call it under torch.no_grad(), or with {name}.detach()")
 
 
 def _elsewhere(index, stream):
@@ -107,6 +113,8 @@ class KV8Pool:
             _refuse(where, f"{name} must be [rows, {heads}, {self.head_dim}] of {tuple(dtypes)}, got {tuple(shape)} of {t.dtype}")
         if stride[2] != 1:
             _refuse(where, f"{name}: the features of a head must lie next to each other")
+        if t.requires_grad:
+            _no_gradient(where, name, t)
         return t.data_ptr(), stride[0], stride[1]
 
     def _seqs(self, seqs, where, n_rows):
@@ -185,6 +193,8 @@ class KV8Pool:
         if lse is not None:
             if not (isinstance(lse, torch.Tensor) and lse.device == self.device and lse.dtype == torch.float32 and lse.shape == (n, heads) and lse.is_contiguous()):
                 _refuse(where, f"lse must be a contiguous float32 tensor [{n}, {heads}] on {self.device}")
+            if lse.requires_grad:
+                _no_gradient(where, "lse", lse)
         elif return_lse:
             lse = q.new_empty((n, heads), dtype=torch.float32)
         ws = q.new_empty(need, dtype=torch.uint8) if need else None
@@ -204,6 +214,8 @@ def token_logprobs(logits, tokens=None, top=0, stream=None):
     where = "token_logprobs"
     if not (isinstance(logits, torch.Tensor) and logits.is_cuda and logits.dim() == 2 and logits.dtype in _DTYPES):
         _refuse(where, f"logits must be [rows, vocab] of {tuple(_DTYPES)} on the GPU")
+    if logits.requires_grad:
+        _no_gradient(where, "logits", logits)
     index = logits.device.index
     if _elsewhere(index, stream):
         with _Elsewhere(logits.device, stream):
