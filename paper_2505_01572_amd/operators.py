@@ -30,6 +30,8 @@ class _Elsewhere:
     """Makes device and stream current, so that what torch allocates belongs to the stream the kernels run on."""
 
     def __init__(self, device, stream):
+        if stream is not None and stream.device != device:
+            _refuse("stream", f"a stream of {stream.device} given for tensors on {device}")
         self.device, self.stream = torch.cuda.device(device), torch.cuda.stream(stream) if stream is not None else None
 
     def __enter__(self):
