@@ -151,7 +151,8 @@ void pv_cache_destroy(pv_cache *c);
 
 /* The same with keys and values in 8 bits (kv_bits = 8; 0: the model's storage type, which is what the two calls above give): half the memory and half of what a step reads of
  * them, e4m3 codes with a power-of-two scale for 16 tokens and head (the form is described at pv_kv8_pool below).  Keys and values are rounded to four significant bits when they are stored, and every row, also of
- * the block that brings them, attends to them as stored.  bf16 models with head_dim 64 or 128.  All calls on a cache work alike; the caches of a batch store alike.
+ * the block that brings them, attends to them as stored.  A block's later rows may change what is stored of earlier tokens of
+ * the same 16, whether they are accepted or not (pv_kv8_append says by how much).  bf16 models with head_dim 64 or 128.  All calls on a cache work alike; the caches of a batch store alike.
  * The page pool is the layers' codes ([n_layers] pools' codes), and behind them, rounded up to 256 bytes, their scales.  pv_cache_export gives the stored values (bf16, exact). */
 int pv_cache_bytes_kv(const pv_model *m, int32_t max_tokens, int32_t kv_bits, size_t *page_pool_bytes, size_t *workspace_bytes);
 int pv_cache_create_kv(const pv_model *m, void *d_page_pool, size_t page_pool_bytes, void *d_workspace, size_t workspace_bytes,
@@ -327,7 +328,8 @@ int pv_kv8_bytes(const pv_kv8_pool *pool, size_t *codes_bytes, size_t *scales_by
 
 /* Quantise keys and values as they are written: row i of sequence s becomes token prefix_len[s] + i of it.  The scale of a block is the smallest power of two (from
  * 2^-100 on) that leaves no code above 448; a block that holds earlier tokens (positions below prefix_len) keeps its scale, or, if a new token needs a larger one, has their codes
- * rounded to that.  Codes are rounded to nearest, ties to the even code; what is not finite becomes NaN and has no say in the scale.  k, v: element (row, head, feature) at
+ * rounded to that: numbers below 2^-6 of the new scale move, by 2^-10 of it at most (2^-17 of the block's largest number), others stay.  So what is stored of a token, and outputs that see it, depend
+ * to that extent on later tokens of its block, also on drafts and tree nodes that are rejected or that no row sees.  Codes are rounded to nearest, ties to the even code; what is not finite becomes NaN and has no say in the scale.  k, v: element (row, head, feature) at
  * row * row_stride + head * head_stride + feature, of type dtype (pv_dtype); addresses and strides multiples of 16 bytes.  A page must not be
  * the place of rows twice in a call, neither of two sequences nor under two entries of a table (what such a page holds then is not defined; nothing outside it is touched). */
 int pv_kv8_append(const pv_kv8_pool *pool, const pv_kv8_seqs *seqs, const void *k, int64_t k_row_stride, int64_t k_head_stride,
