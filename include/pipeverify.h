@@ -341,7 +341,7 @@ int pv_kv8_read(const pv_kv8_pool *pool, const pv_kv8_seqs *seqs, void *k, int64
 
 /* Attention of every row over the cache: out = softmax(scale * q K^T) V, query head a over kv head a / (n_q_heads / n_kv_heads).  The keys and values of the call's own rows are in the
  * cache already (pv_kv8_append with the same tables).  mask == NULL: row i of sequence s sees tokens 0 .. prefix_len[s] + i.  Else (a draft tree) mask[row] has bit t set
- * if the row sees token prefix_len[s] + t, and every row sees all tokens before prefix_len[s], none from prefix_len[s] + 64 on.  A row that sees no token: zeros, and -infinity in lse.  What a row does
+ * if the row sees token prefix_len[s] + t, t less than 64 and than the number of rows that s has in the call (other bits say nothing), and every row sees all tokens before prefix_len[s].  A row that sees no token: zeros, and -infinity in lse.  What a row does
  * not see has no influence on it, NaN included, but for the range of the sums: values whose scale is less than 2^-64 of the largest among the keys of the sequence and kv head up to the call's last row may
  * count as zeros, and the values a row sees times their number have to stay below 2^127.  q, out: PV_BF16 or PV_F16, addressed as above (out may be q); lse: NULL, or float [n_rows][n_q_heads],
  * log(sum(exp(scale * q K^T))).  n_q_heads is a multiple of n_kv_heads, (n_rows + n_seq) * n_q_heads <= 2^24,

@@ -163,7 +163,7 @@ class KV8Pool:
     def attention(self, seqs, q, scale=None, mask=None, out=None, return_lse=False, lse=None, stream=None):
         """softmax(scale q K^T) V of every row of q [rows, n_q_heads, head_dim] (bfloat16 or float16) over its sequence's tokens; scale: 1 / sqrt(head_dim) unless
         given.  Without a mask a row sees the tokens up to its own position.  mask: int64 or uint64 [rows], bit t: the row sees token prefix_len + t
-        (a draft tree: its ancestors and itself); all tokens before prefix_len are seen.  Returns out, or (out, lse) with lse float32 [rows, n_q_heads]."""
+        (a draft tree: its ancestors and itself), t less than 64 and than the sequence's rows in the call; all tokens before prefix_len are seen.  Returns out, or (out, lse) with lse float32 [rows, n_q_heads]."""
         where = "KV8Pool.attention"
         if _elsewhere(self._index, stream):
             with _Elsewhere(self.device, stream):
