@@ -151,7 +151,7 @@ void pv_cache_destroy(pv_cache *c);
 
 /* The same with keys and values in 8 bits (kv_bits = 8; 0: the model's storage type, which is what the two calls above give): half the memory and half of what a step reads of
  * them, e4m3 codes with a power-of-two scale for 16 tokens and head (the form is described at pv_kv8_pool below).  Keys and values are rounded to four significant bits when they are stored, and every row, also of
- * the block that brings them, attends to them as stored.  A block's later rows may change what is stored of earlier tokens of
+ * the block that brings them, attends to them as stored, with weights rounded to 11 significant bits (16 where keys and values are in the model's type).  A block's later rows may change what is stored of earlier tokens of
  * the same 16, whether they are accepted or not (pv_kv8_append says by how much).  bf16 models with head_dim 64 or 128.  All calls on a cache work alike; the caches of a batch store alike.
  * The page pool is the layers' codes ([n_layers] pools' codes), and behind them, rounded up to 256 bytes, their scales.  pv_cache_export gives the stored values (bf16, exact). */
 int pv_cache_bytes_kv(const pv_model *m, int32_t max_tokens, int32_t kv_bits, size_t *page_pool_bytes, size_t *workspace_bytes);
@@ -344,7 +344,7 @@ int pv_kv8_read(const pv_kv8_pool *pool, const pv_kv8_seqs *seqs, void *k, int64
  * if the row sees token prefix_len[s] + t, t less than 64 and than the number of rows that s has in the call (other bits say nothing), and every row sees all tokens before prefix_len[s].  A row that sees no token: zeros, and -infinity in lse.  What a row does
  * not see has no influence on it, NaN included, but for the range of the sums: values whose scale is less than 2^-64 of the largest among the keys of the sequence and kv head up to the call's last row may
  * count as zeros, and the values a row sees times their number have to stay below 2^127.  q, out: PV_BF16 or PV_F16, addressed as above (out may be q); lse: NULL, or float [n_rows][n_q_heads],
- * log(sum(exp(scale * q K^T))).  n_q_heads is a multiple of n_kv_heads, (n_rows + n_seq) * n_q_heads <= 2^24,
+ * log(sum(exp(scale * q K^T))).  Weights are rounded to 11 significant bits before they meet the values for PV_BF16, to 22 for PV_F16; all sums have 32 bits.  n_q_heads is a multiple of n_kv_heads, (n_rows + n_seq) * n_q_heads <= 2^24,
  * table_pages * page_tokens <= 2^30, scale is finite.  workspace: at least
  * pv_kv8_attention_bytes, 16-byte aligned, for this call alone until it has run. */
 int pv_kv8_attention_bytes(const pv_kv8_pool *pool, const pv_kv8_seqs *seqs, int32_t n_q_heads, size_t *bytes);
