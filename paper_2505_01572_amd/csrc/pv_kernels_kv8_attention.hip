@@ -344,7 +344,7 @@ __device__ inline void kv8_finish4(const kv8_attn_args &a, const kv8_row &w, int
 
 // Few rows: one workgroup is a kv head, a tile of 16 packed rows of a sequence, a chunk of its keys; the waves take 64 keys in turn, straight from memory to registers, and are joined
 // through LDS at the end.  Bound by the read of the codes: the next 64 keys' K is asked for when this one's scores are there, V when its products are.  32 sequences of up to 8192 keys, one row of 32
-// heads each: 45.5 us and 4.9 for the chunks' join, 266 MB at 5.8 TB/s (a read stream: 6.55); one sequence of four rows over 65536 keys 25.9 and 4.6, 133 MB at 5.1.
+// heads each: 44.7 us and 4.6 for the chunks' join, 266 MB at 5.9 TB/s (a read stream: 6.55); one sequence of four rows over 65000 keys 25.7 and 4.6, 133 MB at 5.2.
 template <int HD, int IO>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 k_kv8_attn(const kv8_attn_args a)
@@ -555,7 +555,7 @@ k_kv8_attn(const kv8_attn_args a)
 // Many rows: a workgroup is a kv head, 64 RT packed rows of a sequence (16 RT a wave), a chunk of its keys.  64 keys at a time go through LDS as 16-bit numbers: each wave asks for a
 // group of 16 two steps ahead and converts it one step ahead, once for all rows, while the products of this step run in the other wave of its SIMD.  Bound by a wave's instructions: of 64 keys 64 products
 // of 16 turns, and beside them some 340 vector and 150 scalar instructions (exponentials, maxima, the rounding of the weights, the codes' conversion) that overlap with the other wave's products only in part.  Two
-// prompts of 2048 rows on 6100 tokens, 32 heads of 128: 428 us, 783 TFLOP/s (a library's product of 8192^3: 1254).
+// prompts of 2048 rows on 6100 tokens, 32 heads of 128: 419 us, 800 TFLOP/s (a library's product of 8192^3: 1254).
 template <int HD, int RT>
 struct kv8_wide {
     static constexpr int KS = HD / 32, ET = HD / 16;
