@@ -362,6 +362,77 @@ int pv_token_logprobs_bytes(int64_t rows, int32_t vocab, int32_t top, size_t *by
 int pv_token_logprobs(const void *logits, int64_t row_stride, int32_t dtype, int64_t rows, int32_t vocab, const int32_t *tokens, int32_t n_tokens, float *logprobs,
                       float *entropy, float *lse, int32_t top, int32_t *top_ids, float *top_logprobs, void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* ---- operators around a key/value cache in 16 bits, and drafts verified by sampling ----
+ *
+ * What a program with a decoder of its own needs for a step of speculative decoding beside the 8-bit cache: rotary positions, a cache in bf16 or f16 that is written with the keys rotated on the way, attention over it for
+ * decoded tokens, prompts and draft trees of any number of nodes, the acceptance of drafts by the target's probabilities, and the accepted path of a tree made the sequence's end.  All pointers are device memory; nothing is
+ * allocated, synchronised or kept, so the calls may be captured into graphs. */
+
+/* Rotary positions.  A pair of features (a, b) of a row at position p becomes amplitude * (a cos - b sin, a sin + b cos) of the angle p * turns[i] full circles; turns: device double [rotary_dim / 2], 8-byte aligned (base^(-2i /
+ * rotary_dim) / 2 pi, scaled as the model wants it).  Pair i of a head is its features (i, i + rotary_dim / 2), or, interleaved, (2i, 2i + 1); features from rotary_dim on stay as they are.  rotary_dim is a multiple
+ * of 16.  Angles are made in 64 bits, the rest in 32, rounded once. */
+typedef struct {
+    const double *turns;
+    int32_t rotary_dim, interleaved;
+    float amplitude;
+} pv_rotary;
+
+/* Rows of heads, element (row, head, feature) at row * row_stride + head * head_stride + feature of type dtype, addresses and strides multiples of 16 bytes, turned by positions [n_rows] (int32, any sign).  out may be x; it must
+ * not overlap it otherwise.  head_dim: a multiple of 16 up to 1024; n_rows <= 2^24. */
+int pv_rotate(const pv_rotary *rotary, const int32_t *positions, const void *x, int64_t x_row_stride, int64_t x_head_stride, void *out, int64_t out_row_stride, int64_t out_head_stride,
+              int32_t n_rows, int32_t n_heads, int32_t head_dim, int32_t dtype, void *hip_stream);
+
+/* The cache: keys and values in bf16 or f16 (dtype),
+ *   pages  [n_pages][n_kv_heads][2 (K, V)][page_tokens / 16][16 * head_dim], 16-byte aligned; inside a block of 16 tokens
+ *          K [head_dim / 8][token][8 features],  V [head_dim / 32][token / 4][feature % 16][feature / 16 % 2][token % 4]
+ * head_dim is 64 or 128, page_tokens a power of two from 16 to 65536, a page less than 2^32 bytes.  It does not have to be cleared before use. */
+typedef struct {
+    void *pages;
+    int32_t n_pages, n_kv_heads, head_dim, page_tokens, dtype;
+} pv_kv16_pool;
+
+/* Bytes of a pool's pages. */
+int pv_kv16_bytes(const pv_kv16_pool *pool, size_t *bytes);
+
+/* Write keys and values: row i of sequence s (pv_kv8_seqs, whose rules for rows of no sequence and pages that do not exist hold here as well) becomes token prefix_len[s] + i of it, rounded to the pool's type.  With a rotary (else NULL),
+ * keys are rotated on the way by positions [n_rows] (int32; NULL: the tokens' own), and, where q is not NULL, the queries of the same rows, into q_out (which may be q; rows of no sequence are left as they are).  k, v, q, q_out:
+ * addressed as in pv_rotate, of type dtype (pv_dtype).  A page must not be the place of rows twice in a call.  n_rows <= 2^20 - 16. */
+int pv_kv16_append(const pv_kv16_pool *pool, const pv_kv8_seqs *seqs, const void *k, int64_t k_row_stride, int64_t k_head_stride, const void *v, int64_t v_row_stride, int64_t v_head_stride,
+                   const pv_rotary *rotary, const int32_t *positions, const void *q, int64_t q_row_stride, int64_t q_head_stride, int32_t n_q_heads,
+                   void *q_out, int64_t q_out_row_stride, int64_t q_out_head_stride, int32_t dtype, void *hip_stream);
+
+/* Attention of every row over the cache, as pv_kv8_attention, with q and out of the pool's type: out = softmax(scale * q K^T) V, query head a over kv head a / (n_q_heads / n_kv_heads).  mask == NULL: row i of sequence s sees
+ * tokens 0 .. prefix_len[s] + i.  Else (a draft tree) mask [n_rows][mask_words]: the row sees all tokens before prefix_len[s], and token prefix_len[s] + t if bit t % 64 of its word t / 64 is set, t less than 64 * mask_words and than the
+ * number of rows that s has in the call.  A row that sees no token: zeros, and -infinity in lse (NULL, or float [n_rows][n_q_heads]).  What a row does not see has no influence on it, NaN and infinities included; a
+ * value that it sees and that is infinite or NaN makes its output infinite or NaN.  Weights meet the values as pairs of numbers of the pool's type (16 significant bits in bf16, 22 in f16); all sums have 32 bits.
+ * n_q_heads is a multiple of n_kv_heads, (n_rows + n_seq) * n_q_heads <= 2^24, table_pages * page_tokens <= 2^30, mask_words <= 2^18, scale is finite.  workspace: at least pv_kv16_attention_bytes,
+ * 16-byte aligned, for this call alone until it has run. */
+int pv_kv16_attention_bytes(const pv_kv16_pool *pool, const pv_kv8_seqs *seqs, int32_t n_q_heads, size_t *bytes);
+int pv_kv16_attention(const pv_kv16_pool *pool, const pv_kv8_seqs *seqs, const void *q, int64_t q_row_stride, int64_t q_head_stride, int32_t n_q_heads,
+                      const uint64_t *mask, int32_t mask_words, float scale, void *out, int64_t out_row_stride, int64_t out_head_stride, float *lse,
+                      void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* After a tree: token prefix_len[s] + path[row_start[s] + d] becomes token prefix_len[s] + d, for d = 0 .. accepted[s] (as pv_verify_drafts leaves both: the root and the accepted nodes; the prefix is then accepted[s] + 1 longer).
+ * path: int32 [n_rows], rising numbers of the sequence's rows (one that is less than its place, or no row of the sequence, moves nothing); accepted: int32 [n_seq].  n_seq <= 65535. */
+int pv_kv16_keep(const pv_kv16_pool *pool, const pv_kv8_seqs *seqs, const int32_t *path, const int32_t *accepted, void *hip_stream);
+
+/* Verify drafts by sampling.  Sequence s has rows row_start[s] .. row_start[s + 1] - 1 (int32 [n_seq + 1], rising) of `rows`: its first row's token is settled, each further row carries a draft, tokens [rows] (int32).  logits: row r
+ * at r * row_stride elements of type dtype, vocab of them, any alignment of rows: what the target says of the token behind row r, p_r = softmax(logits / T), T = temperatures[s] (float [n_seq]; NULL: temperature for all).
+ * T = 0 (and, on the device, one that is negative or NaN): the most probable token alone, of equal ones the lowest id.  u: [rows][2], float or double, from [0, 1).
+ *   parent == NULL, a chain: the draft x of row c is taken if u[c][0] * q(x) < p_{c-1}(x), and all before it are; q = draft_probs row c (float, at c * draft_row_stride), what x was drawn from, or, NULL, 1 at x (a
+ *     draft that was not drawn).  *next_token = a draw from max(p_{c-1} - q, 0) where the draft of row c was the first that was not taken (from p_{c-1}, should rounding leave nothing of that), from p of the last row where all were.
+ *   parent [rows] (int32), a tree: the row hangs under row parent[row] of its sequence, a lower number than its own (others are no nodes).  From the first row on, the children of the node reached are tried in order, a child with u[row][0]: taken if
+ *     u * (1 - the sum of p of the children refused before it) < p(its token); a token that an earlier child had is refused.  *next_token = a draw from p of the last node reached without its children's tokens.
+ *   A draw behind row r: the lowest id at which the sum of the (remaining) probabilities in the order of ids passes u[r][1] times their whole sum.
+ * So tokens are distributed as the target alone would have them, whatever the drafts.  accepted [n_seq]: drafts taken; next_token [n_seq]; path [rows] (NULL where there is no tree): row_start[s] + d = the number in its sequence of the d-th row reached, from
+ * the first row (0) on, -1 behind the last and in rows of no sequence; probs [rows]: p of each row's draft (1 in a sequence's first row, 0 in rows of no sequence).  A sequence without rows: 0 and -1.  All of it in 64 bits.
+ * A logit of -infinity or NaN has probability 0; a row with +infinity, or of nothing else, has no probabilities: no draft is taken behind it, and a draw there is -1 (as where no token has any left).  A token outside [0, vocab) is never taken.
+ * vocab <= 2^21, rows and n_seq <= 2^20, each times ceil(vocab / 4096) < 2^24; workspace: at least pv_verify_drafts_bytes, 16-byte aligned, for this call alone until it has run. */
+int pv_verify_drafts_bytes(int64_t rows, int32_t n_seq, int32_t vocab, size_t *bytes);
+int pv_verify_drafts(const int32_t *row_start, int32_t n_seq, const void *logits, int64_t row_stride, int32_t dtype, int64_t rows, int32_t vocab, const int32_t *tokens,
+                     const void *u, int32_t u_is_double, const float *draft_probs, int64_t draft_row_stride, const int32_t *parent, const float *temperatures, float temperature,
+                     int32_t *accepted, int32_t *next_token, int32_t *path, float *probs, void *workspace, size_t workspace_bytes, void *hip_stream);
+
 /* ---- instrumentation ---- */
 
 typedef enum {

@@ -18,6 +18,7 @@ _GLOBAL = ("embed", "final_norm", "lm_head")
 
 
 TokenLogprobs = collections.namedtuple("TokenLogprobs", "logprobs entropy lse top_ids top_logprobs")
+DraftVerdict = collections.namedtuple("DraftVerdict", "accepted next_token path probs")
 
 
 class PVError(RuntimeError):
@@ -43,6 +44,14 @@ class pv_kv8_seqs(ctypes.Structure):
                [(n, ctypes.c_int32) for n in ("n_seq", "n_rows", "table_pages")]
 
 
+class pv_rotary(ctypes.Structure):
+    _fields_ = [("turns", ctypes.c_void_p), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("amplitude", ctypes.c_float)]
+
+
+class pv_kv16_pool(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p)] + [(n, ctypes.c_int32) for n in ("n_pages", "n_kv_heads", "head_dim", "page_tokens", "dtype")]
+
+
 EXPORTS = [
     "pv_model_bytes", "pv_prompt_bytes", "pv_cache_bytes", "pv_model_create", "pv_model_destroy", "pv_load_weights",
     "pv_cache_create", "pv_cache_destroy", "pv_cache_set_page_table", "pv_prefill", "pv_verify",
@@ -51,6 +60,7 @@ EXPORTS = [
     "pv_profile_select", "pv_profile_read", "pv_cache_readmit", "pv_calib_copy", "pv_calib_read", "pv_verify_async_static", "pv_verify_batch", "pv_verify_tree", "pv_cache_use_graphs", "pv_load_weights_q4",
     "pv_kv8_bytes", "pv_kv8_append", "pv_kv8_read", "pv_kv8_attention_bytes", "pv_kv8_attention", "pv_token_logprobs_bytes", "pv_token_logprobs",
     "pv_cache_bytes_kv", "pv_cache_create_kv", "pv_cache_logprobs",
+    "pv_rotate", "pv_kv16_bytes", "pv_kv16_append", "pv_kv16_attention_bytes", "pv_kv16_attention", "pv_kv16_keep", "pv_verify_drafts_bytes", "pv_verify_drafts",
 ]
 
 _lib = None
@@ -108,6 +118,15 @@ def lib():
         L.pv_cache_bytes_kv.argtypes = [vp, i32, i32, P(sz), P(sz)]
         L.pv_cache_create_kv.argtypes = [vp, vp, sz, vp, sz, i32, i32, P(vp)]
         L.pv_cache_logprobs.argtypes = [vp, vp, i32, vp, vp, vp, i32, vp, vp, P(i32), vp]
+        rotp, pool16p = P(pv_rotary), P(pv_kv16_pool)
+        L.pv_rotate.argtypes = [rotp, vp, *rows, *rows, i32, i32, i32, i32, vp]
+        L.pv_kv16_bytes.argtypes = [pool16p, P(sz)]
+        L.pv_kv16_append.argtypes = [pool16p, seqsp, *rows, *rows, rotp, vp, *rows, i32, *rows, i32, vp]
+        L.pv_kv16_attention_bytes.argtypes = [pool16p, seqsp, i32, P(sz)]
+        L.pv_kv16_attention.argtypes = [pool16p, seqsp, *rows, i32, vp, i32, ctypes.c_float, *rows, vp, vp, sz, vp]
+        L.pv_kv16_keep.argtypes = [pool16p, seqsp, vp, vp, vp]
+        L.pv_verify_drafts_bytes.argtypes = [i64, i32, i32, P(sz)]
+        L.pv_verify_drafts.argtypes = [vp, i32, vp, i64, i32, i64, i32, vp, vp, i32, vp, i64, vp, vp, ctypes.c_float, vp, vp, vp, vp, vp, sz, vp]
         L.pv_strerror.argtypes = [ctypes.c_int]; L.pv_strerror.restype = ctypes.c_char_p
         L.pv_last_error.argtypes = []; L.pv_last_error.restype = ctypes.c_char_p
         _lib = L

@@ -8,7 +8,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpipeverify.so")
 SOURCES = ["pv_api.hip", "pv_kernels_common.hip", "pv_kernels_vector.hip", "pv_kernels_matrix.hip", "pv_kernels_attention.hip", "pv_kernels_prefill.hip",
-           "pv_kernels_kv8.hip", "pv_kernels_kv8_attention.hip", "pv_kernels_logprobs.hip"]
+           "pv_kernels_kv8.hip", "pv_kernels_kv8_attention.hip", "pv_kernels_logprobs.hip",
+           "pv_kernels_kv16.hip", "pv_kernels_kv16_attention.hip", "pv_kernels_drafts.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
