@@ -10,7 +10,7 @@
 // refused draft has a drafter's probabilities, every segment of that row is summed anew first, under max(p - q, 0).
 #include "pv_matrix_common.h"
 
-struct dv_part { double sum; float top; int first; };       // of a segment: sum of e^((x - top) / T), largest logit, its lowest id (T = 0: no sum)
+struct __align__(16) dv_part { double sum; float top; int first; };       // of a segment: sum of e^((x - top) / T), largest logit, its lowest id (T = 0: no sum)
 
 struct dv_args {
     const char *logits; int64_t row_bytes;
@@ -35,11 +35,11 @@ __device__ inline dv_seq dv_seq_at(const dv_args &a, int s)
     if (q.row0 < 0 || q.rows < 0) q.rows = 0;
     return q;
 }
-// 1 / T (of infinity: next to nothing); 0: the most probable token alone
+// log2(e) / T (of an infinite T: next to nothing); 0: the most probable token alone
 __device__ inline double dv_cold(const dv_args &a, int s)
 {
     const float t = a.temperature != nullptr ? a.temperature[s] : a.hot;
-    return t > 0.f ? fmax(1.0 / (double)t, 1e-300) : 0.0;
+    return t > 0.f ? fmax(1.4426950408889634074 / (double)t, 1e-300) : 0.0;
 }
 __device__ inline double dv_u(const dv_args &a, int row, int which)
 {
@@ -47,16 +47,18 @@ __device__ inline double dv_u(const dv_args &a, int row, int which)
     return a.u64 ? ((const double *)a.u)[i] : (double)((const float *)a.u)[i];
 }
 
-// e^y, y <= 0 or NaN: 2^n times the series of e^z, |z| <= ln(2) / 2, up to z^11 (what is left out is below 10^-14)
-__device__ inline double dv_exp(double y)
+// 2^((x - top) cold), for a result of at most 1: a whole power of two, put into the exponent, times 2^r, |r| <= 1/2, by the polynomial of degree 8 that meets it at the nine Chebyshev points (off by 1.1 10^-12 of it at most; a sum
+// of rounded probabilities turns on 10^-11 of them, so a ninth degree would buy nothing).  What is below 2^-1000, -infinity and NaN: 2^-1000.
+__device__ inline double dv_power(float x, double cold, double top)
 {
-    const double t = fmax(y * 1.4426950408889634074, -1100.0), n = rint(t), z = (t - n) * 0.69314718055994530942;
-    double e = 1.0 / 39916800.0;
-    e = fma(e, z, 1.0 / 3628800.0); e = fma(e, z, 1.0 / 362880.0); e = fma(e, z, 1.0 / 40320.0); e = fma(e, z, 1.0 / 5040.0); e = fma(e, z, 1.0 / 720.0);
-    e = fma(e, z, 1.0 / 120.0); e = fma(e, z, 1.0 / 24.0); e = fma(e, z, 1.0 / 6.0); e = fma(e, z, 0.5); e = fma(e, z, 1.0); e = fma(e, z, 1.0);
-    return ldexp(e, (int)n);
+    const double t = fmax(((double)x - top) * cold, -1000.0), m = t + 6755399441055744.0, r = t - (m - 6755399441055744.0);      // (1.5 2^52: what is added to it is rounded to a whole number, in its low bits)
+    double e = 1.3255224878668817e-06;
+    e = fma(e, r, 1.5310079402249296e-05); e = fma(e, r, 0.00015403455852453838); e = fma(e, r, 0.0013333450568000645); e = fma(e, r, 0.009618129159402558);
+    e = fma(e, r, 0.05550410941205933); e = fma(e, r, 0.2402265069581299); e = fma(e, r, 0.6931471805459335); e = fma(e, r, 1.0);
+    const uint64_t b = __double_as_longlong(e);
+    return __longlong_as_double((int64_t)((uint64_t)((uint32_t)(b >> 32) + ((uint32_t)__double_as_longlong(m) << 20)) << 32 | (uint32_t)b));
 }
-__device__ inline double dv_weight(float x, float top, double cold) { return x > -INFINITY ? dv_exp(((double)x - (double)top) * cold) : 0.0; }      // (NaN: 0)
+__device__ inline double dv_weight(float x, double cold, double top) { return x > -INFINITY ? dv_power(x, cold, top) : 0.0; }      // (NaN: 0)
 
 template <typename T> __device__ inline float dv_one(const char *p, int64_t i);
 template <> __device__ inline float dv_one<float>(const char *p, int64_t i) { return ((const float *)p)[i]; }
@@ -69,15 +71,64 @@ template <> __device__ inline float dv_get<float>(const uint32_t *w, int i) { re
 template <> __device__ inline float dv_get<__bf16>(const uint32_t *w, int i) { return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16); }
 template <> __device__ inline float dv_get<_Float16>(const uint32_t *w, int i) { const dv_h2 h = __builtin_bit_cast(dv_h2, w[i >> 1]); return (float)(i & 1 ? h.y : h.x); }
 
-// 16 bytes from an address that is a multiple of 4
+// 16 bytes (8) from an address that is a multiple of 4
+typedef __attribute__((ext_vector_type(2), aligned(4))) unsigned int dv_u32x2;
 typedef __attribute__((ext_vector_type(4), aligned(4))) unsigned int dv_u32x4;
 __device__ inline u32x4 dv_load16(const char *p) { const dv_u32x4 v = *(const dv_u32x4 *)p; return (u32x4){v.x, v.y, v.z, v.w}; }
+__device__ inline u32x4 dv_load16_once(const char *p) { const dv_u32x4 v = __builtin_nontemporal_load((const dv_u32x4 *)p); return (u32x4){v.x, v.y, v.z, v.w}; }
+template <typename T> __device__ constexpr uint32_t dv_none() { return sizeof(T) == 4 ? 0xff800000u : __is_same(T, __bf16) ? 0xff80ff80u : 0xfc00fc00u; }      // -infinity
 
+// N tokens' logits and, where there are any, the drafter's probabilities from token i on; behind `end`: -infinity and 0
+template <typename T, int N> __device__ inline void dv_tokens(const char *src, const float *drafter, int i, int end, float (&x)[N], float (&d)[N])
+{
+    constexpr int W = N * (int)sizeof(T) / 4;
+    static_assert(N % 4 == 0 && (W == 2 || W % 4 == 0), "");
+    const bool whole = i + N <= end;
+    uint32_t w[W];
+#pragma unroll
+    for (int k = 0; k < W; ++k) w[k] = dv_none<T>();
+#pragma unroll
+    for (int k = 0; k < N; ++k) d[k] = 0.f;
+    const char *at = src + (int64_t)i * sizeof(T);
+    if (whole) {
+        if constexpr (W == 2) { const dv_u32x2 v = *(const dv_u32x2 *)at; w[0] = v.x; w[1] = v.y; }
+        else {
+#pragma unroll
+            for (int k = 0; k < W / 4; ++k) { const u32x4 v = dv_load16(at + 16 * k); w[4 * k] = v.x; w[4 * k + 1] = v.y; w[4 * k + 2] = v.z; w[4 * k + 3] = v.w; }
+        }
+    }
+    if (whole && drafter != nullptr) {
+#pragma unroll
+        for (int k = 0; k < N / 4; ++k) {
+            const u32x4 v = dv_load16((const char *)(drafter + i + 4 * k));
+            d[4 * k] = __uint_as_float(v.x); d[4 * k + 1] = __uint_as_float(v.y); d[4 * k + 2] = __uint_as_float(v.z); d[4 * k + 3] = __uint_as_float(v.w);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[k] = dv_get<T>(w, k);
+    if (!whole && i < end) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) if (i + k < end) { x[k] = dv_one<T>(src, i + k); if (drafter != nullptr) d[k] = drafter[i + k]; }
+    }
+}
+
+// Sums over lanes N apart within 16 lanes by rotations, over the others by exchanges: vector instructions
+template <int N> __device__ inline double dv_rotated(double v)
+{
+    const uint64_t b = __double_as_longlong(v);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0u, (uint32_t)b, 0x120 + N, 0xF, 0xF, true), hi = __builtin_amdgcn_update_dpp(0u, (uint32_t)(b >> 32), 0x120 + N, 0xF, 0xF, true);
+    return v + __longlong_as_double((int64_t)((uint64_t)hi << 32 | lo));
+}
+__device__ inline double dv_over_16(double v) { return dv_rotated<8>(dv_rotated<4>(dv_rotated<2>(dv_rotated<1>(v)))); }
 __device__ inline double dv_over_wave(double v)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d, 64);
-    return v;
+    v = dv_over_16(v);
+    uint64_t b = __double_as_longlong(v);
+    auto l = __builtin_amdgcn_permlane16_swap((uint32_t)b, (uint32_t)b, false, false), h = __builtin_amdgcn_permlane16_swap((uint32_t)(b >> 32), (uint32_t)(b >> 32), false, false);
+    v = __longlong_as_double((int64_t)((uint64_t)h[0] << 32 | l[0])) + __longlong_as_double((int64_t)((uint64_t)h[1] << 32 | l[1]));
+    b = __double_as_longlong(v);
+    l = __builtin_amdgcn_permlane32_swap((uint32_t)b, (uint32_t)b, false, false); h = __builtin_amdgcn_permlane32_swap((uint32_t)(b >> 32), (uint32_t)(b >> 32), false, false);
+    return __longlong_as_double((int64_t)((uint64_t)h[0] << 32 | l[0])) + __longlong_as_double((int64_t)((uint64_t)h[1] << 32 | l[1]));
 }
 __device__ inline int dv_min_over_wave(int v)
 {
@@ -85,11 +136,20 @@ __device__ inline int dv_min_over_wave(int v)
     for (int d = 1; d < 64; d <<= 1) v = min(v, __shfl_xor(v, d, 64));
     return v;
 }
+// ... up to and with the own lane
+__device__ inline double dv_up_to(double v)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) { const double o = __shfl_up(v, d, 64); if (lane >= d) v += o; }
+    return v;
+}
 
-// Segment seg of a row: tokens begin(seg) .. begin(seg + 1) - 1.  Its 16 bytes of a thread begin at a multiple of four bytes: a row of 16-bit numbers that does not has one token more in its first segment.
+// Segment seg of a row: tokens begin(seg) .. begin(seg + 1) - 1.  16 bytes of a thread begin at a multiple of four: a row of 16-bit numbers that does not has one token more in its first segment.
 template <typename T> __device__ inline int dv_head(const char *src) { return sizeof(T) == 2 && ((uintptr_t)src & 2) ? 1 : 0; }
 __device__ inline int dv_begin(int seg, int head, int size) { return seg == 0 ? 0 : head + seg * size; }
 
+// The rows' sums.  Bound by the exponentials: some 17 instruction slots a logit, most of them in 64 bits.
 template <typename T, int E>
 __global__ void __launch_bounds__(256)
 k_draft_rows(const dv_args a)
@@ -106,9 +166,8 @@ k_draft_rows(const dv_args a)
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int i0 = base + (u * NT + tid) * V;
-        constexpr uint32_t inf = sizeof(T) == 4 ? 0xff800000u : __is_same(T, __bf16) ? 0xff80ff80u : 0xfc00fc00u;      // -infinity
-        u32x4 v = {inf, inf, inf, inf};
-        if (i0 + V <= a.vocab) v = dv_load16(src + (int64_t)i0 * sizeof(T));
+        u32x4 v = {dv_none<T>(), dv_none<T>(), dv_none<T>(), dv_none<T>()};
+        if (i0 + V <= a.vocab) v = dv_load16_once(src + (int64_t)i0 * sizeof(T));
         x[4 * u] = v.x; x[4 * u + 1] = v.y; x[4 * u + 2] = v.z; x[4 * u + 3] = v.w;
     }
     // those that no 16 bytes hold: ahead of the first, behind the last
@@ -136,10 +195,14 @@ k_draft_rows(const dv_args a)
     double sum = 0.0;
     int first = 0x7fffffff;
     if (cold > 0.0) {
-        sum = dv_weight(x0, top, cold);
+        const double most = top;
+        double odd = 0.0;
 #pragma unroll
-        for (int i = 0; i < E; ++i) sum += dv_weight(dv_get<T>(x, i), top, cold);
-        sum = dv_over_wave(sum);
+        for (int d = 0; d < D; ++d) if (sizeof(T) == 2) asm volatile("" : "+v"(x[d]));     // (taken apart anew: 32 bits of each number would be twice the registers)
+#pragma unroll
+        for (int i = 0; i < E; ++i) { const double w = dv_power(dv_get<T>(x, i), cold, most); if (i & 1) odd += w; else sum += w; }
+        sum = dv_over_wave((sum + odd) + dv_power(x0, cold, most));
+        if (top == -INFINITY) sum = 0.0;
     } else {
         if (alone >= 0 && x0 == top) first = alone;
 #pragma unroll
@@ -157,106 +220,138 @@ k_draft_rows(const dv_args a)
     }
 }
 
-// A row's segments joined, by each GL lanes side by side: largest logit, sum of exponentials, the lowest id of the largest
-struct dv_row { float top; double sum; int first; bool any; };      // any: it has probabilities (its largest logit is a number)
+// A row's segments joined, by each GL lanes side by side: largest logit, sum of exponentials, the lowest id of the largest.  Four segments a lane stay in registers between the two passes.
+struct dv_row { double sum; float top; int first; bool any; };      // any: it has probabilities (its largest logit is a number)
 template <int GL> __device__ inline dv_row dv_row_of(const dv_args &a, int row, double cold)
 {
+    constexpr int K = 4;
     const int l = threadIdx.x % GL;
     const dv_part *p = a.part + (int64_t)row * a.segs;
-    dv_row r = {-INFINITY, 0.0, 0x7fffffff, false};
-    for (int i = l; i < a.segs; i += GL) r.top = fmaxf(r.top, p[i].top);
+    dv_part q[K];
+    dv_row r = {0.0, -INFINITY, 0x7fffffff, false};
 #pragma unroll
-    for (int d = 1; d < GL; d <<= 1) r.top = fmaxf(r.top, __shfl_xor(r.top, d, 64));
+    for (int k = 0; k < K; ++k) { q[k] = {0.0, -INFINITY, 0x7fffffff}; if (l + k * GL < a.segs) q[k] = p[l + k * GL]; }
+#pragma unroll
+    for (int k = 0; k < K; ++k) r.top = fmaxf(r.top, q[k].top);
+    for (int i = l + K * GL; i < a.segs; i += GL) r.top = fmaxf(r.top, p[i].top);
+    r.top = with_rotated<8>(with_rotated<4>(with_rotated<2>(with_rotated<1>(r.top, op_max), op_max), op_max), op_max);
+    if (GL == 64) r.top = with_lane32(with_lane16(r.top, op_max), op_max);
     r.any = r.top > -INFINITY && r.top < INFINITY;
-    for (int i = l; i < a.segs; i += GL) {
-        const dv_part q = p[i];
-        if (cold > 0.0) r.sum += q.sum * dv_weight(q.top, r.top, cold);
-        else if (q.top == r.top) r.first = min(r.first, q.first);
-    }
+    auto add = [&](const dv_part &v) {
+        if (cold > 0.0) r.sum += v.sum * dv_weight(v.top, cold, r.top);
+        else if (v.top == r.top) r.first = min(r.first, v.first);
+    };
 #pragma unroll
-    for (int d = 1; d < GL; d <<= 1) { r.sum += __shfl_xor(r.sum, d, 64); r.first = min(r.first, __shfl_xor(r.first, d, 64)); }
+    for (int k = 0; k < K; ++k) if (k * GL < a.segs) add(q[k]);
+    for (int i = l + K * GL; i < a.segs; i += GL) add(p[i]);
+    if (cold > 0.0) r.sum = GL == 64 ? dv_over_wave(r.sum) : dv_over_16(r.sum);
+    else {
+#pragma unroll
+        for (int d = 1; d < GL; d <<= 1) r.first = min(r.first, __shfl_xor(r.first, d, 64));
+    }
     return r;
 }
-template <typename T> __device__ inline double dv_prob(const dv_args &a, const dv_row &r, int row, int token, double cold)
+// p of a token, from its logit
+__device__ inline double dv_prob(const dv_args &a, const dv_row &r, float x, int token, double cold)
 {
     if (!r.any || token < 0 || token >= a.vocab) return 0.0;
     if (cold == 0.0) return token == r.first ? 1.0 : 0.0;
-    return dv_weight(dv_one<T>(a.logits + (int64_t)row * a.row_bytes, token), r.top, cold) / r.sum;
+    return dv_weight(x, cold, r.top) / r.sum;
 }
 
-// A chain: which drafts are taken, all looked at side by side, 16 lanes each.  The row behind which the draw is, and whether a draft was refused there.
-template <typename T> __device__ inline int2 dv_chain(const dv_args &a, const dv_seq &q, double cold, bool write, int *sh_refused)
+// A chain: which drafts are taken, all looked at side by side, 16 lanes each.  The row behind which the draw is, and whether a draft was refused there; that row's sums in *sh_row where one was.  all: go on behind the first
+// refused one, for every draft's p, and write it.
+struct dv_chain_lds { dv_row row; int refused; };
+template <typename T> __device__ inline int2 dv_chain(const dv_args &a, const dv_seq &q, double cold, bool all, dv_chain_lds *sh)
 {
     constexpr int GL = 16;
-    if (threadIdx.x == 0) *sh_refused = q.rows;
+    if (threadIdx.x == 0) sh->refused = q.rows;
     __syncthreads();
     const int n = blockDim.x / GL;
     for (int j0 = 1; j0 < q.rows; j0 += n) {             // (uniform: lanes without a draft look at the last one)
-        const int j = min(j0 + (int)threadIdx.x / GL, q.rows - 1), row = q.row0 + j, token = a.tokens[row];
+        const int j = min(j0 + (int)threadIdx.x / GL, q.rows - 1), row = q.row0 + j, token = a.tokens[row], safe = min(max(token, 0), a.vocab - 1);
+        const float x = dv_one<T>(a.logits + (int64_t)(row - 1) * a.row_bytes, safe);
+        const double u = dv_u(a, row, 0), d = a.probs == nullptr ? 1.0 : safe == token ? (double)a.probs[(int64_t)row * a.probs_row + safe] : 0.0;
         const dv_row r = dv_row_of<GL>(a, row - 1, cold);
-        const double p = dv_prob<T>(a, r, row - 1, token, cold);
-        const double d = a.probs == nullptr ? 1.0 : token >= 0 && token < a.vocab ? (double)a.probs[(int64_t)row * a.probs_row + token] : 0.0;
+        const double p = dv_prob(a, r, x, token, cold);
         if (threadIdx.x % GL == 0) {
-            if (!(dv_u(a, row, 0) * d < p)) atomicMin(sh_refused, j);
-            if (write) a.out_probs[row] = (float)p;
+            if (!(u * d < p)) atomicMin(&sh->refused, j);
+            if (all) a.out_probs[row] = (float)p;
         }
+        const int before = j0;
+        __syncthreads();
+        const int refused = sh->refused;
+        if (refused >= before && refused < min(before + n, q.rows) && refused == j && threadIdx.x % GL == 0) sh->row = r;
+        __syncthreads();
+        if (!all && refused < q.rows) break;
     }
-    __syncthreads();
-    const int refused = *sh_refused;
+    const int refused = sh->refused;
     return make_int2(q.row0 + min(refused, q.rows) - 1, refused < q.rows);
 }
 
-// max(p - q, 0) of a segment's tokens, summed, where a draft with a drafter's probabilities was refused
+// max(p - q, 0) of a segment's tokens, summed, where a draft with a drafter's probabilities was refused.  The walk along the chain is made anew by every workgroup: it is three trips to memory, a launch for it costs more.
 template <typename T, int E>
 __global__ void __launch_bounds__(256)
 k_draft_rest(const dv_args a)
 {
-    constexpr int NT = 256, SIZE = NT * E;
-    __shared__ int sh_refused;
+    constexpr int NT = 256, SIZE = NT * E, N = 8;
+    __shared__ dv_chain_lds sh_chain;
     __shared__ double sh_sum[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int s = blockIdx.x / a.segs, seg = blockIdx.x - s * a.segs;
     const dv_seq q = dv_seq_at(a, s);
     if (q.rows == 0) return;
     const double cold = dv_cold(a, s);
-    const int2 w = dv_chain<T>(a, q, cold, seg == 0, &sh_refused);
+    const int2 w = dv_chain<T>(a, q, cold, seg == 0, &sh_chain);
     if (seg == 0 && tid == 0) a.walk[s] = w;
     if (!w.y || cold == 0.0) return;
-    const dv_row r = dv_row_of<64>(a, w.x, cold);
+    const dv_row r = sh_chain.row;
     const char *src = a.logits + (int64_t)w.x * a.row_bytes;
     const float *drafter = a.probs + (int64_t)(w.x + 1) * a.probs_row;
-    const int head = dv_head<T>(src), begin = dv_begin(seg, head, SIZE), end = min(dv_begin(seg + 1, head, SIZE), a.vocab);
+    const int head = dv_head<T>(src), begin = head + seg * SIZE, end = min(begin + SIZE, a.vocab);
     const double inv = 1.0 / r.sum;
     double sum = 0.0;
-    for (int i = begin + tid; i < end; i += NT) sum += fmax(dv_weight(dv_one<T>(src, i), r.top, cold) * inv - (double)drafter[i], 0.0);
+    if (head && seg == 0 && tid == 0) sum = fmax(dv_weight(dv_one<T>(src, 0), cold, r.top) * inv - (double)drafter[0], 0.0);
+    float x[E / N][N], d[E / N][N];
+#pragma unroll
+    for (int k = 0; k < E / N; ++k) dv_tokens<T, N>(src, drafter, begin + (k * NT + tid) * N, end, x[k], d[k]);
+#pragma unroll
+    for (int k = 0; k < E / N; ++k)
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum += fmax(dv_weight(x[k][i], cold, r.top) * inv - (double)d[k][i], 0.0);
     sum = dv_over_wave(sum);
     if (lane == 0) sh_sum[wave] = sum;
     __syncthreads();
     if (tid == 0) a.rest[(int64_t)s * a.segs + seg] = (sh_sum[0] + sh_sum[1]) + (sh_sum[2] + sh_sum[3]);
 }
 
-// The draw of a sequence, and before it the walk along its tree.
+// The draw of a sequence, and before it the walk along its tree.  Some five trips to memory, one behind the other.
 #define DV_NODES 1024                       // nodes at a time
 #define DV_MAX_SEGS 512
-template <typename T, int E>
-__global__ void __launch_bounds__(512)
+template <typename T, int E, int NT>
+__global__ void __launch_bounds__(NT)
 k_draft_pick(const dv_args a)
 {
-    constexpr int NT = 512, NW = NT / 64, SIZE = 256 * E, GL = 16;
-    __shared__ double sh_p[DV_NODES], sh_seg[DV_MAX_SEGS], sh_wave[NW];
-    __shared__ int sh_parent[DV_NODES], sh_token[DV_NODES], sh_refused, sh_pick, sh_id;
+    constexpr int NW = NT / 64, SIZE = 256 * E, N = SIZE / NT, GL = 16, SC = DV_MAX_SEGS / 64;
+    constexpr bool TREE = NT == 1024;
+    __shared__ double sh_p[TREE ? DV_NODES : 1], sh_u[TREE ? DV_NODES : 1], sh_seg[DV_MAX_SEGS], sh_wave[NW];
+    __shared__ int sh_parent[TREE ? DV_NODES : 1], sh_token[TREE ? DV_NODES : 1], sh_walk[2], sh_pick, sh_id;
+    __shared__ dv_chain_lds sh_chain;
     __shared__ uint32_t sh_out[(SIZE + 32) / 32];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, s = blockIdx.x;
     const dv_seq q = dv_seq_at(a, s);
+    int2 w = make_int2(0, 0);
+    if (a.probs != nullptr) w = a.walk[s];   // (of a sequence without rows: anything)
     if (q.rows == 0) { if (tid == 0) { a.accepted[s] = 0; a.next[s] = -1; } return; }
     const double cold = dv_cold(a, s);
     int node = q.row0, depth = 0;           // the row that the draw is behind
-    bool refused = false;                   // ... under a drafter's probabilities
-    for (int i = tid; i < a.segs; i += NT) sh_seg[i] = 0.0;
-    if (a.parent == nullptr) {
-        int2 w;
-        if (a.probs != nullptr) w = a.walk[s];
-        else w = dv_chain<T>(a, q, cold, true, &sh_refused);
+    bool refused = false;                   // ... and a draft was refused there (of a chain)
+    if (a.probs == nullptr) {
+        for (int i = tid; i < a.segs; i += NT) sh_seg[i] = 0.0;
+        __syncthreads();
+    }
+    if constexpr (!TREE) {
+        if (a.probs == nullptr) w = dv_chain<T>(a, q, cold, true, &sh_chain);
         node = w.x; refused = w.y != 0; depth = node - q.row0;
         if (a.path != nullptr) for (int i = tid; i <= depth; i += NT) a.path[q.row0 + i] = i;
         if (tid == 0) a.out_probs[q.row0] = 1.f;
@@ -267,12 +362,14 @@ k_draft_pick(const dv_args a)
         for (int n0 = 1; n0 < q.rows; n0 += DV_NODES) {
             const int n = min(DV_NODES, q.rows - n0);
             for (int i0 = 0; i0 < n; i0 += NT / GL) {
-                const int i = min(i0 + tid / GL, n - 1), local = n0 + i, up = a.parent[q.row0 + local], token = a.tokens[q.row0 + local];
-                const bool good = up >= 0 && up < local;
+                const int i = min(i0 + tid / GL, n - 1), row = q.row0 + n0 + i, up = a.parent[row], token = a.tokens[row], safe = min(max(token, 0), a.vocab - 1);
+                const double u = dv_u(a, row, 0);
+                const bool good = up >= 0 && up < n0 + i;
                 const int over = q.row0 + (good ? up : 0);
+                const float x = dv_one<T>(a.logits + (int64_t)over * a.row_bytes, safe);
                 const dv_row r = dv_row_of<GL>(a, over, cold);
-                const double p = good ? dv_prob<T>(a, r, over, token, cold) : 0.0;
-                if (tid % GL == 0) { sh_p[i] = p; sh_parent[i] = good ? up : -1; sh_token[i] = token; a.out_probs[q.row0 + local] = (float)p; }
+                const double p = good ? dv_prob(a, r, x, token, cold) : 0.0;
+                if (tid % GL == 0) { sh_p[i] = p; sh_u[i] = u; sh_parent[i] = good ? up : -1; sh_token[i] = token; a.out_probs[row] = (float)p; }
             }
             __syncthreads();
             if (wave == 0) {
@@ -281,10 +378,10 @@ k_draft_pick(const dv_args a)
                     const int up = i < n ? sh_parent[i] : -2;
                     uint64_t todo = __ballot(up == at);
                     while (todo) {
-                        const int k = b + __ffsll((unsigned long long)todo) - 1, token = sh_token[k], row = q.row0 + n0 + k;
+                        const int k = b + __ffsll((unsigned long long)todo) - 1, token = sh_token[k];
                         // a token that an earlier child has had
                         bool had = false;
-                        for (int j = max(at + 1, 1) - n0; j < k; j += 64) {
+                        for (int j = at + 1 - n0; j < k; j += 64) {
                             const int c = j + lane;
                             bool same = false;
                             if (c < k) same = c >= 0 ? sh_parent[c] == at && sh_token[c] == token : a.parent[q.row0 + n0 + c] == at && a.tokens[q.row0 + n0 + c] == token;
@@ -292,7 +389,7 @@ k_draft_pick(const dv_args a)
                         }
                         const double p = had ? 0.0 : sh_p[k];
                         todo &= todo - 1;
-                        if (dv_u(a, row, 0) * left < p) {
+                        if (sh_u[k] * left < p) {
                             at = n0 + k; ++depth; left = 1.0;
                             if (lane == 0) a.path[q.row0 + depth] = at;
                             for (int j = lane; j < a.segs; j += 64) sh_seg[j] = 0.0;
@@ -307,118 +404,126 @@ k_draft_pick(const dv_args a)
                         }
                     }
                 }
-                if (lane == 0) { sh_refused = at; sh_pick = depth; sh_wave[0] = left; }
+                if (lane == 0) { sh_walk[0] = at; sh_walk[1] = depth; sh_wave[0] = left; }
             }
             __syncthreads();
-            at = sh_refused; depth = sh_pick; left = sh_wave[0];
+            at = sh_walk[0]; depth = sh_walk[1]; left = sh_wave[0];
             __syncthreads();
         }
         node = q.row0 + at;
     }
-    if (tid == 0) { a.accepted[s] = depth; sh_id = -1; }
-    __syncthreads();
-    const dv_row r = dv_row_of<64>(a, node, cold);
-    if (!r.any) { if (tid == 0) a.next[s] = -1; return; }
-    if (cold == 0.0) { if (tid == 0) a.next[s] = r.first; return; }      // (with a refused draft too: it was another token)
+    const double u = dv_u(a, node, 1);
     const char *src = a.logits + (int64_t)node * a.row_bytes;
     const int head = dv_head<T>(src);
-    // without a drafter's probabilities: the refused tokens
-    const int last = a.probs != nullptr ? 0 : a.parent != nullptr ? q.rows : refused ? node - q.row0 + 2 : 0;
-    const int from = node - q.row0 + 1;
-    if (a.probs == nullptr && a.parent == nullptr && refused && tid == 0) {
-        const int token = a.tokens[node + 1];
-        if (token >= 0 && token < a.vocab) sh_seg[max(token - head, 0) / SIZE] = dv_prob<T>(a, r, node, token, cold);
-    }
-    __syncthreads();
-    // what the segments weigh
+    const dv_part *part = a.part + (int64_t)node * a.segs;
+    const double *rest = a.rest + (int64_t)s * a.segs;
+    const bool drawn = refused && a.probs != nullptr;
+    const dv_row r = dv_row_of<64>(a, node, cold);
+    if (tid == 0) { a.accepted[s] = depth; sh_id = -1; }
+    if (!r.any) { if (tid == 0) a.next[s] = -1; return; }
+    if (cold == 0.0) { if (tid == 0) a.next[s] = r.first; return; }      // (with a refused draft too: it was another token)
     const double inv = 1.0 / r.sum;
-    double total = 0.0;
-    for (int pass = 0; pass < 2 && !(total > 0.0); ++pass) {      // (nothing left of p - q, which rounding can bring about: p)
-        if (pass == 1) refused = false;
-        for (int i = tid; i < a.segs; i += NT) {
-            double w;
-            if (refused && a.probs != nullptr) w = a.rest[(int64_t)s * a.segs + i];
-            else { const dv_part p = a.part[(int64_t)node * a.segs + i]; w = p.sum * dv_weight(p.top, r.top, cold) * inv - (a.probs != nullptr ? 0.0 : sh_seg[i]); }
-            sh_seg[i] = fmax(w, 0.0);
+    // without a drafter's probabilities: the refused tokens, those of rows from .. last
+    const int from = node - q.row0 + 1, last = a.probs != nullptr ? 0 : TREE ? q.rows : refused ? from + 1 : 0;
+    if (!TREE && a.probs == nullptr && refused) {
+        if (tid == 0) {
+            const int token = a.tokens[node + 1];
+            if (token >= 0 && token < a.vocab) sh_seg[max(token - head, 0) / SIZE] = dv_prob(a, r, dv_one<T>(src, token), token, cold);
         }
         __syncthreads();
-        if (wave == 0) {
-            // sums up to each segment, 64 at a time
-            double before = 0.0;
-            for (int k = 0; k < a.segs; k += 64) {
-                double v = k + lane < a.segs ? sh_seg[k + lane] : 0.0;
+    }
+    // what the segments weigh, a lane a segment, in every wave alike
+    double sums[SC], total = 0.0;            // (up to and with each)
+    bool under = drawn;
+    for (int pass = 0; pass < 2; ++pass) {   // (nothing left of p - q, which rounding can bring about: p)
+        total = 0.0;
 #pragma unroll
-                for (int d = 1; d < 64; d <<= 1) { const double o = __shfl_up(v, d, 64); if (lane >= d) v += o; }
-                v += before;
-                before = __shfl(v, 63, 64);
-                if (k + lane < a.segs) sh_seg[k + lane] = v;      // (from here on: the sum up to and with it)
+        for (int c = 0; c < SC; ++c) {
+            sums[c] = 0.0;
+            if (c * 64 >= a.segs) continue;
+            const int i = c * 64 + lane;
+            double v = 0.0;
+            if (i < a.segs) {
+                if (under) v = rest[i];
+                else { const dv_part p = part[i]; v = p.sum * dv_weight(p.top, cold, r.top) * inv - (a.probs != nullptr ? 0.0 : sh_seg[i]); }
             }
-            if (lane == 0) sh_wave[0] = before;
+            sums[c] = total + dv_up_to(fmax(v, 0.0));
+            total = __shfl(sums[c], 63, 64);
         }
-        __syncthreads();
-        total = sh_wave[0];
-        __syncthreads();
-        if (a.probs == nullptr) break;
+        if (total > 0.0 || !under) break;
+        under = false;
     }
-    const double target = dv_u(a, node, 1) * total;
-    if (wave == 0) {
-        int pick = 0x7fffffff, some = -1;     // the first segment whose sum passes the target; the last that weighs anything
-        for (int k = lane; k < a.segs; k += 64) {
-            const double v = sh_seg[k], b = k > 0 ? sh_seg[k - 1] : 0.0;
-            if (v > b) { some = max(some, k); if (v > target) pick = min(pick, k); }
-        }
-        pick = dv_min_over_wave(pick);
-        some = -dv_min_over_wave(-some);
-        if (lane == 0) sh_pick = pick != 0x7fffffff ? pick : max(some, 0);
-    }
-    __syncthreads();
-    const int picked = sh_pick;
-    const float *drafter = refused && a.probs != nullptr ? a.probs + (int64_t)(node + 1) * a.probs_row : nullptr;
-    // the segment, and, should rounding have left nothing in it, the others in turn
-    for (int turn = -1; turn < a.segs; ++turn) {
-        const int seg = turn < 0 ? picked : turn;
-        const int begin = dv_begin(seg, head, SIZE), end = min(dv_begin(seg + 1, head, SIZE), a.vocab);
-        for (int i = tid; i < (SIZE + 32) / 32; i += NT) sh_out[i] = 0u;
-        __syncthreads();
-        for (int i = from + tid; i < last; i += NT) {
-            const int token = a.tokens[q.row0 + i];
-            const bool out = a.parent == nullptr || a.parent[q.row0 + i] == node - q.row0;
-            if (out && token >= begin && token < end) atomicOr(&sh_out[(token - begin) >> 5], 1u << ((token - begin) & 31));
-        }
-        __syncthreads();
-        // a thread's tokens lie side by side
-        const int per = (end - begin + NT - 1) / NT, i0 = begin + tid * per, i1 = min(i0 + per, end);
-        auto weight = [&](int i) {
-            if ((sh_out[(i - begin) >> 5] >> ((i - begin) & 31)) & 1) return 0.0;
-            const double p = dv_weight(dv_one<T>(src, i), r.top, cold) * inv;
-            return drafter != nullptr ? fmax(p - (double)drafter[i], 0.0) : p;
-        };
-        double mine = 0.0;
-        for (int i = i0; i < i1; ++i) mine += weight(i);
-        double upto = mine;
+    const double target = u * total;
+    // the first segment whose sum passes the target, or the last that weighs anything, and the sum before it
+    int picked = -1;
+    double before_it = 0.0;
+    {
+        double before = 0.0;
+        bool found = false;
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) { const double o = __shfl_up(upto, d, 64); if (lane >= d) upto += o; }
+        for (int c = 0; c < SC; ++c) {
+            if (c * 64 >= a.segs || found) continue;
+            double b = __shfl_up(sums[c], 1, 64);
+            if (lane == 0) b = before;
+            const uint64_t some = __ballot(sums[c] > b), past = __ballot(sums[c] > b && sums[c] > target);
+            const int l = past ? __ffsll((unsigned long long)past) - 1 : some ? 63 - __clzll((long long)some) : 0;
+            if (some) { picked = c * 64 + l; before_it = __shfl(b, l, 64); }
+            found = past != 0;
+            before = __shfl(sums[c], 63, 64);
+        }
+    }
+    const float *drafter = under ? a.probs + (int64_t)(node + 1) * a.probs_row : nullptr;
+    __syncthreads();
+    // the segment, and, should rounding have left nothing in it, the others in turn
+    for (int turn = picked < 0 ? 0 : -1; turn < a.segs; ++turn) {
+        const int seg = turn < 0 ? picked : turn, base = head + seg * SIZE, begin = dv_begin(seg, head, SIZE), end = min(base + SIZE, a.vocab), i0 = base + tid * N;
+        // a thread's tokens lie side by side (the one ahead of a row's first 16 bytes goes with the first thread's)
+        float x[N], d[N], x0 = -INFINITY, d0 = 0.f;
+        dv_tokens<T, N>(src, drafter, i0, end, x, d);
+        if (tid == 0 && begin < base) { x0 = dv_one<T>(src, 0); if (drafter != nullptr) d0 = drafter[0]; }
+        if (last > from) {
+            for (int i = tid; i < (SIZE + 32) / 32; i += NT) sh_out[i] = 0u;
+            __syncthreads();
+            for (int i = from + tid; i < last; i += NT) {
+                const int token = a.tokens[q.row0 + i];
+                const bool out = !TREE || a.parent[q.row0 + i] == node - q.row0;
+                if (out && token >= begin && token < end) atomicOr(&sh_out[(token - begin) >> 5], 1u << ((token - begin) & 31));
+            }
+            __syncthreads();
+            auto out = [&](int i) { return (sh_out[(i - begin) >> 5] >> ((i - begin) & 31)) & 1u; };
+#pragma unroll
+            for (int k = 0; k < N; ++k) if (i0 + k < end && out(i0 + k)) x[k] = -INFINITY;
+            if (begin < base && out(0)) x0 = -INFINITY;
+        }
+        const double w0 = tid == 0 ? fmax(dv_weight(x0, cold, r.top) * inv - (double)d0, 0.0) : 0.0;
+        double v[N], mine = w0;
+#pragma unroll
+        for (int k = 0; k < N; ++k) { v[k] = fmax(dv_weight(x[k], cold, r.top) * inv - (double)d[k], 0.0); mine += v[k]; }
+        double upto = dv_up_to(mine);
         if (lane == 63) sh_wave[wave] = upto;
         if (tid == 0) sh_pick = 0x7fffffff;
         __syncthreads();
-        double before = turn < 0 && seg > 0 ? sh_seg[seg - 1] : 0.0;
-        for (int k = 0; k < wave; ++k) before += sh_wave[k];
-        const double bound = turn < 0 ? target : -1.0, b = before + (upto - mine);
-        if (mine > 0.0) {
-            if (b + mine > bound) atomicMin(&sh_pick, tid);
-            atomicMax(&sh_id, tid);           // the last thread that has any
+        double b = turn < 0 ? before_it : 0.0;
+        for (int k = 0; k < wave; ++k) b += sh_wave[k];
+        b += upto - mine;
+        const double bound = turn < 0 ? target : -1.0;
+        const uint64_t some = __ballot(mine > 0.0), past = __ballot(mine > 0.0 && b + mine > bound);
+        if (lane == 0) {
+            if (past) atomicMin(&sh_pick, wave * 64 + __ffsll((unsigned long long)past) - 1);
+            if (some) atomicMax(&sh_id, wave * 64 + 63 - __clzll((long long)some));      // (the last thread that has any)
         }
         __syncthreads();
         const int who = sh_pick != 0x7fffffff ? sh_pick : sh_id;
         __syncthreads();
         if (who < 0) continue;               // (the same for all)
         if (tid == who) {
-            double sum = b;
-            int id = -1;
-            for (int i = i0; i < i1; ++i) {
-                const double w = weight(i);
-                sum += w;
-                if (w > 0.0) { id = i; if (sum > bound) break; }
+            double sum = b + w0;
+            int id = w0 > 0.0 ? 0 : -1;
+            bool stop = w0 > 0.0 && sum > bound;
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                sum += v[k];
+                if (!stop && v[k] > 0.0) { id = i0 + k; stop = sum > bound; }
             }
             a.next[s] = id;
         }
@@ -433,7 +538,7 @@ struct dv_plan { int e, segs; };
 static dv_plan plan(int64_t rows, int vocab)
 {
     dv_plan p;
-    p.e = 16;
+    p.e = rows * ((vocab + 4095) / 4096) > 4096 ? 32 : 16;
     p.segs = (vocab + 256 * p.e - 1) / (256 * p.e);
     return p;
 }
@@ -445,7 +550,7 @@ static int check(int64_t rows, int n_seq, int vocab)
     if (vocab < 1 || vocab > 4096 * DV_MAX_SEGS) { pv_set_error("vocab %d outside [1, %d]", vocab, 4096 * DV_MAX_SEGS); return PV_ERANGE; }
     // a launch has less than 2^32 threads
     const dv_plan p = plan(rows, vocab);
-    if (rows * p.segs >= (1 << 24) || (int64_t)n_seq * p.segs >= (1 << 24) || (int64_t)n_seq * 512 >= (1ll << 32)) { pv_set_error("%lld rows, %d sequences of %d tokens: more than a launch takes", (long long)rows, n_seq, vocab); return PV_ERANGE; }
+    if (rows * p.segs >= (1 << 24) || (int64_t)n_seq * p.segs >= (1 << 24) || (int64_t)n_seq * 1024 >= (1ll << 32)) { pv_set_error("%lld rows, %d sequences of %d tokens: more than a launch takes", (long long)rows, n_seq, vocab); return PV_ERANGE; }
     return PV_OK;
 }
 
@@ -468,7 +573,8 @@ static int launch(const dv_args &a, hipStream_t s)
 {
     if (a.rows > 0) { k_draft_rows<T, E><<<(unsigned)(a.rows * a.segs), 256, 0, s>>>(a); PV_HIP(hipGetLastError()); }
     if (a.probs != nullptr && a.rows > 0) { k_draft_rest<T, E><<<(unsigned)(a.n_seq * a.segs), 256, 0, s>>>(a); PV_HIP(hipGetLastError()); }
-    k_draft_pick<T, E><<<(unsigned)a.n_seq, 512, 0, s>>>(a);
+    if (a.parent != nullptr) k_draft_pick<T, E, 1024><<<(unsigned)a.n_seq, 1024, 0, s>>>(a);
+    else k_draft_pick<T, E, 512><<<(unsigned)a.n_seq, 512, 0, s>>>(a);
     PV_HIP(hipGetLastError());
     return PV_OK;
 }
@@ -498,5 +604,6 @@ extern "C" int pv_verify_drafts(const int32_t *row_start, int32_t n_seq, const v
     a.temperature = temperatures; a.hot = temperature; a.accepted = accepted; a.next = next_token; a.path = path; a.out_probs = probs;
     a.part = (dv_part *)workspace; a.rest = (double *)(a.part + (size_t)rows * p.segs); a.walk = (int2 *)(a.rest + (size_t)n_seq * p.segs);
     hipStream_t s = (hipStream_t)hip_stream;
+    if (p.e == 32) return dtype == PV_F32 ? launch<float, 32>(a, s) : dtype == PV_BF16 ? launch<__bf16, 32>(a, s) : launch<_Float16, 32>(a, s);
     return dtype == PV_F32 ? launch<float, 16>(a, s) : dtype == PV_BF16 ? launch<__bf16, 16>(a, s) : launch<_Float16, 16>(a, s);
 }
