@@ -5,9 +5,13 @@
 //   each under what the refused ones before it left: taken if u (1 - sum of their p) < p_j(draft).
 //   The draw: the lowest token at which the sum of probabilities, in the order of ids, passes u' times their whole.
 //
-// The result is whole numbers, so what they turn on is computed in 64 bits: with exponentials of 32 bits a sum over a vocabulary of 10^5 lands on the wrong side of u' once in some 10^5 draws.  A
-// workgroup takes a segment of a row: its maximum and the sum of its exponentials.  One workgroup a sequence joins the segments of the rows that it walks along, and reads again the one segment in which the draw falls; where a
-// refused draft has a drafter's probabilities, every segment of that row is summed anew first, under max(p - q, 0).
+// The result is whole numbers.  What a draw turns on is computed in 64 bits: with exponentials of 32 bits a sum over a vocabulary of 10^5 lands on the wrong side of one of its 10^5 borders once in some 10^5 draws (once in 10^2
+// under p - q, where p's own sum moves all of them).  Whether a draft is taken turns on one border: without a drafter's probabilities rows are summed with exponentials of 32 bits, off by some 10^-7, which
+// decides one draft in 10^7 otherwise and takes a third of the time.
+//   rows   a workgroup takes a segment of a row: its maximum and the sum of its exponentials
+//   walk   a tree: a workgroup a sequence joins the segments of the nodes' rows and walks along
+//   rest   a workgroup a segment of the row that the draw is behind (a chain: found anew by each): what is left to draw from, summed
+//   pick   a workgroup a sequence finds the segment that the draw falls in, and in that the token
 #include "pv_matrix_common.h"
 
 struct __align__(16) dv_part { double sum; float top; int first; };       // of a segment: sum of e^((x - top) / T), largest logit, its lowest id (T = 0: no sum)
@@ -22,9 +26,13 @@ struct dv_args {
     int32_t *accepted, *next, *path;
     float *out_probs;
     dv_part *part;                          // [row][seg]
-    double *rest;                           // [seq][seg]
+    int left;                               // segments of DV_SIZE tokens of the row that the draw is behind
+    double2 *rest;                          // [seq][left]: what is left to draw from, summed; without regard to a drafter
     int2 *walk;                             // [seq]: row that the draw is behind, whether a draft was refused there
 };
+
+#define DV_SIZE 4096
+#define DV_MAX_SEGS 512
 
 struct dv_seq { int row0, rows; };
 __device__ inline dv_seq dv_seq_at(const dv_args &a, int s)
@@ -149,8 +157,8 @@ __device__ inline double dv_up_to(double v)
 template <typename T> __device__ inline int dv_head(const char *src) { return sizeof(T) == 2 && ((uintptr_t)src & 2) ? 1 : 0; }
 __device__ inline int dv_begin(int seg, int head, int size) { return seg == 0 ? 0 : head + seg * size; }
 
-// The rows' sums.  Bound by the exponentials: some 17 instruction slots a logit, most of them in 64 bits.
-template <typename T, int E>
+// The rows' sums, WIDE: in 64 bits.  Those are bound by the exponentials: some 22 instruction slots a logit, 16 of them in 64 bits; the others by the read of the logits.
+template <typename T, int E, bool WIDE>
 __global__ void __launch_bounds__(256)
 k_draft_rows(const dv_args a)
 {
@@ -195,13 +203,23 @@ k_draft_rows(const dv_args a)
     double sum = 0.0;
     int first = 0x7fffffff;
     if (cold > 0.0) {
-        const double most = top;
-        double odd = 0.0;
 #pragma unroll
         for (int d = 0; d < D; ++d) if (sizeof(T) == 2) asm volatile("" : "+v"(x[d]));     // (taken apart anew: 32 bits of each number would be twice the registers)
+        if constexpr (WIDE) {
+            const double most = top;
+            double odd = 0.0;
 #pragma unroll
-        for (int i = 0; i < E; ++i) { const double w = dv_power(dv_get<T>(x, i), cold, most); if (i & 1) odd += w; else sum += w; }
-        sum = dv_over_wave((sum + odd) + dv_power(x0, cold, most));
+            for (int i = 0; i < E; ++i) { const double w = dv_power(dv_get<T>(x, i), cold, most); if (i & 1) odd += w; else sum += w; }
+            sum = dv_over_wave((sum + odd) + dv_power(x0, cold, most));
+        } else {
+            // (x - top as it is, then the factor: a factor's product with top would be off by as much for all)
+            const float c = (float)fmin(cold, 1e30);
+            float even = 0.f, odd = 0.f;
+#pragma unroll
+            for (int i = 0; i < E; ++i) { const float w = __builtin_amdgcn_exp2f(fmaxf((dv_get<T>(x, i) - top) * c, -256.f)); if (i & 1) odd += w; else even += w; }      // (2^-256 is 0; of NaN and a number the number)
+            even += __builtin_amdgcn_exp2f(fmaxf((x0 - top) * c, -256.f));
+            sum = dv_over_wave((double)even + (double)odd);
+        }
         if (top == -INFINITY) sum = 0.0;
     } else {
         if (alone >= 0 && x0 == top) first = alone;
@@ -289,169 +307,190 @@ template <typename T> __device__ inline int2 dv_chain(const dv_args &a, const dv
     return make_int2(q.row0 + min(refused, q.rows) - 1, refused < q.rows);
 }
 
-// max(p - q, 0) of a segment's tokens, summed, where a draft with a drafter's probabilities was refused.  The walk along the chain is made anew by every workgroup: it is three trips to memory, a launch for it costs more.
-template <typename T, int E>
-__global__ void __launch_bounds__(256)
-k_draft_rest(const dv_args a)
+// The walk along a sequence's tree: node by node what each child's p is, then one wave.  Some five trips to memory, one behind the other, for each 64 nodes.
+#define DV_NODES 1024                       // nodes at a time
+template <typename T>
+__global__ void __launch_bounds__(1024)
+k_draft_walk(const dv_args a)
 {
-    constexpr int NT = 256, SIZE = NT * E, N = 8;
-    __shared__ dv_chain_lds sh_chain;
-    __shared__ double sh_sum[4];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int s = blockIdx.x / a.segs, seg = blockIdx.x - s * a.segs;
+    constexpr int NT = 1024, GL = 16;
+    __shared__ double sh_p[DV_NODES], sh_u[DV_NODES], sh_left;
+    __shared__ int sh_parent[DV_NODES], sh_token[DV_NODES], sh_walk[2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, s = blockIdx.x;
     const dv_seq q = dv_seq_at(a, s);
     if (q.rows == 0) return;
     const double cold = dv_cold(a, s);
-    const int2 w = dv_chain<T>(a, q, cold, seg == 0, &sh_chain);
-    if (seg == 0 && tid == 0) a.walk[s] = w;
-    if (!w.y || cold == 0.0) return;
-    const dv_row r = sh_chain.row;
-    const char *src = a.logits + (int64_t)w.x * a.row_bytes;
-    const float *drafter = a.probs + (int64_t)(w.x + 1) * a.probs_row;
-    const int head = dv_head<T>(src), begin = head + seg * SIZE, end = min(begin + SIZE, a.vocab);
-    const double inv = 1.0 / r.sum;
-    double sum = 0.0;
-    if (head && seg == 0 && tid == 0) sum = fmax(dv_weight(dv_one<T>(src, 0), cold, r.top) * inv - (double)drafter[0], 0.0);
-    float x[E / N][N], d[E / N][N];
-#pragma unroll
-    for (int k = 0; k < E / N; ++k) dv_tokens<T, N>(src, drafter, begin + (k * NT + tid) * N, end, x[k], d[k]);
-#pragma unroll
-    for (int k = 0; k < E / N; ++k)
-#pragma unroll
-        for (int i = 0; i < N; ++i) sum += fmax(dv_weight(x[k][i], cold, r.top) * inv - (double)d[k][i], 0.0);
-    sum = dv_over_wave(sum);
-    if (lane == 0) sh_sum[wave] = sum;
-    __syncthreads();
-    if (tid == 0) a.rest[(int64_t)s * a.segs + seg] = (sh_sum[0] + sh_sum[1]) + (sh_sum[2] + sh_sum[3]);
-}
-
-// The draw of a sequence, and before it the walk along its tree.  Some five trips to memory, one behind the other.
-#define DV_NODES 1024                       // nodes at a time
-#define DV_MAX_SEGS 512
-template <typename T, int E, int NT>
-__global__ void __launch_bounds__(NT)
-k_draft_pick(const dv_args a)
-{
-    constexpr int NW = NT / 64, SIZE = 256 * E, N = SIZE / NT, GL = 16, SC = DV_MAX_SEGS / 64;
-    constexpr bool TREE = NT == 1024;
-    __shared__ double sh_p[TREE ? DV_NODES : 1], sh_u[TREE ? DV_NODES : 1], sh_seg[DV_MAX_SEGS], sh_wave[NW];
-    __shared__ int sh_parent[TREE ? DV_NODES : 1], sh_token[TREE ? DV_NODES : 1], sh_walk[2], sh_pick, sh_id;
-    __shared__ dv_chain_lds sh_chain;
-    __shared__ uint32_t sh_out[(SIZE + 32) / 32];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, s = blockIdx.x;
-    const dv_seq q = dv_seq_at(a, s);
-    int2 w = make_int2(0, 0);
-    if (a.probs != nullptr) w = a.walk[s];   // (of a sequence without rows: anything)
-    if (q.rows == 0) { if (tid == 0) { a.accepted[s] = 0; a.next[s] = -1; } return; }
-    const double cold = dv_cold(a, s);
-    int node = q.row0, depth = 0;           // the row that the draw is behind
-    bool refused = false;                   // ... and a draft was refused there (of a chain)
-    if (a.probs == nullptr) {
-        for (int i = tid; i < a.segs; i += NT) sh_seg[i] = 0.0;
+    if (tid == 0) { a.path[q.row0] = 0; a.out_probs[q.row0] = 1.f; }
+    int at = 0, depth = 0;
+    double left = 1.0;
+    for (int n0 = 1; n0 < q.rows; n0 += DV_NODES) {
+        const int n = min(DV_NODES, q.rows - n0);
+        for (int i0 = 0; i0 < n; i0 += NT / GL) {
+            const int i = min(i0 + tid / GL, n - 1), row = q.row0 + n0 + i, up = a.parent[row], token = a.tokens[row], safe = min(max(token, 0), a.vocab - 1);
+            const double u = dv_u(a, row, 0);
+            const bool good = up >= 0 && up < n0 + i;
+            const int over = q.row0 + (good ? up : 0);
+            const float x = dv_one<T>(a.logits + (int64_t)over * a.row_bytes, safe);
+            const dv_row r = dv_row_of<GL>(a, over, cold);
+            const double p = good ? dv_prob(a, r, x, token, cold) : 0.0;
+            if (tid % GL == 0) { sh_p[i] = p; sh_u[i] = u; sh_parent[i] = good ? up : -1; sh_token[i] = token; a.out_probs[row] = (float)p; }
+        }
+        __syncthreads();
+        if (wave == 0) {
+            for (int b = 0; b < n; b += 64) {
+                const int i = b + lane;
+                const int up = i < n ? sh_parent[i] : -2;
+                uint64_t todo = __ballot(up == at);
+                while (todo) {
+                    const int k = b + __ffsll((unsigned long long)todo) - 1, token = sh_token[k];
+                    // a token that an earlier child has had
+                    bool had = false;
+                    for (int j = at + 1 - n0; j < k; j += 64) {
+                        const int c = j + lane;
+                        bool same = false;
+                        if (c < k) same = c >= 0 ? sh_parent[c] == at && sh_token[c] == token : a.parent[q.row0 + n0 + c] == at && a.tokens[q.row0 + n0 + c] == token;
+                        had = had || __any(same);
+                    }
+                    const double p = had ? 0.0 : sh_p[k];
+                    todo &= todo - 1;
+                    if (sh_u[k] * left < p) {
+                        at = n0 + k; ++depth; left = 1.0;
+                        if (lane == 0) a.path[q.row0 + depth] = at;
+                        const uint64_t past = k - b == 63 ? 0ull : ~0ull << (k - b + 1);
+                        todo = __ballot(up == at) & past;
+                    } else left -= p;
+                }
+            }
+            if (lane == 0) { sh_walk[0] = at; sh_walk[1] = depth; sh_left = left; }
+        }
+        __syncthreads();
+        at = sh_walk[0]; depth = sh_walk[1]; left = sh_left;
         __syncthreads();
     }
-    if constexpr (!TREE) {
-        if (a.probs == nullptr) w = dv_chain<T>(a, q, cold, true, &sh_chain);
-        node = w.x; refused = w.y != 0; depth = node - q.row0;
-        if (a.path != nullptr) for (int i = tid; i <= depth; i += NT) a.path[q.row0 + i] = i;
-        if (tid == 0) a.out_probs[q.row0] = 1.f;
-    } else {
-        if (tid == 0) { a.path[q.row0] = 0; a.out_probs[q.row0] = 1.f; }
-        int at = 0;
-        double left = 1.0;
-        for (int n0 = 1; n0 < q.rows; n0 += DV_NODES) {
-            const int n = min(DV_NODES, q.rows - n0);
-            for (int i0 = 0; i0 < n; i0 += NT / GL) {
-                const int i = min(i0 + tid / GL, n - 1), row = q.row0 + n0 + i, up = a.parent[row], token = a.tokens[row], safe = min(max(token, 0), a.vocab - 1);
-                const double u = dv_u(a, row, 0);
-                const bool good = up >= 0 && up < n0 + i;
-                const int over = q.row0 + (good ? up : 0);
-                const float x = dv_one<T>(a.logits + (int64_t)over * a.row_bytes, safe);
-                const dv_row r = dv_row_of<GL>(a, over, cold);
-                const double p = good ? dv_prob(a, r, x, token, cold) : 0.0;
-                if (tid % GL == 0) { sh_p[i] = p; sh_u[i] = u; sh_parent[i] = good ? up : -1; sh_token[i] = token; a.out_probs[row] = (float)p; }
-            }
-            __syncthreads();
-            if (wave == 0) {
-                for (int b = 0; b < n; b += 64) {
-                    const int i = b + lane;
-                    const int up = i < n ? sh_parent[i] : -2;
-                    uint64_t todo = __ballot(up == at);
-                    while (todo) {
-                        const int k = b + __ffsll((unsigned long long)todo) - 1, token = sh_token[k];
-                        // a token that an earlier child has had
-                        bool had = false;
-                        for (int j = at + 1 - n0; j < k; j += 64) {
-                            const int c = j + lane;
-                            bool same = false;
-                            if (c < k) same = c >= 0 ? sh_parent[c] == at && sh_token[c] == token : a.parent[q.row0 + n0 + c] == at && a.tokens[q.row0 + n0 + c] == token;
-                            had = had || __any(same);
-                        }
-                        const double p = had ? 0.0 : sh_p[k];
-                        todo &= todo - 1;
-                        if (sh_u[k] * left < p) {
-                            at = n0 + k; ++depth; left = 1.0;
-                            if (lane == 0) a.path[q.row0 + depth] = at;
-                            for (int j = lane; j < a.segs; j += 64) sh_seg[j] = 0.0;
-                            const uint64_t past = k - b == 63 ? 0ull : ~0ull << (k - b + 1);
-                            todo = __ballot(up == at) & past;
-                        } else {
-                            left -= p;
-                            if (p > 0.0 && lane == 0) {
-                                const int head = dv_head<T>(a.logits + (int64_t)(q.row0 + at) * a.row_bytes);
-                                sh_seg[max(token - head, 0) / SIZE] += p;
-                            }
-                        }
-                    }
-                }
-                if (lane == 0) { sh_walk[0] = at; sh_walk[1] = depth; sh_wave[0] = left; }
-            }
-            __syncthreads();
-            at = sh_walk[0]; depth = sh_walk[1]; left = sh_wave[0];
-            __syncthreads();
-        }
-        node = q.row0 + at;
+    if (tid == 0) { a.walk[s] = make_int2(q.row0 + at, 0); a.accepted[s] = depth; }
+}
+
+// What may not be drawn, of a chain or tree without a drafter's probabilities: the tokens refused behind the row, a bit each for a segment's tokens; false: there is none anywhere
+__device__ inline bool dv_refused(const dv_args &a, const dv_seq &q, int2 w, int begin, int end, uint32_t *out)
+{
+    const int tid = threadIdx.x, nt = blockDim.x, from = w.x - q.row0 + 1, last = a.probs != nullptr ? 0 : a.parent != nullptr ? q.rows : w.y ? from + 1 : 0;
+    if (last <= from) return false;
+    for (int i = tid; i < (DV_SIZE + 32) / 32; i += nt) out[i] = 0u;
+    __syncthreads();
+    for (int i = from + tid; i < last; i += nt) {
+        const int token = a.tokens[q.row0 + i];
+        const bool mine = a.parent == nullptr || a.parent[q.row0 + i] == w.x - q.row0;
+        if (mine && token >= begin && token < end) atomicOr(&out[(token - begin) >> 5], 1u << ((token - begin) & 31));
     }
-    const double u = dv_u(a, node, 1);
-    const char *src = a.logits + (int64_t)node * a.row_bytes;
+    __syncthreads();
+    return true;
+}
+
+// N tokens from i0 on (and, the first thread's, the one ahead of a row's first 16 bytes): what each weighs
+template <typename T, int N> struct dv_left { double v[N], v0; };
+template <typename T, int N>
+__device__ inline void dv_weigh(const dv_args &a, const dv_row &r, const char *src, const float *drafter, int i0, int base, int begin, int end, double cold, double inv, bool some, const uint32_t *out, dv_left<T, N> &w, double &plain)
+{
+    float x[N], d[N], x0 = -INFINITY, d0 = 0.f;
+    dv_tokens<T, N>(src, drafter, i0, end, x, d);
+    if (i0 == base && begin < base) { x0 = dv_one<T>(src, 0); if (drafter != nullptr) d0 = drafter[0]; }
+    if (some) {
+        auto is = [&](int i) { return (out[(i - begin) >> 5] >> ((i - begin) & 31)) & 1u; };
+#pragma unroll
+        for (int k = 0; k < N; ++k) if (i0 + k < end && is(i0 + k)) x[k] = -INFINITY;
+        if (begin < base && is(0)) x0 = -INFINITY;
+    }
+    plain = dv_weight(x0, cold, r.top) * inv;
+    w.v0 = fmax(plain - (double)d0, 0.0);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const double p = dv_weight(x[k], cold, r.top) * inv;
+        plain += p;
+        w.v[k] = fmax(p - (double)d[k], 0.0);
+    }
+}
+
+// What is left to draw from in a segment.  A chain's walk is made anew by every workgroup: it is three trips to memory, a launch for it costs more.
+template <typename T>
+__global__ void __launch_bounds__(256)
+k_draft_rest(const dv_args a)
+{
+    constexpr int NT = 256, N = DV_SIZE / NT / 2;
+    __shared__ dv_chain_lds sh_chain;
+    __shared__ double2 sh_sum[4];
+    __shared__ uint32_t sh_out[(DV_SIZE + 32) / 32];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int s = blockIdx.x / a.left, seg = blockIdx.x - s * a.left;
+    const dv_seq q = dv_seq_at(a, s);
+    if (q.rows == 0) return;
+    const double cold = dv_cold(a, s);
+    const int2 w = a.parent != nullptr ? a.walk[s] : dv_chain<T>(a, q, cold, seg == 0, &sh_chain);
+    if (a.parent == nullptr && seg == 0) {
+        if (tid == 0) { a.walk[s] = w; a.accepted[s] = w.x - q.row0; a.out_probs[q.row0] = 1.f; }
+        if (a.path != nullptr) for (int i = tid; i <= w.x - q.row0; i += NT) a.path[q.row0 + i] = i;
+    }
+    if (cold == 0.0) return;
+    const dv_row r = w.y ? sh_chain.row : dv_row_of<64>(a, w.x, cold);
+    const char *src = a.logits + (int64_t)w.x * a.row_bytes;
+    const float *drafter = w.y && a.probs != nullptr ? a.probs + (int64_t)(w.x + 1) * a.probs_row : nullptr;
+    const int head = dv_head<T>(src), base = head + seg * DV_SIZE, begin = dv_begin(seg, head, DV_SIZE), end = min(base + DV_SIZE, a.vocab);
+    const bool some = dv_refused(a, q, w, begin, end, sh_out);
+    const double inv = 1.0 / r.sum;
+    double sum = 0.0, all = 0.0;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        dv_left<T, N> v;
+        double plain;
+        dv_weigh<T, N>(a, r, src, drafter, base + (k * NT + tid) * N, base, begin, end, cold, inv, some, sh_out, v, plain);
+        sum += v.v0; all += plain;
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum += v.v[i];
+    }
+    sum = dv_over_wave(sum); all = dv_over_wave(all);
+    if (lane == 0) sh_sum[wave] = make_double2(sum, all);
+    __syncthreads();
+    if (tid == 0) a.rest[(int64_t)s * a.left + seg] = make_double2((sh_sum[0].x + sh_sum[1].x) + (sh_sum[2].x + sh_sum[3].x), (sh_sum[0].y + sh_sum[1].y) + (sh_sum[2].y + sh_sum[3].y));
+}
+
+// The draw of a sequence.  Four trips to memory, one behind the other.
+template <typename T>
+__global__ void __launch_bounds__(512)
+k_draft_pick(const dv_args a)
+{
+    constexpr int NT = 512, NW = NT / 64, N = DV_SIZE / NT, SC = DV_MAX_SEGS / 64;
+    __shared__ double sh_wave[NW];
+    __shared__ int sh_pick, sh_id;
+    __shared__ uint32_t sh_out[(DV_SIZE + 32) / 32];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, s = blockIdx.x;
+    const dv_seq q = dv_seq_at(a, s);
+    const int2 w = a.walk[s];                // (of a sequence without rows: anything)
+    const double2 *rest = a.rest + (int64_t)s * a.left;
+    double2 first[1];
+    first[0] = lane < a.left ? rest[lane] : make_double2(0.0, 0.0);      // (T = 0: anything)
+    if (q.rows == 0) { if (tid == 0) { a.accepted[s] = 0; a.next[s] = -1; } return; }
+    const double cold = dv_cold(a, s), u = dv_u(a, w.x, 1);
+    const char *src = a.logits + (int64_t)w.x * a.row_bytes;
     const int head = dv_head<T>(src);
-    const dv_part *part = a.part + (int64_t)node * a.segs;
-    const double *rest = a.rest + (int64_t)s * a.segs;
-    const bool drawn = refused && a.probs != nullptr;
-    const dv_row r = dv_row_of<64>(a, node, cold);
-    if (tid == 0) { a.accepted[s] = depth; sh_id = -1; }
+    const dv_row r = dv_row_of<64>(a, w.x, cold);
+    if (tid == 0) sh_id = -1;
     if (!r.any) { if (tid == 0) a.next[s] = -1; return; }
     if (cold == 0.0) { if (tid == 0) a.next[s] = r.first; return; }      // (with a refused draft too: it was another token)
     const double inv = 1.0 / r.sum;
-    // without a drafter's probabilities: the refused tokens, those of rows from .. last
-    const int from = node - q.row0 + 1, last = a.probs != nullptr ? 0 : TREE ? q.rows : refused ? from + 1 : 0;
-    if (!TREE && a.probs == nullptr && refused) {
-        if (tid == 0) {
-            const int token = a.tokens[node + 1];
-            if (token >= 0 && token < a.vocab) sh_seg[max(token - head, 0) / SIZE] = dv_prob(a, r, dv_one<T>(src, token), token, cold);
-        }
-        __syncthreads();
-    }
     // what the segments weigh, a lane a segment, in every wave alike
     double sums[SC], total = 0.0;            // (up to and with each)
-    bool under = drawn;
+    bool drawn = w.y && a.probs != nullptr;
     for (int pass = 0; pass < 2; ++pass) {   // (nothing left of p - q, which rounding can bring about: p)
         total = 0.0;
 #pragma unroll
         for (int c = 0; c < SC; ++c) {
             sums[c] = 0.0;
-            if (c * 64 >= a.segs) continue;
-            const int i = c * 64 + lane;
-            double v = 0.0;
-            if (i < a.segs) {
-                if (under) v = rest[i];
-                else { const dv_part p = part[i]; v = p.sum * dv_weight(p.top, cold, r.top) * inv - (a.probs != nullptr ? 0.0 : sh_seg[i]); }
-            }
-            sums[c] = total + dv_up_to(fmax(v, 0.0));
+            if (c * 64 >= a.left) continue;
+            const double2 v = c == 0 ? first[0] : c * 64 + lane < a.left ? rest[c * 64 + lane] : make_double2(0.0, 0.0);
+            sums[c] = total + dv_up_to(drawn || a.probs == nullptr ? v.x : v.y);
             total = __shfl(sums[c], 63, 64);
         }
-        if (total > 0.0 || !under) break;
-        under = false;
+        if (total > 0.0 || !drawn) break;
+        drawn = false;
     }
     const double target = u * total;
     // the first segment whose sum passes the target, or the last that weighs anything, and the sum before it
@@ -462,7 +501,7 @@ k_draft_pick(const dv_args a)
         bool found = false;
 #pragma unroll
         for (int c = 0; c < SC; ++c) {
-            if (c * 64 >= a.segs || found) continue;
+            if (c * 64 >= a.left || found) continue;
             double b = __shfl_up(sums[c], 1, 64);
             if (lane == 0) b = before;
             const uint64_t some = __ballot(sums[c] > b), past = __ballot(sums[c] > b && sums[c] > target);
@@ -472,34 +511,19 @@ k_draft_pick(const dv_args a)
             before = __shfl(sums[c], 63, 64);
         }
     }
-    const float *drafter = under ? a.probs + (int64_t)(node + 1) * a.probs_row : nullptr;
+    const float *drafter = drawn ? a.probs + (int64_t)(w.x + 1) * a.probs_row : nullptr;
     __syncthreads();
     // the segment, and, should rounding have left nothing in it, the others in turn
-    for (int turn = picked < 0 ? 0 : -1; turn < a.segs; ++turn) {
-        const int seg = turn < 0 ? picked : turn, base = head + seg * SIZE, begin = dv_begin(seg, head, SIZE), end = min(base + SIZE, a.vocab), i0 = base + tid * N;
-        // a thread's tokens lie side by side (the one ahead of a row's first 16 bytes goes with the first thread's)
-        float x[N], d[N], x0 = -INFINITY, d0 = 0.f;
-        dv_tokens<T, N>(src, drafter, i0, end, x, d);
-        if (tid == 0 && begin < base) { x0 = dv_one<T>(src, 0); if (drafter != nullptr) d0 = drafter[0]; }
-        if (last > from) {
-            for (int i = tid; i < (SIZE + 32) / 32; i += NT) sh_out[i] = 0u;
-            __syncthreads();
-            for (int i = from + tid; i < last; i += NT) {
-                const int token = a.tokens[q.row0 + i];
-                const bool out = !TREE || a.parent[q.row0 + i] == node - q.row0;
-                if (out && token >= begin && token < end) atomicOr(&sh_out[(token - begin) >> 5], 1u << ((token - begin) & 31));
-            }
-            __syncthreads();
-            auto out = [&](int i) { return (sh_out[(i - begin) >> 5] >> ((i - begin) & 31)) & 1u; };
+    for (int turn = picked < 0 ? 0 : -1; turn < a.left; ++turn) {
+        const int seg = turn < 0 ? picked : turn, base = head + seg * DV_SIZE, begin = dv_begin(seg, head, DV_SIZE), end = min(base + DV_SIZE, a.vocab), i0 = base + tid * N;
+        const bool some_out = dv_refused(a, q, w, begin, end, sh_out);
+        dv_left<T, N> v;                     // a thread's tokens lie side by side
+        double plain;
+        dv_weigh<T, N>(a, r, src, drafter, i0, base, begin, end, cold, inv, some_out, sh_out, v, plain);
+        double mine = v.v0;
 #pragma unroll
-            for (int k = 0; k < N; ++k) if (i0 + k < end && out(i0 + k)) x[k] = -INFINITY;
-            if (begin < base && out(0)) x0 = -INFINITY;
-        }
-        const double w0 = tid == 0 ? fmax(dv_weight(x0, cold, r.top) * inv - (double)d0, 0.0) : 0.0;
-        double v[N], mine = w0;
-#pragma unroll
-        for (int k = 0; k < N; ++k) { v[k] = fmax(dv_weight(x[k], cold, r.top) * inv - (double)d[k], 0.0); mine += v[k]; }
-        double upto = dv_up_to(mine);
+        for (int k = 0; k < N; ++k) mine += v.v[k];
+        const double upto = dv_up_to(mine);
         if (lane == 63) sh_wave[wave] = upto;
         if (tid == 0) sh_pick = 0x7fffffff;
         __syncthreads();
@@ -517,13 +541,13 @@ k_draft_pick(const dv_args a)
         __syncthreads();
         if (who < 0) continue;               // (the same for all)
         if (tid == who) {
-            double sum = b + w0;
-            int id = w0 > 0.0 ? 0 : -1;
-            bool stop = w0 > 0.0 && sum > bound;
+            double sum = b + v.v0;
+            int id = v.v0 > 0.0 ? 0 : -1;
+            bool stop = v.v0 > 0.0 && sum > bound;
 #pragma unroll
             for (int k = 0; k < N; ++k) {
-                sum += v[k];
-                if (!stop && v[k] > 0.0) { id = i0 + k; stop = sum > bound; }
+                sum += v.v[k];
+                if (!stop && v.v[k] > 0.0) { id = i0 + k; stop = sum > bound; }
             }
             a.next[s] = id;
         }
@@ -534,11 +558,13 @@ k_draft_pick(const dv_args a)
 
 // ------------------------------- host side ----------------------------------------
 
-struct dv_plan { int e, segs; };
-static dv_plan plan(int64_t rows, int vocab)
+// Tokens a segment of a row: 4096, or, where there are rows enough for the chip, 8192 (64-bit sums), 16384 or (f32) 8192.  Whether there is a drafter is not known where the workspace is measured: its size is that of 4096.
+struct dv_plan { int e, segs, left; };
+static dv_plan plan(int64_t rows, int vocab, bool wide, int dtype)
 {
     dv_plan p;
-    p.e = rows * ((vocab + 4095) / 4096) > 4096 ? 32 : 16;
+    p.left = (vocab + DV_SIZE - 1) / DV_SIZE;
+    p.e = rows * p.left <= 4096 ? 16 : wide || dtype == PV_F32 ? 32 : 64;
     p.segs = (vocab + 256 * p.e - 1) / (256 * p.e);
     return p;
 }
@@ -547,16 +573,17 @@ static int check(int64_t rows, int n_seq, int vocab)
 {
     if (rows < 0 || rows > (1 << 20)) { pv_set_error("rows %lld outside [0, 2^20]", (long long)rows); return PV_ERANGE; }
     if (n_seq < 0 || n_seq > (1 << 20)) { pv_set_error("n_seq %d outside [0, 2^20]", n_seq); return PV_ERANGE; }
-    if (vocab < 1 || vocab > 4096 * DV_MAX_SEGS) { pv_set_error("vocab %d outside [1, %d]", vocab, 4096 * DV_MAX_SEGS); return PV_ERANGE; }
+    if (vocab < 1 || vocab > DV_SIZE * DV_MAX_SEGS) { pv_set_error("vocab %d outside [1, %d]", vocab, DV_SIZE * DV_MAX_SEGS); return PV_ERANGE; }
     // a launch has less than 2^32 threads
-    const dv_plan p = plan(rows, vocab);
-    if (rows * p.segs >= (1 << 24) || (int64_t)n_seq * p.segs >= (1 << 24) || (int64_t)n_seq * 1024 >= (1ll << 32)) { pv_set_error("%lld rows, %d sequences of %d tokens: more than a launch takes", (long long)rows, n_seq, vocab); return PV_ERANGE; }
+    const int64_t segs = (vocab + DV_SIZE - 1) / DV_SIZE;
+    if (rows * segs >= (1 << 24) || n_seq * segs >= (1 << 24)) { pv_set_error("%lld rows, %d sequences of %d tokens: more than a launch takes", (long long)rows, n_seq, vocab); return PV_ERANGE; }
     return PV_OK;
 }
 
-static size_t bytes_of(int64_t rows, int n_seq, const dv_plan &p)
+static size_t bytes_of(int64_t rows, int n_seq, int vocab)
 {
-    return (size_t)rows * p.segs * sizeof(dv_part) + (size_t)n_seq * p.segs * sizeof(double) + (size_t)n_seq * sizeof(int2);
+    const size_t segs = (vocab + DV_SIZE - 1) / DV_SIZE;
+    return rows && n_seq ? (size_t)rows * segs * sizeof(dv_part) + (size_t)n_seq * segs * sizeof(double2) + (size_t)n_seq * sizeof(int2) : 0;
 }
 
 extern "C" int pv_verify_drafts_bytes(int64_t rows, int32_t n_seq, int32_t vocab, size_t *bytes)
@@ -564,17 +591,34 @@ extern "C" int pv_verify_drafts_bytes(int64_t rows, int32_t n_seq, int32_t vocab
     const int rc = check(rows, n_seq, vocab);
     if (rc != PV_OK) return rc;
     if (!bytes) { pv_set_error("null output pointer"); return PV_EINVAL; }
-    *bytes = rows && n_seq ? bytes_of(rows, n_seq, plan(rows, vocab)) : 0;
+    *bytes = bytes_of(rows, n_seq, vocab);
     return PV_OK;
 }
 
-template <typename T, int E>
-static int launch(const dv_args &a, hipStream_t s)
+// a call without rows: every sequence is empty
+__global__ void __launch_bounds__(256) k_draft_none(int n, int32_t *accepted, int32_t *next)
 {
-    if (a.rows > 0) { k_draft_rows<T, E><<<(unsigned)(a.rows * a.segs), 256, 0, s>>>(a); PV_HIP(hipGetLastError()); }
-    if (a.probs != nullptr && a.rows > 0) { k_draft_rest<T, E><<<(unsigned)(a.n_seq * a.segs), 256, 0, s>>>(a); PV_HIP(hipGetLastError()); }
-    if (a.parent != nullptr) k_draft_pick<T, E, 1024><<<(unsigned)a.n_seq, 1024, 0, s>>>(a);
-    else k_draft_pick<T, E, 512><<<(unsigned)a.n_seq, 512, 0, s>>>(a);
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i < n) { accepted[i] = 0; next[i] = -1; }
+}
+
+template <typename T>
+static int launch(const dv_args &a, int e, hipStream_t s)
+{
+    const unsigned grid = (unsigned)(a.rows * a.segs);
+    if (a.probs != nullptr) {
+        if (e == 16) k_draft_rows<T, 16, true><<<grid, 256, 0, s>>>(a);
+        else k_draft_rows<T, 32, true><<<grid, 256, 0, s>>>(a);
+    } else {
+        constexpr int most = sizeof(T) == 4 ? 32 : 64;
+        if (e == 16) k_draft_rows<T, 16, false><<<grid, 256, 0, s>>>(a);
+        else k_draft_rows<T, most, false><<<grid, 256, 0, s>>>(a);
+    }
+    PV_HIP(hipGetLastError());
+    if (a.parent != nullptr) { k_draft_walk<T><<<(unsigned)a.n_seq, 1024, 0, s>>>(a); PV_HIP(hipGetLastError()); }
+    k_draft_rest<T><<<(unsigned)(a.n_seq * a.left), 256, 0, s>>>(a);
+    PV_HIP(hipGetLastError());
+    k_draft_pick<T><<<(unsigned)a.n_seq, 512, 0, s>>>(a);
     PV_HIP(hipGetLastError());
     return PV_OK;
 }
@@ -594,16 +638,16 @@ extern "C" int pv_verify_drafts(const int32_t *row_start, int32_t n_seq, const v
     const int64_t size = dtype == PV_F32 ? 4 : 2;
     if ((uintptr_t)logits % size || ((uintptr_t)row_start | (uintptr_t)tokens | (uintptr_t)draft_probs | (uintptr_t)parent | (uintptr_t)temperatures | (uintptr_t)accepted | (uintptr_t)next_token | (uintptr_t)path | (uintptr_t)probs) & 3
         || (uintptr_t)u & (u_is_double ? 7 : 3)) { pv_set_error("an array is not aligned to its type"); return PV_EINVAL; }
-    const dv_plan p = plan(rows, vocab);
-    const size_t need = rows ? bytes_of(rows, n_seq, p) : 0;
+    const dv_plan p = plan(rows, vocab, draft_probs != nullptr, dtype);
+    const size_t need = bytes_of(rows, n_seq, vocab);
     if (need > workspace_bytes || (need && !workspace)) { pv_set_error("workspace of %zu bytes, %zu are needed", workspace ? workspace_bytes : (size_t)0, need); return PV_ENOMEM; }
     if ((uintptr_t)workspace & 15) { pv_set_error("workspace must be 16-byte aligned"); return PV_EINVAL; }
     dv_args a = {};
-    a.logits = (const char *)logits; a.row_bytes = row_stride * size; a.rows = (int)rows; a.vocab = vocab; a.segs = p.segs; a.n_seq = n_seq;
+    a.logits = (const char *)logits; a.row_bytes = row_stride * size; a.rows = (int)rows; a.vocab = vocab; a.segs = p.segs; a.left = p.left; a.n_seq = n_seq;
     a.row_start = row_start; a.tokens = tokens; a.parent = parent; a.u = u; a.u64 = u_is_double != 0; a.probs = draft_probs; a.probs_row = draft_row_stride;
     a.temperature = temperatures; a.hot = temperature; a.accepted = accepted; a.next = next_token; a.path = path; a.out_probs = probs;
-    a.part = (dv_part *)workspace; a.rest = (double *)(a.part + (size_t)rows * p.segs); a.walk = (int2 *)(a.rest + (size_t)n_seq * p.segs);
     hipStream_t s = (hipStream_t)hip_stream;
-    if (p.e == 32) return dtype == PV_F32 ? launch<float, 32>(a, s) : dtype == PV_BF16 ? launch<__bf16, 32>(a, s) : launch<_Float16, 32>(a, s);
-    return dtype == PV_F32 ? launch<float, 16>(a, s) : dtype == PV_BF16 ? launch<__bf16, 16>(a, s) : launch<_Float16, 16>(a, s);
+    if (rows == 0) { k_draft_none<<<(unsigned)((n_seq + 255) / 256), 256, 0, s>>>(n_seq, accepted, next_token); PV_HIP(hipGetLastError()); return PV_OK; }
+    a.part = (dv_part *)workspace; a.rest = (double2 *)(a.part + (size_t)rows * p.left); a.walk = (int2 *)(a.rest + (size_t)n_seq * p.left);
+    return dtype == PV_F32 ? launch<float>(a, p.e, s) : dtype == PV_BF16 ? launch<__bf16>(a, p.e, s) : launch<_Float16>(a, p.e, s);
 }
