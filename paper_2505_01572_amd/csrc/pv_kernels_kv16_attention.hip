@@ -2,8 +2,7 @@
 //
 // The query rows of a kv head are packed token by token: row m of a sequence is query head m % group of its token m / group.  Everything is computed transposed: S^T (keys x rows) = K Q^T,
 // O^T (features x rows) = V^T P^T; the accumulators of S^T are, two groups of 16 keys side by side, the second operand of the other product.  Softmax with the running maximum and sum, all in 32 bits,
-// in powers of two.  A weight is a pair of numbers of the cache's type (16 significant bits of bf16, 22 of f16): one would add as much error as the rounding of the output.  f16 weights are
-// kept times 2^15, so that many small ones beside a large one count fully.
+// in powers of two.  f16 weights are kept times 2^15, so that many small ones beside a large one count fully.
 #include <atomic>
 #include "pv_kv16.h"
 
@@ -15,7 +14,7 @@ struct kv16_attn_args {
     float *lse;
     const uint64_t *mask; int words;        // [row][words]
     float *part_o, *part_ml;                // [row][query head][split][HD], [2] (maximum, sum)
-    int group, n_q_heads, nsplit, chunk;    // chunk: keys a split, a multiple of 256
+    int group, n_q_heads, nsplit, chunk;    // chunk: keys a split, a multiple of 64
     float scale2;                           // |scale| log2(e), more than 0 (a scale of 0: 1, and q is 0)
     uint32_t q_and, q_xor;                  // what q passes through: its sign is the scale's
 };
@@ -125,14 +124,11 @@ __device__ inline uint64_t kv16_sees(const uint64_t *mask, int words, int p, int
 {
     uint64_t w = kv16_first(min(end, nk) - p);
     if (mask != nullptr) {
-        const int s = p - len;                                           // slot of the first key
-        if (s <= -64) w = ~0ull;
-        else {
-            const int i = s < 0 ? 0 : s >> 6, sh = s & 63;
-            const uint64_t lo = i < words ? mask[i] : 0ull, hi = s >= 0 && sh != 0 && i + 1 < words ? mask[i + 1] : 0ull;
-            w = s < 0 ? kv16_first(-s) | lo << -s : lo >> sh | (sh != 0 ? hi << (64 - sh) : 0ull);
-            w &= kv16_first(slots - s);
-        }
+        const int s = p - len, i = max(s, 0) >> 6, sh = s & 63;          // slot of the first key
+        const uint64_t lo = mask[min(i, words - 1)], hi = mask[min(i + 1, words - 1)];       // (loads without branches)
+        const uint64_t l = i < words ? lo : 0ull, h = s >= 0 && sh != 0 && i + 1 < words ? hi << (64 - sh) : 0ull;
+        w = s <= -64 ? ~0ull : s < 0 ? kv16_first(-s) | l << -s : l >> sh | h;
+        w &= kv16_first(slots - s);
         w &= kv16_first(nk - p);
     }
     return w;
@@ -287,7 +283,7 @@ __device__ inline void kv16_finish4(const kv16_attn_args &a, const kv16_row &w, 
 }
 
 // Few rows: one workgroup is a kv head, a tile of 16 packed rows of a sequence, a chunk of its keys; the waves take 32 keys in turn, straight from memory to registers, and are joined
-// through LDS at the end.  Bound by the read of the cache: the next 32 keys' K is asked for when this one's scores are there, V when its products are.
+// through LDS at the end.  A weight is a pair of numbers of the cache's type (16 significant bits in bf16, 22 in f16): the matrix cores have the time.  Bound by the read of the cache: the next 32 keys' K is asked for when this one's scores are there, V when its products are.
 template <int HD, typename S>
 __global__ void __launch_bounds__(256)
 k_kv16_attn(const kv16_attn_args a)
@@ -439,22 +435,50 @@ k_kv16_attn(const kv16_attn_args a)
     }
 }
 
-// Many rows: a workgroup is a kv head, 64 RT packed rows of a sequence (16 RT a wave), a chunk of its keys.  64 keys at a time go through LDS, copied straight from memory a step ahead, each wave
-// a group of 16.
-template <int HD, int RT>
+// Many rows: a workgroup is a kv head, 64 RT packed rows of a sequence (16 RT a wave), a chunk of its keys.  64 keys at a time go through LDS, copied straight from memory, each wave a group of 16: values a step ahead,
+// keys two, because the products with the next step's keys are made while this one's scores become weights: those keep the vector ALU busy, which is what bounds it (an exponential takes four turns), the products the
+// matrix cores.  A weight is one number of the cache's type here, 8 significant bits in bf16: rounded to nearest, they add to an output as much as its own rounding does; a pair of them costs half as many products
+// again.  The sum is of the weights before they are rounded.
+template <int HD>
 struct kv16_wide {
     static constexpr int KS = HD / 32;
-    static constexpr int buffer = 4 * 2 * KS * 64;                       // uint4 of 64 keys: [group][K | V][b][lane]
-    static constexpr int lds = 2 * buffer * 16 + 16;                     // and whether numbers that are not finite were among values that not every row sees
+    static constexpr int buffer = 4 * KS * 64;                           // uint4 of 64 keys' K or V: [group][b][lane]
+    static constexpr int lds = 4 * buffer * 16 + 16;                     // two of K, two of V, and whether numbers that are not finite were among values that not every row sees
 };
+
+__device__ inline float kv16_maximum(float a, float b) { return __builtin_elementwise_maximum(a, b); }      // (NaN if either is)
+
+// A row tile's place in the softmax: the score that weights are relative to, what to add to a score for its exponent, what the results so far are worth under it, sum of weights.  The score is the largest so far or up to 8 less
+// (in powers of two): results are scaled to another only where a score goes further, which is hardly ever.  A weight is then up to 2^8, so f16 weights are kept times 2^7.
+#define KV16_SLACK 8.f
+template <typename S> constexpr int kv16_wide_bias() { return __is_same(S, __bf16) ? 0 : 7; }
+struct kv16_tile { float m, c, keep, l; };
+template <typename S> __device__ inline void kv16_under(kv16_tile &T, float mx, float scale2)      // mx: of the lane's 16 scores of the next 64 keys
+{
+    mx = with_lane32(with_lane16(mx, kv16_maximum), kv16_maximum) * scale2;
+    const float m = mx > T.m + KV16_SLACK ? mx : T.m, ref = m == -INFINITY ? 0.f : m;      // (nothing seen so far: 0; a score that is NaN: its weight is)
+    T.keep = __builtin_amdgcn_exp2f(T.m - ref); T.c = (float)kv16_wide_bias<S>() - ref; T.m = m;
+}
+__device__ inline float kv16_maximum4(float m, f32x4 x) { return kv16_maximum(kv16_maximum(kv16_maximum(kv16_maximum(m, x[0]), x[1]), x[2]), x[3]); }
+template <typename S> __device__ inline uint2 kv16_weights4(f32x4 x, float scale2, float c, float &sum)
+{
+    float p[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(x[r], scale2, c));
+    sum += (p[0] + p[1]) + (p[2] + p[3]);
+    uint2 w = make_uint2(kv16_two<S>(p[0], p[1]), kv16_two<S>(p[2], p[3]));
+    asm volatile("" : "+v"(w.x), "+v"(w.y));     // (made here, not where they are used)
+    return w;
+}
+
 template <int HD, int RT, typename S>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 k_kv16_attn_wide(const kv16_attn_args a)
 {
-    using W = kv16_wide<HD, RT>;
+    using W = kv16_wide<HD>;
     constexpr int KS = W::KS, TR = 64 * RT;
     extern __shared__ uint4 wide_lds[];
-    int *spoilt = (int *)(wide_lds + 2 * W::buffer);
+    int *spoilt = (int *)(wide_lds + 4 * W::buffer);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, jl = lane & 15, g = lane >> 4;
     const int kvh = blockIdx.x % a.pool.n_heads, split = blockIdx.y, units = gridDim.x / a.pool.n_heads;
     int tile = 0;
@@ -473,51 +497,82 @@ k_kv16_attn_wide(const kv16_attn_args a)
     const uint32_t block = (uint32_t)(2 * HD) << shift, in_page = (1u << shift) - 1;
     const uint64_t page_bytes = (uint64_t)2 * block * a.pool.n_heads;
     const char *base = a.pool.pages + (size_t)kvh * 2 * block;
-    const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(wide_lds)) + wave * 2 * KS * 1024;
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(wide_lds)) + wave * KS * 1024;
     // this wave's group of 16 keys of step s (one that does not exist: some keys of the pool, that no row sees)
     auto page_of = [&](int s) { return kv16_entry(sq, (k0 + 64 * s + 16 * wave) >> shift); };
-    auto copy = [&](int s, int page) {
+    auto place = [&](int s, int page) {
         const int p = k0 + 64 * s + 16 * wave, at = p < k1 && (uint32_t)page < (uint32_t)a.pool.n_pages ? page : 0;
-        const char *src = uniform_ptr(base + ((uint64_t)(uint32_t)at * page_bytes + (p & in_page) * (2 * HD)));
-        const uint32_t to = lds0 + (uint32_t)(s & 1) * (W::buffer * 16);
-        dma_tiles<KS>(to, src, lane * 16);
-        dma_tiles<KS>(to + KS * 1024, src + block, lane * 16);
+        return uniform_ptr(base + ((uint64_t)(uint32_t)at * page_bytes + (p & in_page) * (2 * HD)));
     };
+    auto copy_k = [&](int s, int page) { dma_tiles<KS>(lds0 + (uint32_t)(s & 1) * (W::buffer * 16), place(s, page), lane * 16); };
+    auto copy_v = [&](int s, int page) { dma_tiles<KS>(lds0 + (uint32_t)(2 + (s & 1)) * (W::buffer * 16), place(s, page) + block, lane * 16); };
     if (threadIdx.x == 0) *spoilt = 0;      // (the first step's barrier lies before its first use)
-    int next = 0;
-    if (steps > 0) { copy(0, page_of(0)); next = page_of(1); }
-    kv16_row row[RT];
+    int page1 = 0, page2 = 0;                // of the steps one and two ahead
+    bool holes = false;                      // some page of the chunk does not exist
+    if (steps > 0) {
+        const int page0 = page_of(0);
+        page1 = page_of(1); page2 = page_of(2);
+        copy_k(0, page0); copy_v(0, page0); copy_k(1, page1);
+        int bad = 0;
+        for (int i = (k0 >> shift) + (int)threadIdx.x; i <= (k1 - 1) >> shift; i += 256) bad |= (uint32_t)sq.table[i] >= (uint32_t)a.pool.n_pages;
+        holes = __syncthreads_or(bad);
+    }
     uint4 q[RT][KS];
     kv16_acc<HD, RT> A;
     kv16_begin(A);
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-        row[t] = kv16_row_at(a, sq, kvh, m0 + (wave * RT + t) * 16 + jl);
-        kv16_load_q<HD>(a, row[t], g, q[t]);
+        kv16_load_q<HD>(a, kv16_row_at(a, sq, kvh, m0 + (wave * RT + t) * 16 + jl), g, q[t]);
     }
-    // q is here before the loop starts: a wait for it inside would also wait for the copies of the next step
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0);
-    asm volatile("" ::: "memory");
     auto sees = [&](int t, int p) {
-        return kv16_sees(a.mask == nullptr ? nullptr : a.mask + (size_t)row[t].row * a.words, a.words, p + 4 * g, len, len + row[t].j + 1, sq.rows, nk);
+        int l = lane;
+        asm volatile("" : "+v"(l));          // (what follows is made where it is needed: kept over the loop it would take the registers of the results)
+        const int at = kv16_row_at(a, sq, kvh, m0 + (wave * RT + t) * 16 + (l & 15)).j;
+        return kv16_sees(a.mask == nullptr ? nullptr : a.mask + (size_t)(sq.row0 + at) * a.words, a.words, p + 4 * (l >> 4), len, len + at + 1, sq.rows, nk);
     };
     auto missing = [&](int p0) {             // which of the step's groups do not exist
         int miss = 0;
         for (int i = 0; i < 4; ++i) miss |= (int)(p0 + 16 * i >= k1 || (uint32_t)kv16_entry(sq, (p0 + 16 * i) >> shift) >= (uint32_t)a.pool.n_pages) << i;
         return miss;
     };
-    for (int s = 0; s < steps; ++s) {
-        const int p0 = k0 + 64 * s;
-        const uint4 *L = wide_lds + (s & 1) * W::buffer + lane;
-        const int miss = missing(p0);
-        const bool edge = p0 + 64 > sure || miss != 0;
-        // step s has landed for every wave, and every wave is done with the other buffer
+    auto wait = [&]() {                      // this wave's copies have landed, its LDS reads are done, and so it is for every wave
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (edge) {                          // each wave looks through its group's values
-            uint4 *V = wide_lds + (s & 1) * W::buffer + (wave * 2 * KS + KS) * 64 + lane;
+    };
+    auto keys = [&](int s, int i, uint4 (&k)[KS]) {      // group i of step s
+        const uint4 *K = wide_lds + (s & 1) * W::buffer + lane;
+#pragma unroll
+        for (int b = 0; b < KS; ++b) k[b] = K[(i * KS + b) * 64];
+    };
+    auto scores = [&](const uint4 (&k)[KS], int i, f32x4 (&X)[RT][4]) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) X[t][i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int b = 0; b < KS; ++b)
+#pragma unroll
+            for (int t = 0; t < RT; ++t) X[t][i] = kv16_mfma<S>(k[b], q[t][b], X[t][i]);
+    };
+    auto is_edge = [&](int s) { return k0 + 64 * s + 64 > sure || holes; };
+    auto hide = [&](int s, f32x4 (&X)[RT][4]) {          // what rows do not see of step s
+        const int p0 = k0 + 64 * s, miss = missing(p0);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            const uint64_t w = sees(t, p0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) X[t][i][r] = ((w >> (16 * i + r)) & 1) && !((miss >> i) & 1) ? X[t][i][r] : -INFINITY;
+        }
+    };
+    kv16_tile T[RT];
+    auto step = [&](int s, f32x4 (&X)[RT][4], f32x4 (&next)[RT][4]) {
+        wait();                              // keys of step s + 1 and values of step s are there, and no wave reads the buffers that are filled next
+        if (s + 2 < steps) copy_k(s + 2, page2);
+        if (s + 1 < steps) copy_v(s + 1, page1);
+        page1 = page2; page2 = page_of(s + 3);
+        if (is_edge(s)) {                    // each wave looks through its group's values
+            uint4 *V = wide_lds + (2 + (s & 1)) * W::buffer + wave * KS * 64 + lane;
             uint32_t strange = 0;
 #pragma unroll
             for (int b = 0; b < KS; ++b) {
@@ -531,83 +586,205 @@ k_kv16_attn_wide(const kv16_attn_args a)
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
         }
-        if (s + 1 < steps) { copy(s + 1, next); next = page_of(s + 2); }
-        f32x4 X[RT][4];
+        // A step's work in twelve parts, in each of which the matrix cores and the vector ALU have about as much to do, LDS asked a part ahead: the scores of the next step beside the first half of the weights, the products with the
+        // first half of the values beside the second half of the weights, those with the second half beside the next maximum
+        uint2 P[RT][4];
+        float ps[RT], mx[RT];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) { ps[t] = 0.f; mx[t] = -INFINITY; }
+        uint4 k[2][KS], va[2][2];
+        // (8 bytes at a time, as an operand's registers lie: both halves in one load would have to be moved)
+        uint32_t half[2] = {lane * 2u, lane * 2u + 1};
+        asm volatile("" : "+v"(half[1]));
+        const uint2 *V = (const uint2 *)(wide_lds + (2 + (s & 1)) * W::buffer);
+        auto values = [&](int n, uint4 (&v)[2]) {            // features 32 (n % KS) ... of groups 2 (n / KS) and the next
+            const int u = n / KS, b = n % KS;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint2 x = V[(2 * u * KS + b) * 128 + half[h]], y = V[((2 * u + 1) * KS + b) * 128 + half[h]];
+                v[h] = make_uint4(x.x, x.y, y.x, y.y);
+            }
+        };
+        auto products = [&](int n, const uint4 (&v)[2]) {
+            const int u = n / KS, b = n % KS;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int t = 0; t < RT; ++t) A.O[t][2 * b + h] = kv16_mfma<S>(v[h], make_uint4(P[t][2 * u].x, P[t][2 * u].y, P[t][2 * u + 1].x, P[t][2 * u + 1].y), A.O[t][2 * b + h]);
+        };
+        auto weights = [&](int n, int half_of) {             // n of 2 RT: two groups of a tile
+            const int t = n >> 1, i = 2 * half_of + (n & 1);
+            P[t][i] = kv16_weights4<S>(X[t][i], a.scale2, T[t].c, ps[t]);
+        };
+        keys(s + 1, 0, k[0]);                // (behind the last step: of what the buffer holds, not used)
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-#pragma unroll
-            for (int t = 0; t < RT; ++t) X[t][i] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int b = 0; b < KS; ++b) {
-                const uint4 k = L[(i * 2 * KS + b) * 64];
-#pragma unroll
-                for (int t = 0; t < RT; ++t) X[t][i] = kv16_mfma<S>(k, q[t][b], X[t][i]);
-            }
+            if (i < 3) keys(s + 1, i + 1, k[(i + 1) & 1]); else values(0, va[0]);
+            __builtin_amdgcn_sched_barrier(0);
+            scores(k[i & 1], i, next);
+            if (i < 2 * RT) weights(i, 0);
             __builtin_amdgcn_sched_barrier(0);
         }
-        uint64_t there = ~0ull;
-        if (miss) {
+        if (s + 1 < steps && is_edge(s + 1)) hide(s + 1, next);
+        bool same = true;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) if ((miss >> i) & 1) there &= ~(0xffffull << (16 * i));
+        for (int t = 0; t < RT; ++t) same = same && T[t].keep == 1.f;
+        if (!__all(same)) {
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+#pragma unroll
+                for (int e = 0; e < HD / 16; ++e)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) A.O[t][e][r] *= T[t].keep;
         }
-        uint2 P[RT][4], PL[RT][4];
-        kv16_softmax<S>(A, X, a.scale2, edge, [&](int t) { return sees(t, p0) & there; }, P, PL);
-        kv16_output<S>(A, P, PL, [&](int i, int b) { return L[(i * 2 * KS + KS + b) * 64]; });
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int n = 0; n < 2 * KS; ++n) {
+            if (n + 1 < 2 * KS) values(n + 1, va[(n + 1) & 1]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (n < KS) {                    // (2 RT weights in KS parts)
+#pragma unroll
+                for (int w = n; w < 2 * RT; w += KS) weights(w, 1);
+            } else {
+#pragma unroll
+                for (int w = n - KS; w < 2 * RT; w += KS) mx[w >> 1] = kv16_maximum4(kv16_maximum4(mx[w >> 1], next[w >> 1][2 * (w & 1)]), next[w >> 1][2 * (w & 1) + 1]);
+            }
+            products(n, va[n & 1]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            T[t].l = fmaf(T[t].l, T[t].keep, ps[t]);
+            if (s + 1 < steps) kv16_under<S>(T[t], mx[t], a.scale2);
+        }
+    };
+    f32x4 X0[RT][4], X1[RT][4];
+    if (steps > 0) {
+        wait();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { uint4 k[KS]; keys(0, i, k); scores(k, i, X0); }
+        if (is_edge(0)) hide(0, X0);
+    }
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        T[t] = {-INFINITY, 0.f, 0.f, 0.f};
+        if (steps > 0) {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mx = kv16_maximum4(mx, X0[t][i]);
+            kv16_under<S>(T[t], mx, a.scale2);
+        }
+    }
+    for (int s = 0; s < steps; s += 2) {
+        step(s, X0, X1);
+        if (s + 1 < steps) step(s + 1, X1, X0);
     }
     if (steps > 0 && *spoilt != 0)           // (written ahead of a step's last barrier)
         kv16_put_strange<S, HD, RT>(A, k0, k1, 32,
-            [&](int p) { const int of = k0 + (p - k0) / 64 * 64; return of + 64 <= sure && missing(of) == 0; },      // (theirs went through the products)
+            [&](int p) { const int of = k0 + (p - k0) / 64 * 64; return of + 64 <= sure && !holes; },      // (theirs went through the products)
             [&](int t, int p) { return sees(t, p); },
             [&](int p, int i, int b) {
                 const int q = p + 16 * i, page = q < k1 ? kv16_entry(sq, q >> shift) : -1;
                 if ((uint32_t)page >= (uint32_t)a.pool.n_pages) return make_uint4(0u, 0u, 0u, 0u);
                 return ((const uint4 *)(base + ((uint64_t)(uint32_t)page * page_bytes + block + (q & in_page) * (2 * HD))))[b * 64 + lane];
             });
-    const float unit = __builtin_bit_cast(float, (127 - kv16_bias<S>()) << 23);
+    const float unit = __builtin_bit_cast(float, (127 - kv16_wide_bias<S>()) << 23);
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-        const float Z = with_lane32(with_lane16(A.l[t], op_add), op_add) * unit;
-        if (!row[t].live) continue;
+        const float Z = with_lane32(with_lane16(T[t].l, op_add), op_add) * unit;
+        int l = lane;
+        asm volatile("" : "+v"(l));          // (the row is found anew, not kept over the loop)
+        const kv16_row row = kv16_row_at(a, sq, kvh, m0 + (wave * RT + t) * 16 + (l & 15));
+        if (!row.live) continue;
 #pragma unroll
         for (int e = 0; e < HD / 16; ++e) {
             const float o[4] = {A.O[t][e][0] * unit, A.O[t][e][1] * unit, A.O[t][e][2] * unit, A.O[t][e][3] * unit};
-            kv16_finish4<S, HD>(a, row[t], e * 16 + 4 * g, o, A.m[t], Z, whole, split);
+            kv16_finish4<S, HD>(a, row, e * 16 + 4 * g, o, T[t].m, Z, whole, split);
         }
     }
 }
 
-// The chunks of a row's keys joined: WR waves a row and query head, four chunks of each 4 HD bytes on their way a thread; four waves where chunks are more than 16
-template <int HD, typename S, int WR>
-__global__ void __launch_bounds__(256)
-k_kv16_attn_merge(const kv16_attn_args a, int TR)
+// Chunks that a row and head have (0: written already, or no such row)
+__device__ inline int kv16_chunks(const kv16_attn_args &a, int row, int head, int TR)
 {
-    constexpr int TPC = HD / 4, NG = WR * (64 / TPC), FL = 4;
-    __shared__ float4 sh[4][TPC];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t id = WR == 4 ? blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
-    const int row = __builtin_amdgcn_readfirstlane((int)(id / a.n_q_heads)), head = __builtin_amdgcn_readfirstlane((int)(id % a.n_q_heads));
-    if (row >= a.seqs.n_rows) return;
-    const size_t at = (size_t)row * a.n_q_heads + head;
-    const float2 *ml = (const float2 *)(a.part_ml + at * a.nsplit * 2);
-    const int t = lane % TPC, cg = (WR == 4 ? wave * (64 / TPC) : 0) + lane / TPC;
-    const float *po = a.part_o + at * a.nsplit * HD + 4 * t;
-    // asked for beside the sequence's tables, whatever these turn out to say: the statistics of up to 64 chunks, and the first outputs
-    float2 one = ml[min(lane, a.nsplit - 1)];
-    float4 v[FL];
-#pragma unroll
-    for (int i = 0; i < FL; ++i) v[i] = *(const float4 *)(po + (size_t)min(cg + i * NG, a.nsplit - 1) * HD);
     const int rows[1] = {row};
     int s[1];
     kv16_seqs_of_rows(a.seqs.row_start, a.seqs.n_seq, rows, s);
     const int si = __builtin_amdgcn_readfirstlane(s[0]);
-    if (si >= a.seqs.n_seq) return;
+    if (si >= a.seqs.n_seq) return 0;
     const kv16_seq sq = kv16_seq_at(a.seqs, si);
     const int j = row - sq.row0;
-    if (j < 0 || j >= sq.rows) return;
+    if (j < 0 || j >= sq.rows) return 0;
     const int tile = (j * a.group + head % a.group) / TR, last = (min((tile + 1) * TR, sq.rows * a.group) - 1) / a.group;
     const int nk = kv16_keys(sq, a.pool.page_shift, last, a.mask != nullptr);
-    if (nk <= a.chunk) return;              // (written already)
-    const int n = (nk + a.chunk - 1) / a.chunk;
+    return nk <= a.chunk ? 0 : (nk + a.chunk - 1) / a.chunk;
+}
+
+// The chunks of a row's keys joined, up to 16 of them: HD / 4 lanes a row and head, all of its chunks on their way at once.  A wave's heads are of one row: asked for beside the sequence's tables, whatever these turn out to say
+template <int HD, typename S>
+__global__ void __launch_bounds__(256)
+k_kv16_attn_join(const kv16_attn_args a, int TR)
+{
+    constexpr int TPC = HD / 4, HW = 64 / TPC, FL = 8;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane % TPC;
+    const int per = (a.n_q_heads + HW - 1) / HW, id = blockIdx.x * 4 + wave, row = __builtin_amdgcn_readfirstlane(id / per), head0 = (id - row * per) * HW + lane / TPC;
+    if (row >= a.seqs.n_rows) return;
+    const int head = min(head0, a.n_q_heads - 1);
+    const size_t at = (size_t)row * a.n_q_heads + head;
+    const float *po = a.part_o + at * a.nsplit * HD + 4 * t;
+    float2 one = ((const float2 *)(a.part_ml + at * a.nsplit * 2))[min(lane % 16, a.nsplit - 1)];
+    float4 v[FL];
+#pragma unroll
+    for (int i = 0; i < FL; ++i) if (i < a.nsplit) v[i] = *(const float4 *)(po + (size_t)i * HD);
+    // (a wave's heads may lie in two tiles, of different numbers of chunks)
+    const int n0 = kv16_chunks(a, row, min((id - row * per) * HW, a.n_q_heads - 1), TR), n1 = kv16_chunks(a, row, min((id - row * per) * HW + HW - 1, a.n_q_heads - 1), TR);
+    int n = n0;
+    if (n0 != n1) for (int h = 0; h < HW; ++h) { const int m = kv16_chunks(a, row, min((id - row * per) * HW + h, a.n_q_heads - 1), TR); if (lane / TPC == h) n = m; }
+    if (lane % 16 >= n) one = make_float2(-INFINITY, 0.f);
+    const float M = with_rotated<8>(with_rotated<4>(with_rotated<2>(with_rotated<1>(one.x, op_max), op_max), op_max), op_max), ref = M == -INFINITY ? 0.f : M;
+    const float w = __builtin_amdgcn_exp2f(one.x - ref);
+    const float L = with_rotated<8>(with_rotated<4>(with_rotated<2>(with_rotated<1>(w * one.y, op_add), op_add), op_add), op_add);
+    float o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c0 = 0; c0 < 16; c0 += FL) {
+        if (c0 >= a.nsplit) break;
+        if (c0 > 0) {
+#pragma unroll
+            for (int i = 0; i < FL; ++i) if (c0 + i < a.nsplit) v[i] = *(const float4 *)(po + (size_t)(c0 + i) * HD);
+        }
+#pragma unroll
+        for (int i = 0; i < FL; ++i) {
+            const float wc = __shfl(w, (lane & ~15) + c0 + i, 64);
+            if (c0 + i < n) { o[0] = fmaf(wc, v[i].x, o[0]); o[1] = fmaf(wc, v[i].y, o[1]); o[2] = fmaf(wc, v[i].z, o[2]); o[3] = fmaf(wc, v[i].w, o[3]); }      // (others: anything)
+        }
+    }
+    if (n == 0 || head0 >= a.n_q_heads) return;
+    const float inv = L == 0.f ? 0.f : 1.f / L, y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+    kv16_store4<S>(a, row, head, 4 * t, y);
+    if (a.lse != nullptr && t == 0) a.lse[at] = L == 0.f ? -INFINITY : (M + __log2f(L)) * 0.69314718055994530942f;
+}
+
+// More than 16: four waves a row and head, four chunks of each 4 HD bytes on their way a thread
+template <int HD, typename S>
+__global__ void __launch_bounds__(256)
+k_kv16_attn_merge(const kv16_attn_args a, int TR)
+{
+    constexpr int TPC = HD / 4, NG = 4 * (64 / TPC), FL = 4;
+    __shared__ float4 sh[4][TPC];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int row = (int)(blockIdx.x / a.n_q_heads), head = (int)(blockIdx.x % a.n_q_heads);
+    const size_t at = (size_t)row * a.n_q_heads + head;
+    const float2 *ml = (const float2 *)(a.part_ml + at * a.nsplit * 2);
+    const int t = lane % TPC, cg = wave * (64 / TPC) + lane / TPC;
+    const float *po = a.part_o + at * a.nsplit * HD + 4 * t;
+    // asked for beside the sequence's tables: the statistics of up to 64 chunks, and the first outputs
+    float2 one = ml[min(lane, a.nsplit - 1)];
+    float4 v[FL];
+#pragma unroll
+    for (int i = 0; i < FL; ++i) v[i] = *(const float4 *)(po + (size_t)min(cg + i * NG, a.nsplit - 1) * HD);
+    const int n = kv16_chunks(a, row, head, TR);
+    if (n == 0) return;
     if (lane >= n) one = make_float2(-INFINITY, 0.f);
     float M = one.x, L = 0.f;
     for (int c = 64 + lane; c < n; c += 64) M = fmaxf(M, ml[c].x);
@@ -633,16 +810,12 @@ k_kv16_attn_merge(const kv16_attn_args a, int TR)
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) { o[i] = with_lane32(o[i], op_add); if (TPC <= 16) o[i] = with_lane16(o[i], op_add); }
-    if (WR == 4) {
-        if (lane < TPC) sh[wave][lane] = make_float4(o[0], o[1], o[2], o[3]);
-        __syncthreads();
-        if (wave != 0) return;
-        const float4 x = sh[0][t], y = sh[1][t], z = sh[2][t], w = sh[3][t];
-        o[0] = (x.x + y.x) + (z.x + w.x); o[1] = (x.y + y.y) + (z.y + w.y); o[2] = (x.z + y.z) + (z.z + w.z); o[3] = (x.w + y.w) + (z.w + w.w);
-    }
-    if (lane >= TPC) return;
-    const float inv = L == 0.f ? 0.f : 1.f / L, y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-    kv16_store4<S>(a, row, head, 4 * t, y);
+    if (lane < TPC) sh[wave][lane] = make_float4(o[0], o[1], o[2], o[3]);
+    __syncthreads();
+    if (wave != 0 || lane >= TPC) return;
+    const float4 x = sh[0][t], y = sh[1][t], z = sh[2][t], w = sh[3][t];
+    const float inv = L == 0.f ? 0.f : 1.f / L, r[4] = {((x.x + y.x) + (z.x + w.x)) * inv, ((x.y + y.y) + (z.y + w.y)) * inv, ((x.z + y.z) + (z.z + w.z)) * inv, ((x.w + y.w) + (z.w + w.w)) * inv};
+    kv16_store4<S>(a, row, head, 4 * t, r);
     if (a.lse != nullptr && lane == 0) a.lse[at] = L == 0.f ? -INFINITY : (M + __log2f(L)) * 0.69314718055994530942f;
 }
 
@@ -659,13 +832,27 @@ static kv16_plan plan(int n_seq, int n_rows, int group, int kv_heads, int hd, in
     const bool little = packed * kv_heads <= (1 << 26) / (keys > 0 ? keys : 1) && (packed <= (int64_t)32 * n_seq || keys * 4 * hd <= 2 << 20);
     p.tr = packed <= (int64_t)16 * n_seq || little ? 16 : packed <= (int64_t)64 * n_seq ? 64 : 128;
     p.units = (int)((packed + (int64_t)n_seq * (p.tr - 1)) / p.tr);
-    const int64_t tiles = packed / p.tr > n_seq ? packed / p.tr : n_seq, base = tiles * kv_heads, most = (keys + 255) / 256, want = p.tr == 16 && n_seq > 1 ? 1024 : 512;
-    int64_t n = (want + base - 1) / base;
-    n = n < most ? n : most;
-    n = n < 256 ? n : 256;
-    if (p.tr == 16 && most <= (base >= 256 ? 8 : packed <= (int64_t)16 * n_seq ? 4 : 3)) n = 1;
+    const int64_t tiles = packed / p.tr > n_seq ? packed / p.tr : n_seq, base = tiles * kv_heads, most = (keys + 255) / 256;
+    int64_t n, unit;
+    if (p.tr == 16) {
+        const int64_t want = n_seq > 1 ? 1024 : 512;
+        n = (want + base - 1) / base; unit = 256;
+        n = n < most ? n : most;
+        n = n < 256 ? n : 256;
+        if (most <= (base >= 256 ? 8 : packed <= (int64_t)16 * n_seq ? 4 : 3)) n = 1;
+    } else {
+        // by what each number of chunks would take, in steps of a workgroup that shares its CU with another (alone: 0.65)
+        const int64_t all = (int64_t)p.units * kv_heads, steps = (keys + 63) / 64;
+        double best = 0;
+        n = 1; unit = 64;
+        for (int64_t c = 1; c <= most && c <= 64; ++c) {
+            const int64_t w = all * c;
+            const double rounds = w <= 1024 ? (double)((w + 511) / 512) : w / 512.0 + 0.5, t = rounds * ((steps + c - 1) / c + 3) * (w <= 256 ? 0.65 : 1.0) + (c > 1 ? 2.0 + (double)packed * kv_heads * c * hd * 1e-6 : 0.0);
+            if (c == 1 || t < best) { best = t; n = c; }
+        }
+    }
     n = n > 1 ? n : 1;
-    p.chunk = (int)(((keys + n - 1) / n + 255) / 256 * 256);
+    p.chunk = (int)(((keys + n - 1) / n + unit - 1) / unit * unit);
     p.chunk = p.chunk > 256 ? p.chunk : 256;
     p.nsplit = (int)((keys + p.chunk - 1) / p.chunk);
     p.nsplit = p.nsplit > 1 ? p.nsplit : 1;
@@ -706,8 +893,8 @@ static int allow_lds()
     PV_HIP(hipGetDevice(&dev));
     const uint64_t bit = 1ull << (dev & 63);
     if (dev < 64 && (done.load(std::memory_order_acquire) & bit)) return PV_OK;
-    PV_HIP(hipFuncSetAttribute((const void *)k_kv16_attn_wide<HD, 1, S>, hipFuncAttributeMaxDynamicSharedMemorySize, kv16_wide<HD, 1>::lds));
-    PV_HIP(hipFuncSetAttribute((const void *)k_kv16_attn_wide<HD, 2, S>, hipFuncAttributeMaxDynamicSharedMemorySize, kv16_wide<HD, 2>::lds));
+    PV_HIP(hipFuncSetAttribute((const void *)k_kv16_attn_wide<HD, 1, S>, hipFuncAttributeMaxDynamicSharedMemorySize, kv16_wide<HD>::lds));
+    PV_HIP(hipFuncSetAttribute((const void *)k_kv16_attn_wide<HD, 2, S>, hipFuncAttributeMaxDynamicSharedMemorySize, kv16_wide<HD>::lds));
     if (dev < 64) done.fetch_or(bit, std::memory_order_release);
     return PV_OK;
 }
@@ -718,15 +905,17 @@ static int launch(const kv16_attn_args &a, const kv16_plan &p, hipStream_t s)
     const dim3 grid(p.units * a.pool.n_heads, p.nsplit);
     if (p.tr == 16) k_kv16_attn<HD, S><<<grid, 256, 0, s>>>(a);
     else {
-        if (kv16_wide<HD, 1>::lds > 65536) { const int rc = allow_lds<HD, S>(); if (rc != PV_OK) return rc; }
-        if (p.tr == 64) k_kv16_attn_wide<HD, 1, S><<<grid, 256, kv16_wide<HD, 1>::lds, s>>>(a);
-        else k_kv16_attn_wide<HD, 2, S><<<grid, 256, kv16_wide<HD, 2>::lds, s>>>(a);
+        if (kv16_wide<HD>::lds > 65536) { const int rc = allow_lds<HD, S>(); if (rc != PV_OK) return rc; }
+        if (p.tr == 64) k_kv16_attn_wide<HD, 1, S><<<grid, 256, kv16_wide<HD>::lds, s>>>(a);
+        else k_kv16_attn_wide<HD, 2, S><<<grid, 256, kv16_wide<HD>::lds, s>>>(a);
     }
     PV_HIP(hipGetLastError());
     if (p.nsplit == 1) return PV_OK;
-    const int64_t waves = (int64_t)a.seqs.n_rows * a.n_q_heads;
-    if (p.nsplit > 16) k_kv16_attn_merge<HD, S, 4><<<(unsigned)waves, 256, 0, s>>>(a, p.tr);
-    else k_kv16_attn_merge<HD, S, 1><<<(unsigned)((waves + 3) / 4), 256, 0, s>>>(a, p.tr);
+    if (p.nsplit > 16) k_kv16_attn_merge<HD, S><<<(unsigned)(a.seqs.n_rows * a.n_q_heads), 256, 0, s>>>(a, p.tr);
+    else {
+        const int per = (a.n_q_heads + 256 / HD - 1) / (256 / HD);
+        k_kv16_attn_join<HD, S><<<(unsigned)(((int64_t)a.seqs.n_rows * per + 3) / 4), 256, 0, s>>>(a, p.tr);
+    }
     PV_HIP(hipGetLastError());
     return PV_OK;
 }
