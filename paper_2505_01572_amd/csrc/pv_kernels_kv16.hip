@@ -6,7 +6,7 @@
 
 struct rot_args {
     const double *turns;                    // of a pair, per position
-    int units, interleaved;                 // units of 16 features that are rotated
+    int units, rest, interleaved;           // units of two pieces of 16 bytes that are rotated, and those that are not
     float amplitude;
     const int32_t *positions;               // of the rows; NULL: the tokens' own
 };
@@ -26,48 +26,80 @@ __device__ inline void rot_angle(int pos, double turns, float amplitude, float &
     c = amplitude * (((quarter + 1) & 2) ? -b : b);
 }
 
-// Unit u of 16 features of a head: two pieces of 8, as they pair up where the unit is rotated, else one behind the other
+// A thread's unit u of a row's heads: two pieces of 16 bytes, of PE numbers each, as far apart as the members of a pair are, so that neighbours read what lies side by side.  (Pairs of neighbours lie in one piece.)
+template <typename T> constexpr int rot_pe() { return 16 / (int)sizeof(T); }
 __device__ inline void rot_pieces(const rot_args &r, int u, int &p0, int &p1)
 {
-    if (u < r.units && !r.interleaved) { p0 = u; p1 = u + r.units; }
-    else { p0 = 2 * u; p1 = 2 * u + 1; }
+    p0 = u < r.units ? u : u + r.units;
+    p1 = p0 + (u < r.units ? r.units : r.rest);
 }
-__device__ inline void rot_turn(const rot_args &r, int u, const float c[8], const float s[8], float a[8], float b[8])
+template <int PE> __device__ inline void rot_turn(const rot_args &r, int u, const float (&c)[PE], const float (&s)[PE], float (&a)[PE], float (&b)[PE])
 {
     if (u >= r.units) return;
     if (r.interleaved) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < PE / 2; ++i) {
             const float x = a[2 * i], y = a[2 * i + 1], z = b[2 * i], w = b[2 * i + 1];
             a[2 * i] = x * c[i] - y * s[i]; a[2 * i + 1] = fmaf(x, s[i], y * c[i]);
-            b[2 * i] = z * c[i + 4] - w * s[i + 4]; b[2 * i + 1] = fmaf(z, s[i + 4], w * c[i + 4]);
+            b[2 * i] = z * c[PE / 2 + i] - w * s[PE / 2 + i]; b[2 * i + 1] = fmaf(z, s[PE / 2 + i], w * c[PE / 2 + i]);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { const float x = a[i], y = b[i]; a[i] = x * c[i] - y * s[i]; b[i] = fmaf(x, s[i], y * c[i]); }
+        for (int i = 0; i < PE; ++i) { const float x = a[i], y = b[i]; a[i] = x * c[i] - y * s[i]; b[i] = fmaf(x, s[i], y * c[i]); }
     }
 }
-__device__ inline void rot_angles(const rot_args &r, int u, int pos, float c[8], float s[8])
+template <int PE> __device__ inline void rot_angles(const rot_args &r, int u, int pos, float (&c)[PE], float (&s)[PE])
 {
     if (u >= r.units) return;
+    const int first = r.interleaved ? u * (PE / 2) : u * PE, second = r.interleaved ? (u + r.units) * (PE / 2) : first + PE / 2;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) rot_angle(pos, r.turns[8 * u + i], r.amplitude, c[i], s[i]);
+    for (int i = 0; i < PE; ++i) rot_angle(pos, r.turns[i < PE / 2 ? first + i : second + i - PE / 2], r.amplitude, c[i], s[i]);
 }
 
-// Rows of heads: a thread has a row and a unit of its features, and takes the heads slot, slot + slots, ...
-template <typename T>
-__device__ inline void rot_heads(const rot_args &r, const rot_rows &x, int64_t row, int u, const float c[8], const float s[8], int slot, int slots)
+// A piece's numbers in 32 bits, and back to memory
+template <typename T> __device__ inline void rot_numbers(u32x4 w, float (&v)[rot_pe<T>()])
 {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t d = w[i];
+        if constexpr (sizeof(T) == 4) v[i] = __uint_as_float(d);
+        else if constexpr (__is_same(T, __bf16)) { v[2 * i] = __uint_as_float(d << 16); v[2 * i + 1] = __uint_as_float(d & 0xffff0000u); }
+        else { const kv16_h2 h = __builtin_bit_cast(kv16_h2, d); v[2 * i] = (float)h.x; v[2 * i + 1] = (float)h.y; }
+    }
+}
+template <typename S, int PE> __device__ inline void rot_store(char *p, const float (&v)[PE])
+{
+    if constexpr (sizeof(S) == 4) *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]);
+    else if constexpr (PE == 4) *(uint2 *)p = make_uint2(kv16_two<S>(v[0], v[1]), kv16_two<S>(v[2], v[3]));
+    else *(uint4 *)p = make_uint4(kv16_two<S>(v[0], v[1]), kv16_two<S>(v[2], v[3]), kv16_two<S>(v[4], v[5]), kv16_two<S>(v[6], v[7]));
+}
+
+// Rows of heads: a thread has a row and a unit of its features, and takes the heads first, first + step, ..., four of them on their way at once (13312 rows of 64 heads of bf16, their keys and values: 143 us one at a time, 121
+// so).  f32 by pieces of 32 bytes, in which neighbours' accesses leave gaps: 8191 rows of 40 heads 87 us
+template <typename T>
+__device__ inline void rot_heads(const rot_args &r, const rot_rows &x, int64_t row, int u, const float (&c)[rot_pe<T>()], const float (&s)[rot_pe<T>()], int first, int step)
+{
+    constexpr int HB = 4;
     int p0, p1;
     rot_pieces(r, u, p0, p1);
-    constexpr int E = sizeof(T);
-    for (int h = slot; h < x.heads; h += slots) {
-        const char *src = x.src + row * x.src_row + h * x.src_head;
-        char *dst = x.dst + row * x.dst_row + h * x.dst_head;
-        float a[8], b[8];
-        kv16_load8<T>(src + p0 * 8 * E, a); kv16_load8<T>(src + p1 * 8 * E, b);
-        rot_turn(r, u, c, s, a, b);
-        kv16_store8<T>(dst + p0 * 8 * E, a); kv16_store8<T>(dst + p1 * 8 * E, b);
+    const char *src = x.src + row * x.src_row;
+    char *dst = x.dst + row * x.dst_row;
+    for (int h0 = first; h0 < x.heads; h0 += HB * step) {
+        u32x4 a[HB], b[HB];
+#pragma unroll
+        for (int i = 0; i < HB; ++i) {
+            const u32x4 *at = (const u32x4 *)(src + min(h0 + i * step, x.heads - 1) * x.src_head);
+            if (i == 0 || h0 + i * step < x.heads) { a[i] = at[p0]; b[i] = at[p1]; }
+        }
+#pragma unroll
+        for (int i = 0; i < HB; ++i) {
+            if (h0 + i * step >= x.heads) break;
+            float v[rot_pe<T>()], w[rot_pe<T>()];
+            rot_numbers<T>(a[i], v); rot_numbers<T>(b[i], w);
+            rot_turn(r, u, c, s, v, w);
+            char *to = dst + (h0 + i * step) * x.dst_head;
+            rot_store<T>(to + p0 * 16, v); rot_store<T>(to + p1 * 16, w);
+        }
     }
 }
 
@@ -79,7 +111,7 @@ k_rotate(const rot_args r, const rot_rows x, int n_rows, int head_units, int slo
     const int u = (int)(id % head_units), slot = (int)(id / head_units % slots);
     const int64_t row = id / head_units / slots;
     if (row >= n_rows) return;
-    float c[8], s[8];
+    float c[rot_pe<T>()], s[rot_pe<T>()];
     rot_angles(r, u, r.positions[row], c, s);
     rot_heads<T>(r, x, row, u, c, s, slot, slots);
 }
@@ -100,7 +132,7 @@ template <int HD, typename T, typename S>
 __global__ void __launch_bounds__(256)
 k_kv16_append(const kv16_append_args a)
 {
-    constexpr int U = HD / 16, E = sizeof(T), NS = 256 / (KV16_ROWS * U);
+    constexpr int PE = rot_pe<T>(), U = HD / (2 * PE), E = sizeof(T), NS = 256 / (KV16_ROWS * U);
     __shared__ kv16_place place[KV16_ROWS];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, first = blockIdx.y * KV16_ROWS;
     {
@@ -131,38 +163,45 @@ k_kv16_append(const kv16_append_args a)
     if (p.pos < 0) return;
     const int64_t row = first + r;
     const int in_page = p.pos & ((1 << a.pool.page_shift) - 1), sub = in_page >> 4, t = in_page & 15;
-    float c[8], s[8];
+    // queries' heads, keys', values', dealt out one after the other
+    auto begin = [&](int before) { const int b = (slot - before) % slots; return b < 0 ? b + slots : b; };
+    float c[PE], s[PE];
     rot_angles(a.rot, u, p.turn, c, s);
     rot_heads<T>(a.rot, a.q, row, u, c, s, slot, slots);
     if (p.page < 0) return;
     int p0, p1;
     rot_pieces(a.rot, u, p0, p1);
-    for (int h = slot; h < a.k.heads; h += slots) {
-        const char *src = a.k.src + row * a.k.src_row + h * a.k.src_head;
+    for (int h = begin(a.q.heads); h < a.k.heads; h += slots) {
+        const u32x4 *src = (const u32x4 *)(a.k.src + row * a.k.src_row + h * a.k.src_head);
         char *dst = a.pool.pages + kv16_block<HD>(a.pool, p.page, h, 0, sub);
-        float x[8], y[8];
-        kv16_load8<T>(src + p0 * 8 * E, x); kv16_load8<T>(src + p1 * 8 * E, y);
+        float x[PE], y[PE];
+        rot_numbers<T>(src[p0], x); rot_numbers<T>(src[p1], y);
         rot_turn(a.rot, u, c, s, x, y);
-        *(uint4 *)(dst + kv16_k_at(t, 8 * p0)) = kv16_pack8<S>(x); *(uint4 *)(dst + kv16_k_at(t, 8 * p1)) = kv16_pack8<S>(y);
+        rot_store<S>(dst + kv16_k_at(t, PE * p0), x); rot_store<S>(dst + kv16_k_at(t, PE * p1), y);
     }
     // values: four tokens lie side by side, and go together if they come together: with the first of them
     if ((t & 3) != 0 && !(p.left >> 30)) return;
-    const int n = min(4 - (t & 3), p.left & ((1 << 30) - 1)), f0 = 32 * (u >> 1) + 8 * (u & 1);
-    for (int h = slot; h < a.v.heads; h += slots) {
+    const int n = min(4 - (t & 3), p.left & ((1 << 30) - 1)), f0 = 32 * (u / (16 / PE)) + PE * (u % (16 / PE));
+    for (int h = begin(a.q.heads + a.k.heads); h < a.v.heads; h += slots) {
         const char *src = a.v.src + row * a.v.src_row + h * a.v.src_head;
         char *dst = a.pool.pages + kv16_block<HD>(a.pool, p.page, h, 1, sub);
-        float x[4][8], y[4][8];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) if (i < n) { kv16_load8<T>(src + i * a.v.src_row + f0 * E, x[i]); kv16_load8<T>(src + i * a.v.src_row + (f0 + 16) * E, y[i]); }
+        auto of = [&](int i, int f) { return *(const u32x4 *)(src + i * a.v.src_row + f * E); };
         if (n == 4) {
+            u32x4 x[4], y[4];
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                *(uint4 *)(dst + kv16_v_at(t, f0 + e)) = make_uint4(kv16_two<S>(x[0][e], x[1][e]), kv16_two<S>(x[2][e], x[3][e]), kv16_two<S>(y[0][e], y[1][e]), kv16_two<S>(y[2][e], y[3][e]));
+            for (int i = 0; i < 4; ++i) { x[i] = of(i, f0); y[i] = of(i, f0 + 16); }
+            auto two = [&](u32x4 l, u32x4 m, int e) {
+                if constexpr (__is_same(T, S)) return e & 1 ? l[e / 2] >> 16 | (m[e / 2] & 0xffff0000u) : (l[e / 2] & 0xffffu) | m[e / 2] << 16;
+                else { float v[PE], w[PE]; rot_numbers<T>(l, v); rot_numbers<T>(m, w); return kv16_two<S>(v[e], w[e]); }
+            };
+#pragma unroll
+            for (int e = 0; e < PE; ++e) *(uint4 *)(dst + kv16_v_at(t, f0 + e)) = make_uint4(two(x[0], x[1], e), two(x[2], x[3], e), two(y[0], y[1], e), two(y[2], y[3], e));
         } else {
+            for (int i = 0; i < n; ++i) {
+                float x[PE], y[PE];
+                rot_numbers<T>(of(i, f0), x); rot_numbers<T>(of(i, f0 + 16), y);
 #pragma unroll
-            for (int i = 0; i < 3; ++i) if (i < n) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) { *(S *)(dst + kv16_v_at(t + i, f0 + e)) = (S)x[i][e]; *(S *)(dst + kv16_v_at(t + i, f0 + 16 + e)) = (S)y[i][e]; }
+                for (int e = 0; e < PE; ++e) { *(S *)(dst + kv16_v_at(t + i, f0 + e)) = (S)x[e]; *(S *)(dst + kv16_v_at(t + i, f0 + 16 + e)) = (S)y[e]; }
             }
         }
     }
@@ -275,7 +314,13 @@ static int check_rotary(const pv_rotary *r, int head_dim)
     if (!(r->amplitude - r->amplitude == 0.f)) { pv_set_error("rotary: the amplitude is not finite"); return PV_EINVAL; }
     return PV_OK;
 }
-static rot_args rotary_of(const pv_rotary *r, const int32_t *positions) { return {r->turns, r->rotary_dim / 16, r->interleaved != 0, r->amplitude, positions}; }
+static int unit_of(int dtype) { return dtype == PV_F32 ? 8 : 16; }       // numbers a thread's unit has
+static rot_args rotary_of(const pv_rotary *r, const int32_t *positions, int head_dim, int dtype)
+{
+    const int n = unit_of(dtype);
+    if (r == nullptr) return {nullptr, 0, head_dim / n, 0, 1.f, nullptr};
+    return {r->turns, r->rotary_dim / n, (head_dim - r->rotary_dim) / n, r->interleaved != 0, r->amplitude, positions};
+}
 static rot_rows rows_of(const void *src, int64_t row, int64_t head, void *dst, int64_t dst_row, int64_t dst_head, int heads, int dtype)
 {
     const int64_t e = dtype == PV_F32 ? 4 : 2;
@@ -293,9 +338,9 @@ extern "C" int pv_rotate(const pv_rotary *rotary, const int32_t *positions, cons
     if (n_rows == 0 || n_heads == 0) return PV_OK;
     if (!positions || ((uintptr_t)positions & 3)) { pv_set_error("positions: null or not aligned"); return PV_EINVAL; }
     if ((rc = pv_kv8_check_rows("x", x, x_row_stride, x_head_stride, dtype)) != PV_OK || (rc = pv_kv8_check_rows("out", out, out_row_stride, out_head_stride, dtype)) != PV_OK) return rc;
-    const rot_args r = rotary_of(rotary, positions);
+    const rot_args r = rotary_of(rotary, positions, head_dim, dtype);
     const rot_rows rows = rows_of(x, x_row_stride, x_head_stride, out, out_row_stride, out_head_stride, n_heads, dtype);
-    const int units = head_dim / 16;
+    const int units = head_dim / unit_of(dtype);
     // heads are shared by as many threads as fill the chip
     const int64_t base = (int64_t)n_rows * units;
     int64_t slots = (524288 + base - 1) / base;
@@ -336,12 +381,12 @@ extern "C" int pv_kv16_append(const pv_kv16_pool *pool, const pv_kv8_seqs *seqs,
     if (q && ((rc = pv_kv8_check_rows("q", q, q_row_stride, q_head_stride, dtype)) != PV_OK || (rc = pv_kv8_check_rows("q_out", q_out, q_out_row_stride, q_out_head_stride, dtype)) != PV_OK)) return rc;
     kv16_append_args a = {};
     a.pool = pv_kv16_pool_args(pool); a.seqs = pv_kv16_seqs_args(seqs);
-    if (rotary) a.rot = rotary_of(rotary, positions);
+    a.rot = rotary_of(rotary, positions, pool->head_dim, dtype);
     a.k = rows_of(k, k_row_stride, k_head_stride, nullptr, 0, 0, pool->n_kv_heads, dtype);
     a.v = rows_of(v, v_row_stride, v_head_stride, nullptr, 0, 0, pool->n_kv_heads, dtype);
     a.q = rows_of(q, q_row_stride, q_head_stride, q_out, q_out_row_stride, q_out_head_stride, q ? n_q_heads : 0, dtype);
     // the heads of 16 rows are shared by as many workgroups as fill the chip
-    const int blocks = (seqs->n_rows + KV16_ROWS - 1) / KV16_ROWS, per = 256 / (KV16_ROWS * pool->head_dim / 16), heads = a.q.heads > pool->n_kv_heads ? a.q.heads : pool->n_kv_heads;
+    const int blocks = (seqs->n_rows + KV16_ROWS - 1) / KV16_ROWS, per = 256 / (KV16_ROWS * pool->head_dim / unit_of(dtype)), heads = a.q.heads + 2 * pool->n_kv_heads;
     int slots = (1024 + blocks - 1) / blocks;
     slots = slots < (heads + per - 1) / per ? slots : (heads + per - 1) / per;
     a.slots = slots > 1 ? slots : 1;
