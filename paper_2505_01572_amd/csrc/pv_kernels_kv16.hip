@@ -75,7 +75,7 @@ template <typename S, int PE> __device__ inline void rot_store(char *p, const fl
 }
 
 // Rows of heads: a thread has a row and a unit of its features, and takes the heads first, first + step, ..., four of them on their way at once (13312 rows of 64 heads of bf16, their keys and values: 143 us one at a time, 121
-// so).  f32 by pieces of 32 bytes, in which neighbours' accesses leave gaps: 8191 rows of 40 heads 87 us
+// so).  8191 rows of 40 heads of f32 in pieces of 32 bytes, between which neighbours' accesses leave gaps, 87 us, so 65 (a copy of as many bytes: 65)
 template <typename T>
 __device__ inline void rot_heads(const rot_args &r, const rot_rows &x, int64_t row, int u, const float (&c)[rot_pe<T>()], const float (&s)[rot_pe<T>()], int first, int step)
 {
@@ -213,21 +213,27 @@ struct kv16_keep_args {
     const int32_t *path, *accepted;
 };
 
-// A wave a sequence, head and kind: eight tokens of the path at a time are read, then written.  A path's numbers rise and none is less than its place, so what a later token comes from has not been
-// written to by then.
+// A wave a sequence, head and kind: 16 tokens of the path at a time are read, then written.  A path's numbers rise and none is less than its place, so what a later token comes from has not been
+// written to by then.  Bound by the trips to the tables, the path and the tokens, one behind the other.
+// (What a thread holds of them must not end up in LDS, where the compiler puts arrays that it cannot keep in registers: for its place there a kernel asks the launch's packet, in host memory, 17 us where 5 do.)
 template <int HD>
 __global__ void __launch_bounds__(64)
 k_kv16_keep(const kv16_keep_args a)
 {
-    constexpr int B = 8;
+    constexpr int B = 16, KL = HD / 8, VL = HD / 2;           // tokens at a time; lanes a token: 16 bytes of keys each; two values (features 16 apart, 8 bytes apart) each
+    __shared__ int64_t sh_from[64], sh_to[64];
     const int lane = threadIdx.x, which = blockIdx.x & 1, head = blockIdx.x >> 1, shift = a.pool.page_shift;
+    const int accepted = a.accepted[blockIdx.y];
     const kv16_seq q = kv16_seq_at(a.seqs, blockIdx.y);
-    const int n = (int)min((int64_t)a.accepted[blockIdx.y] + 1, (int64_t)q.rows);
-    auto place = [&](int local) -> int64_t {
+    const int n = (int)min((int64_t)accepted + 1, (int64_t)q.rows);
+    auto place = [&](int local) -> int64_t {                  // of the token's first key; of values: of its group of four's first 16 bytes, times 4, and its number in the group
         const int64_t pos = (int64_t)q.len + local;
-        const int page = pos < 0x7fffffff ? kv16_page(q, a.pool.n_pages, (int)pos >> shift) : -1, in_page = (int)pos & ((1 << shift) - 1);
-        return page < 0 ? -1 : (int64_t)kv16_block<HD>(a.pool, page, head, which, in_page >> 4) + (which ? kv16_v_at(in_page & 15, 0) : kv16_k_at(in_page & 15, 0));
+        const int page = pos < 0x7fffffff ? kv16_page(q, a.pool.n_pages, (int)pos >> shift) : -1, in_page = (int)pos & ((1 << shift) - 1), t = in_page & 15;
+        if (page < 0) return -1;
+        const int64_t block = (int64_t)kv16_block<HD>(a.pool, page, head, which, in_page >> 4);
+        return which ? (block + kv16_v_at(t & ~3, 0)) * 4 + (t & 3) : block + kv16_k_at(t, 0);
     };
+    char *pages = a.pool.pages;
     for (int d0 = 0; d0 < n; d0 += 64) {
         int64_t from = -1, to = -1;
         if (d0 + lane < n) {
@@ -236,38 +242,43 @@ k_kv16_keep(const kv16_keep_args a)
         }
         if (to < 0) from = -1;
         const uint64_t moves = __ballot(from >= 0);
+        sh_from[lane] = from; sh_to[lane] = to;
+        __syncthreads();
         for (int b = 0; b < 64; b += B) {
             if (((moves >> b) & ((1 << B) - 1)) == 0) continue;
             if (which == 0) {
-                uint4 x[B * HD / 512];
+                constexpr int N = B * KL / 64;
+                u32x4 x[N];
 #pragma unroll
-                for (int i = 0; i < B * HD / 512; ++i) {
-                    const int id = i * 64 + lane, t = b + id / (HD / 8), p = id % (HD / 8);
-                    const int64_t f = __shfl((long long)from, t, 64);
-                    if (f >= 0) x[i] = *(const uint4 *)(a.pool.pages + f + kv16_k_at(0, 8 * p));
-                }
+                for (int i = 0; i < N; ++i) x[i] = *(const u32x4 *)(pages + max(sh_from[b + (i * 64 + lane) / KL], (int64_t)0) + lane % KL * 256);      // (of a token that does not move: some of the pool)
 #pragma unroll
-                for (int i = 0; i < B * HD / 512; ++i) {
-                    const int id = i * 64 + lane, t = b + id / (HD / 8), p = id % (HD / 8);
-                    const int64_t f = __shfl((long long)from, t, 64), o = __shfl((long long)to, t, 64);
-                    if (f >= 0) *(uint4 *)(a.pool.pages + o + kv16_k_at(0, 8 * p)) = x[i];
+                for (int i = 0; i < N; ++i) {
+                    const int t = b + (i * 64 + lane) / KL;
+                    if (sh_from[t] >= 0) *(u32x4 *)(pages + sh_to[t] + lane % KL * 256) = x[i];
                 }
             } else {
-                uint16_t x[B * HD / 64];
+                constexpr int N = B * VL / 64;
+                const int at = lane % VL / 16 * 1024 + lane % 16 * 16;
+                uint32_t x[N];
 #pragma unroll
-                for (int i = 0; i < B * HD / 64; ++i) {
-                    const int id = i * 64 + lane, t = b + id / HD, e = id % HD;
-                    const int64_t f = __shfl((long long)from, t, 64);
-                    if (f >= 0) x[i] = *(const uint16_t *)(a.pool.pages + f + kv16_v_at(0, e));
+                for (int i = 0; i < N; ++i) {
+                    const int64_t f = max(sh_from[b + (i * 64 + lane) / VL], (int64_t)0);
+                    const u32x4 v = *(const u32x4 *)(pages + f / 4 + at);      // values of features f and f + 16 of four tokens
+                    const int r = (int)(f & 3) * 16;
+                    x[i] = ((uint32_t)(((uint64_t)v.y << 32 | v.x) >> r) & 0xffffu) | (uint32_t)(((uint64_t)v.w << 32 | v.z) >> r) << 16;
                 }
 #pragma unroll
-                for (int i = 0; i < B * HD / 64; ++i) {
-                    const int id = i * 64 + lane, t = b + id / HD, e = id % HD;
-                    const int64_t f = __shfl((long long)from, t, 64), o = __shfl((long long)to, t, 64);
-                    if (f >= 0) *(uint16_t *)(a.pool.pages + o + kv16_v_at(0, e)) = x[i];
+                for (int i = 0; i < N; ++i) {
+                    const int t = b + (i * 64 + lane) / VL;
+                    if (sh_from[t] >= 0) {
+                        const int64_t o = sh_to[t];
+                        uint16_t *to2 = (uint16_t *)(pages + o / 4 + at) + (o & 3);
+                        to2[0] = (uint16_t)x[i]; to2[4] = (uint16_t)(x[i] >> 16);
+                    }
                 }
             }
         }
+        __syncthreads();
     }
 }
 
@@ -385,9 +396,9 @@ extern "C" int pv_kv16_append(const pv_kv16_pool *pool, const pv_kv8_seqs *seqs,
     a.k = rows_of(k, k_row_stride, k_head_stride, nullptr, 0, 0, pool->n_kv_heads, dtype);
     a.v = rows_of(v, v_row_stride, v_head_stride, nullptr, 0, 0, pool->n_kv_heads, dtype);
     a.q = rows_of(q, q_row_stride, q_head_stride, q_out, q_out_row_stride, q_out_head_stride, q ? n_q_heads : 0, dtype);
-    // the heads of 16 rows are shared by as many workgroups as fill the chip
+    // the heads of 16 rows are shared by as many workgroups as fill the chip several times over (13312 rows of 64 heads, their keys and values: 1024 workgroups 123 us, 2048 117, 4096 111)
     const int blocks = (seqs->n_rows + KV16_ROWS - 1) / KV16_ROWS, per = 256 / (KV16_ROWS * pool->head_dim / unit_of(dtype)), heads = a.q.heads + 2 * pool->n_kv_heads;
-    int slots = (1024 + blocks - 1) / blocks;
+    int slots = (4096 + blocks - 1) / blocks;
     slots = slots < (heads + per - 1) / per ? slots : (heads + per - 1) / per;
     a.slots = slots > 1 ? slots : 1;
     hipStream_t s = (hipStream_t)hip_stream;
