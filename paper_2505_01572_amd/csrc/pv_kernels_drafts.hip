@@ -240,17 +240,24 @@ k_draft_rows(const dv_args a)
 
 // A row's segments joined, by each GL lanes side by side: largest logit, sum of exponentials, the lowest id of the largest.  Four segments a lane stay in registers between the two passes.
 struct dv_row { double sum; float top; int first; bool any; };      // any: it has probabilities (its largest logit is a number)
-template <int GL> __device__ inline dv_row dv_row_of(const dv_args &a, int row, double cold)
+struct dv_parts { dv_part q[4]; };
+template <int GL> __device__ inline dv_parts dv_parts_of(const dv_args &a, int row)
+{
+    const int l = threadIdx.x % GL;
+    const dv_part *p = a.part + (int64_t)row * a.segs;
+    dv_parts r;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) { r.q[k] = {0.0, -INFINITY, 0x7fffffff}; if (l + k * GL < a.segs) r.q[k] = p[l + k * GL]; }
+    return r;
+}
+template <int GL> __device__ inline dv_row dv_row_of(const dv_args &a, int row, double cold, const dv_parts &parts)
 {
     constexpr int K = 4;
     const int l = threadIdx.x % GL;
     const dv_part *p = a.part + (int64_t)row * a.segs;
-    dv_part q[K];
     dv_row r = {0.0, -INFINITY, 0x7fffffff, false};
 #pragma unroll
-    for (int k = 0; k < K; ++k) { q[k] = {0.0, -INFINITY, 0x7fffffff}; if (l + k * GL < a.segs) q[k] = p[l + k * GL]; }
-#pragma unroll
-    for (int k = 0; k < K; ++k) r.top = fmaxf(r.top, q[k].top);
+    for (int k = 0; k < K; ++k) r.top = fmaxf(r.top, parts.q[k].top);
     for (int i = l + K * GL; i < a.segs; i += GL) r.top = fmaxf(r.top, p[i].top);
     r.top = with_rotated<8>(with_rotated<4>(with_rotated<2>(with_rotated<1>(r.top, op_max), op_max), op_max), op_max);
     if (GL == 64) r.top = with_lane32(with_lane16(r.top, op_max), op_max);
@@ -260,7 +267,7 @@ template <int GL> __device__ inline dv_row dv_row_of(const dv_args &a, int row, 
         else if (v.top == r.top) r.first = min(r.first, v.first);
     };
 #pragma unroll
-    for (int k = 0; k < K; ++k) if (k * GL < a.segs) add(q[k]);
+    for (int k = 0; k < K; ++k) if (k * GL < a.segs) add(parts.q[k]);
     for (int i = l + K * GL; i < a.segs; i += GL) add(p[i]);
     if (cold > 0.0) r.sum = GL == 64 ? dv_over_wave(r.sum) : dv_over_16(r.sum);
     else {
@@ -287,10 +294,13 @@ template <typename T> __device__ inline int2 dv_chain(const dv_args &a, const dv
     __syncthreads();
     const int n = blockDim.x / GL;
     for (int j0 = 1; j0 < q.rows; j0 += n) {             // (uniform: lanes without a draft look at the last one)
-        const int j = min(j0 + (int)threadIdx.x / GL, q.rows - 1), row = q.row0 + j, token = a.tokens[row], safe = min(max(token, 0), a.vocab - 1);
+        const int j = min(j0 + (int)threadIdx.x / GL, q.rows - 1), row = q.row0 + j, token = a.tokens[row];
+        const double u = dv_u(a, row, 0);
+        const dv_parts parts = dv_parts_of<GL>(a, row - 1);          // (on their way while the token comes, and what depends on it)
+        const int safe = min(max(token, 0), a.vocab - 1);
         const float x = dv_one<T>(a.logits + (int64_t)(row - 1) * a.row_bytes, safe);
-        const double u = dv_u(a, row, 0), d = a.probs == nullptr ? 1.0 : safe == token ? (double)a.probs[(int64_t)row * a.probs_row + safe] : 0.0;
-        const dv_row r = dv_row_of<GL>(a, row - 1, cold);
+        const double d = a.probs == nullptr ? 1.0 : safe == token ? (double)a.probs[(int64_t)row * a.probs_row + safe] : 0.0;
+        const dv_row r = dv_row_of<GL>(a, row - 1, cold, parts);
         const double p = dv_prob(a, r, x, token, cold);
         if (threadIdx.x % GL == 0) {
             if (!(u * d < p)) atomicMin(&sh->refused, j);
@@ -331,7 +341,7 @@ k_draft_walk(const dv_args a)
             const bool good = up >= 0 && up < n0 + i;
             const int over = q.row0 + (good ? up : 0);
             const float x = dv_one<T>(a.logits + (int64_t)over * a.row_bytes, safe);
-            const dv_row r = dv_row_of<GL>(a, over, cold);
+            const dv_row r = dv_row_of<GL>(a, over, cold, dv_parts_of<GL>(a, over));
             const double p = good ? dv_prob(a, r, x, token, cold) : 0.0;
             if (tid % GL == 0) { sh_p[i] = p; sh_u[i] = u; sh_parent[i] = good ? up : -1; sh_token[i] = token; a.out_probs[row] = (float)p; }
         }
@@ -422,15 +432,15 @@ k_draft_rest(const dv_args a)
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int s = blockIdx.x / a.left, seg = blockIdx.x - s * a.left;
     const dv_seq q = dv_seq_at(a, s);
-    if (q.rows == 0) return;
     const double cold = dv_cold(a, s);
+    if (q.rows == 0) return;
     const int2 w = a.parent != nullptr ? a.walk[s] : dv_chain<T>(a, q, cold, seg == 0, &sh_chain);
     if (a.parent == nullptr && seg == 0) {
         if (tid == 0) { a.walk[s] = w; a.accepted[s] = w.x - q.row0; a.out_probs[q.row0] = 1.f; }
         if (a.path != nullptr) for (int i = tid; i <= w.x - q.row0; i += NT) a.path[q.row0 + i] = i;
     }
     if (cold == 0.0) return;
-    const dv_row r = w.y ? sh_chain.row : dv_row_of<64>(a, w.x, cold);
+    const dv_row r = w.y ? sh_chain.row : dv_row_of<64>(a, w.x, cold, dv_parts_of<64>(a, w.x));
     const char *src = a.logits + (int64_t)w.x * a.row_bytes;
     const float *drafter = w.y && a.probs != nullptr ? a.probs + (int64_t)(w.x + 1) * a.probs_row : nullptr;
     const int head = dv_head<T>(src), base = head + seg * DV_SIZE, begin = dv_begin(seg, head, DV_SIZE), end = min(base + DV_SIZE, a.vocab);
@@ -467,11 +477,13 @@ k_draft_pick(const dv_args a)
     const double2 *rest = a.rest + (int64_t)s * a.left;
     double2 first[1];
     first[0] = lane < a.left ? rest[lane] : make_double2(0.0, 0.0);      // (T = 0: anything)
+    const double cold = dv_cold(a, s);
     if (q.rows == 0) { if (tid == 0) { a.accepted[s] = 0; a.next[s] = -1; } return; }
-    const double cold = dv_cold(a, s), u = dv_u(a, w.x, 1);
+    const dv_parts parts = dv_parts_of<64>(a, w.x);
+    const double u = dv_u(a, w.x, 1);
     const char *src = a.logits + (int64_t)w.x * a.row_bytes;
     const int head = dv_head<T>(src);
-    const dv_row r = dv_row_of<64>(a, w.x, cold);
+    const dv_row r = dv_row_of<64>(a, w.x, cold, parts);
     if (tid == 0) sh_id = -1;
     if (!r.any) { if (tid == 0) a.next[s] = -1; return; }
     if (cold == 0.0) { if (tid == 0) a.next[s] = r.first; return; }      // (with a refused draft too: it was another token)

@@ -577,9 +577,13 @@ def verify_drafts(row_start, logits, tokens, u, draft_probs=None, parent=None, t
         if len(_drafts_need) > 256:
             _drafts_need.clear()
         need = _drafts_need[key] = b.value
-    accepted, following = logits.new_empty((2, n), dtype=torch.int32).unbind(0)
-    path = None if parent is None else logits.new_empty(rows, dtype=torch.int32)
-    probs = logits.new_empty(rows, dtype=torch.float32)
+    # (one allocation for all that is returned)
+    if parent is None:
+        accepted, following, probs = logits.new_empty(2 * n + rows, dtype=torch.int32).split((n, n, rows))
+        path = None
+    else:
+        accepted, following, probs, path = logits.new_empty(2 * n + 2 * rows, dtype=torch.int32).split((n, n, rows, rows))
+    probs = probs.view(torch.float32)
     ws = logits.new_empty(need, dtype=torch.uint8) if need else None
     rc = L.pv_verify_drafts(start, n, logits.data_ptr(), row_stride, _DTYPES[logits.dtype], rows, vocab, tp, u.data_ptr(), u.dtype == torch.float64, qp, qr, pp, hp, hot,
                             accepted.data_ptr(), following.data_ptr(), None if path is None else path.data_ptr(), probs.data_ptr(), None if ws is None else ws.data_ptr(), need, _raw_stream(index))
