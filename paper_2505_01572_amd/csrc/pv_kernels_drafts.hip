@@ -159,7 +159,7 @@ __device__ inline int dv_begin(int seg, int head, int size) { return seg == 0 ? 
 
 // The rows' sums, WIDE: in 64 bits.  Those are bound by the exponentials: some 22 instruction slots a logit, 16 of them in 64 bits; the others by the read of the logits.
 template <typename T, int E, bool WIDE>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WIDE ? 4 : 8)))
 k_draft_rows(const dv_args a)
 {
     constexpr int NT = 256, V = 16 / (int)sizeof(T), U = E / V, D = E * (int)sizeof(T) / 4, SIZE = NT * E;
@@ -216,7 +216,14 @@ k_draft_rows(const dv_args a)
             const float c = (float)fmin(cold, 1e30);
             float even = 0.f, odd = 0.f;
 #pragma unroll
-            for (int i = 0; i < E; ++i) { const float w = __builtin_amdgcn_exp2f(fmaxf((dv_get<T>(x, i) - top) * c, -256.f)); if (i & 1) odd += w; else even += w; }      // (2^-256 is 0; of NaN and a number the number)
+            for (int i = 0; i < E; ++i) { const float w = __builtin_amdgcn_exp2f((dv_get<T>(x, i) - top) * c); if (i & 1) odd += w; else even += w; }
+            if (__any(!(even + odd < INFINITY))) {            // NaN among them (or -infinity at an infinite T): once more, with care
+                even = odd = 0.f;
+#pragma unroll
+                for (int d = 0; d < D; ++d) if (sizeof(T) == 2) asm volatile("" : "+v"(x[d]));
+#pragma unroll
+                for (int i = 0; i < E; ++i) { even += __builtin_amdgcn_exp2f(fmaxf((dv_get<T>(x, i) - top) * c, -256.f)); asm volatile("" : "+v"(even)); }      // (2^-256 is 0; of NaN and a number the number; one after the other: no registers for more)
+            }
             even += __builtin_amdgcn_exp2f(fmaxf((x0 - top) * c, -256.f));
             sum = dv_over_wave((double)even + (double)odd);
         }
