@@ -120,12 +120,12 @@ template <int HD, int RT> __device__ inline void kv16_begin(kv16_acc<HD, RT> &A)
 
 // Which of 64 keys from p on a row sees: without a mask those before `end`; with one those before len, and the slots from there on that its bits name, of the first `slots`; all before nk.  Bit i: key p + i.
 __device__ inline uint64_t kv16_first(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; }
-__device__ inline uint64_t kv16_sees(const uint64_t *mask, int words, int p, int len, int end, int slots, int nk)
+template <typename WORD> __device__ inline uint64_t kv16_sees(bool masked, WORD word, int words, int p, int len, int end, int slots, int nk)       // word(i): word i of the row's mask
 {
     uint64_t w = kv16_first(min(end, nk) - p);
-    if (mask != nullptr) {
+    if (masked) {
         const int s = p - len, i = max(s, 0) >> 6, sh = s & 63;          // slot of the first key
-        const uint64_t lo = mask[min(i, words - 1)], hi = mask[min(i + 1, words - 1)];       // (loads without branches)
+        const uint64_t lo = word(min(i, words - 1)), hi = word(min(i + 1, words - 1));       // (loads without branches)
         const uint64_t l = i < words ? lo : 0ull, h = s >= 0 && sh != 0 && i + 1 < words ? hi << (64 - sh) : 0ull;
         w = s <= -64 ? ~0ull : s < 0 ? kv16_first(-s) | l << -s : l >> sh | h;
         w &= kv16_first(slots - s);
@@ -353,7 +353,7 @@ k_kv16_attn(const kv16_attn_args a)
     asm volatile("" ::: "memory");
     load_k(p0);
     load_v();
-    auto sees = [&](int p) { return kv16_sees(mrow, a.words, p + 4 * g, len, len + row.j + 1, sq.rows, nk); };
+    auto sees = [&](int p) { return kv16_sees(mrow != nullptr, [&](int i) { return mrow[i]; }, a.words, p + 4 * g, len, len + row.j + 1, sq.rows, nk); };
     bool spoilt = false;                    // numbers that are not finite among values that not every row sees
     if (p0 < k1) pages(p0 + 4 * STEP, ahead);
     while (p0 < k1) {
@@ -443,7 +443,8 @@ template <int HD>
 struct kv16_wide {
     static constexpr int KS = HD / 32;
     static constexpr int buffer = 4 * KS * 64;                           // uint4 of 64 keys' K or V: [group][b][lane]
-    static constexpr int lds = 4 * buffer * 16 + 16;                     // two of K, two of V, and whether numbers that are not finite were among values that not every row sees
+    static constexpr int masks = 1024;                                   // words of masks that there is room for
+    static constexpr int lds = 4 * buffer * 16 + 16 + masks * 8;         // two of K, two of V, whether numbers that are not finite were among values that not every row sees, masks of the tile's tokens
 };
 
 __device__ inline float kv16_maximum(float a, float b) { return __builtin_elementwise_maximum(a, b); }      // (NaN if either is)
@@ -479,6 +480,7 @@ k_kv16_attn_wide(const kv16_attn_args a)
     constexpr int KS = W::KS, TR = 64 * RT;
     extern __shared__ uint4 wide_lds[];
     int *spoilt = (int *)(wide_lds + 4 * W::buffer);
+    uint64_t *masks = (uint64_t *)(wide_lds + 4 * W::buffer + 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, jl = lane & 15, g = lane >> 4;
     const int kvh = blockIdx.x % a.pool.n_heads, split = blockIdx.y, units = gridDim.x / a.pool.n_heads;
     int tile = 0;
@@ -492,7 +494,8 @@ k_kv16_attn_wide(const kv16_attn_args a)
     if (k0 >= nk && split > 0) return;
     const bool whole = nk <= a.chunk;
     const int sure = min(nk, a.mask != nullptr ? len : len + m0 / a.group + 1);     // keys before this one are seen by every row
-    const int steps = (k1 - k0 + 63) >> 6;
+    const int steps = (k1 - k0 + 63) >> 6, j0 = m0 / a.group;
+    const bool near = a.mask != nullptr && k1 > sure && (int64_t)(last - j0 + 1) * a.words <= W::masks;
 
     const uint32_t block = (uint32_t)(2 * HD) << shift, in_page = (1u << shift) - 1;
     const uint64_t page_bytes = (uint64_t)2 * block * a.pool.n_heads;
@@ -515,6 +518,8 @@ k_kv16_attn_wide(const kv16_attn_args a)
         copy_k(0, page0); copy_v(0, page0); copy_k(1, page1);
         int bad = 0;
         for (int i = (k0 >> shift) + (int)threadIdx.x; i <= (k1 - 1) >> shift; i += 256) bad |= (uint32_t)sq.table[i] >= (uint32_t)a.pool.n_pages;
+        // masks that steps of this chunk will ask for (read from memory there, they held up a step by some 2 us)
+        if (near) for (int i = threadIdx.x; i < (last - j0 + 1) * a.words; i += 256) masks[i] = a.mask[(size_t)(sq.row0 + j0) * a.words + i];
         holes = __syncthreads_or(bad);
     }
     uint4 q[RT][KS];
@@ -528,11 +533,13 @@ k_kv16_attn_wide(const kv16_attn_args a)
         int l = lane;
         asm volatile("" : "+v"(l));          // (what follows is made where it is needed: kept over the loop it would take the registers of the results)
         const int at = kv16_row_at(a, sq, kvh, m0 + (wave * RT + t) * 16 + (l & 15)).j;
-        return kv16_sees(a.mask == nullptr ? nullptr : a.mask + (size_t)(sq.row0 + at) * a.words, a.words, p + 4 * (l >> 4), len, len + at + 1, sq.rows, nk);
+        if (near) return kv16_sees(true, [&](int i) { return masks[(at - j0) * a.words + i]; }, a.words, p + 4 * (l >> 4), len, 0, sq.rows, nk);
+        return kv16_sees(a.mask != nullptr, [&](int i) { return a.mask[(size_t)(sq.row0 + at) * a.words + i]; }, a.words, p + 4 * (l >> 4), len, len + at + 1, sq.rows, nk);
     };
     auto missing = [&](int p0) {             // which of the step's groups do not exist
         int miss = 0;
-        for (int i = 0; i < 4; ++i) miss |= (int)(p0 + 16 * i >= k1 || (uint32_t)kv16_entry(sq, (p0 + 16 * i) >> shift) >= (uint32_t)a.pool.n_pages) << i;
+        for (int i = 0; i < 4; ++i) miss |= (int)(p0 + 16 * i >= k1) << i;
+        if (holes) for (int i = 0; i < 4; ++i) miss |= (int)((uint32_t)kv16_entry(sq, (p0 + 16 * i) >> shift) >= (uint32_t)a.pool.n_pages) << i;
         return miss;
     };
     auto wait = [&]() {                      // this wave's copies have landed, its LDS reads are done, and so it is for every wave
@@ -821,16 +828,22 @@ k_kv16_attn_merge(const kv16_attn_args a, int TR)
 
 // ------------------------------- host side ----------------------------------------
 
-// How a call's work is cut.  Rows a tile: 16, straight from memory, where sequences have no more (in the mean: what each has is on the device), else 64 or 128 through LDS.
-// Chunks of keys until there are two workgroups a CU, or twice as many where sequences of different lengths come out at different times.  Few keys are one workgroup's, which saves the launch that joins.
+// How a call's work is cut, from what the host knows: its rows (sequences are taken to have as many each), and how far the tables reach.
+// Rows a tile: 16, straight from memory, where sequences have no more, and where the whole work is small, so that what the other kernel pays for going through LDS weighs more than keys read again for every 16 rows.  Else 64, or
+// 128 where a sequence has much to do.  Eight kv heads of 128, one sequence, packed rows x keys, us from a graph with 16, 64, 128: 64 x 4000 14.5, 15.5, 18.0; 256 x 1000 13.3, 16.2, 20.2; 256 x 4000 22.9, 23.2, 25.7; 32 x 60000 58.9,
+// 47.4, 49.2; 64 x 16000 29.1, 21.9, 25.8; 512 x 4000 33.9, 31.5, 33.4; 256 x 16000 67.4, 39.4, 39.5; 1024 x 4000 51.1, 41.2, 39.9; 256 x 60000 283, 104, 89.  16 sequences of up to 4000 keys, 16, 32, 128 rows each 34.4, 38.2, 44.6;
+// 46.9, 34.1, 49.9; 84.7, 72.0, 80.8.
+// Chunks of keys, 16 rows a tile: until there are two workgroups a CU, or four where sequences of different lengths come out at different times; few keys are one workgroup's, which saves the launch that joins.  More rows: as
+// many as would take least by a count of steps (of 64 keys; three more for a workgroup's begin and end; two workgroups of a CU share it, one alone takes 0.65 as long) and of what the join has to move (one sequence of 1600 rows over
+// 4301 keys 82 us with six chunks, in two rounds of workgroups, 68 with four, in one).
 struct kv16_plan { int tr, units, nsplit, chunk; };
 
 static kv16_plan plan(int n_seq, int n_rows, int group, int kv_heads, int hd, int64_t keys)
 {
     kv16_plan p;
     const int64_t packed = (int64_t)n_rows * group;
-    const bool little = packed * kv_heads <= (1 << 26) / (keys > 0 ? keys : 1) && (packed <= (int64_t)32 * n_seq || keys * 4 * hd <= 2 << 20);
-    p.tr = packed <= (int64_t)16 * n_seq || little ? 16 : packed <= (int64_t)64 * n_seq ? 64 : 128;
+    const bool little = packed * kv_heads <= (7 << 20) / (keys > 0 ? keys : 1);
+    p.tr = packed <= (int64_t)16 * n_seq || little ? 16 : packed <= (int64_t)64 * n_seq || packed / n_seq <= (2 << 20) / (keys > 0 ? keys : 1) ? 64 : 128;
     p.units = (int)((packed + (int64_t)n_seq * (p.tr - 1)) / p.tr);
     const int64_t tiles = packed / p.tr > n_seq ? packed / p.tr : n_seq, base = tiles * kv_heads, most = (keys + 255) / 256;
     int64_t n, unit;
@@ -842,7 +855,7 @@ static kv16_plan plan(int n_seq, int n_rows, int group, int kv_heads, int hd, in
         if (most <= (base >= 256 ? 8 : packed <= (int64_t)16 * n_seq ? 4 : 3)) n = 1;
     } else {
         // by what each number of chunks would take, in steps of a workgroup that shares its CU with another (alone: 0.65)
-        const int64_t all = (int64_t)p.units * kv_heads, steps = (keys + 63) / 64;
+        const int64_t all = ((packed + n_seq - 1) / n_seq + p.tr - 1) / p.tr * n_seq * kv_heads, steps = (keys + 63) / 64;
         double best = 0;
         n = 1; unit = 64;
         for (int64_t c = 1; c <= most && c <= 64; ++c) {
