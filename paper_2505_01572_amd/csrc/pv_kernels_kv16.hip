@@ -147,7 +147,7 @@ k_kv16_append(const kv16_append_args a)
                 const kv16_seq q = kv16_seq_at(a.seqs, mine);
                 const int local = at - q.row0;
                 const int64_t pos = (int64_t)q.len + local;
-                if (local >= 0 && local < q.rows && pos < 0x7fffffff) {
+                if (local >= 0 && local < q.rows && pos <= 0x7fffffff) {
                     p.pos = (int)pos;
                     p.turn = a.rot.positions != nullptr ? a.rot.positions[at] : p.pos;
                     p.page = kv16_page(q, a.pool.n_pages, p.pos >> a.pool.page_shift);
@@ -228,7 +228,7 @@ k_kv16_keep(const kv16_keep_args a)
     const int n = (int)min((int64_t)accepted + 1, (int64_t)q.rows);
     auto place = [&](int local) -> int64_t {                  // of the token's first key; of values: of its group of four's first 16 bytes, times 4, and its number in the group
         const int64_t pos = (int64_t)q.len + local;
-        const int page = pos < 0x7fffffff ? kv16_page(q, a.pool.n_pages, (int)pos >> shift) : -1, in_page = (int)pos & ((1 << shift) - 1), t = in_page & 15;
+        const int page = pos <= 0x7fffffff ? kv16_page(q, a.pool.n_pages, (int)pos >> shift) : -1, in_page = (int)pos & ((1 << shift) - 1), t = in_page & 15;
         if (page < 0) return -1;
         const int64_t block = (int64_t)kv16_block<HD>(a.pool, page, head, which, in_page >> 4);
         return which ? (block + kv16_v_at(t & ~3, 0)) * 4 + (t & 3) : block + kv16_k_at(t, 0);

@@ -712,7 +712,7 @@ k_kv16_attn_wide(const kv16_attn_args a)
     }
 }
 
-// Chunks that a row and head have (0: written already, or no such row)
+// Chunks that a row, the whole wave's, and a lane's head have (0: written already, or no such row)
 __device__ inline int kv16_chunks(const kv16_attn_args &a, int row, int head, int TR)
 {
     const int rows[1] = {row};
@@ -744,10 +744,7 @@ k_kv16_attn_join(const kv16_attn_args a, int TR)
     float4 v[FL];
 #pragma unroll
     for (int i = 0; i < FL; ++i) if (i < a.nsplit) v[i] = *(const float4 *)(po + (size_t)i * HD);
-    // (a wave's heads may lie in two tiles, of different numbers of chunks)
-    const int n0 = kv16_chunks(a, row, min((id - row * per) * HW, a.n_q_heads - 1), TR), n1 = kv16_chunks(a, row, min((id - row * per) * HW + HW - 1, a.n_q_heads - 1), TR);
-    int n = n0;
-    if (n0 != n1) for (int h = 0; h < HW; ++h) { const int m = kv16_chunks(a, row, min((id - row * per) * HW + h, a.n_q_heads - 1), TR); if (lane / TPC == h) n = m; }
+    const int n = kv16_chunks(a, row, head, TR);              // (a wave's heads may lie in two tiles, of different numbers of chunks)
     if (lane % 16 >= n) one = make_float2(-INFINITY, 0.f);
     const float M = with_rotated<8>(with_rotated<4>(with_rotated<2>(with_rotated<1>(one.x, op_max), op_max), op_max), op_max), ref = M == -INFINITY ? 0.f : M;
     const float w = __builtin_amdgcn_exp2f(one.x - ref);
