@@ -3,7 +3,9 @@
 Values, and keys that are not rotated, are rounded to the pool's type once: equal to torch's conversion, bit for bit, in the whole pool, and moved tokens likewise.  Rotated numbers: as in tests/test_gpu_rotary.py.
 Attention: an output is off by half a step, eps / 2 of its value, plus what the arithmetic in 32 bits adds to the weights: scores of at most 64 in magnitude whose products are summed in chains of at
 most 12 (error 12 * 64 * 2^-24 < 2^-14 of a weight), once in the numerator and once in the sum, and the weights' pairs (2^-16 in bf16, 2^-21 in f16): under 2^-12 of sum(weight * |value|).  Where there are many rows a weight is one
-number of the type, off by up to half a step of it: 2^-9 in bf16 (2^-12 in f16) of sum(weight * |value|) more, which is asked for of calls of more than 16 rows and heads of a kv head.
+number of the type, off by up to half a step of it, which is asked for of calls of more than 16 rows and heads of a kv head.  Half a step: a type of p significant bits has numbers 2^(e + 1 - p) apart from 2^e to 2^(e + 1), so that
+the nearest is off by up to 2^(e - p), which is 2^-p of a number of at least 2^e: 2^-8 in bf16, 2^-11 in f16, eps / 2 of both.  The sum that an output is divided by is of the weights as they were, so an output is off by
+|sum(d_i w_i v_i)| / sum(w_i) <= eps / 2 * sum(weight * |value|), |d_i| <= eps / 2: half of that is too little.  (Nine keys whose weights are rounded once to bf16, all else in 64 bits: 1.067 times a bound with eps / 4 here, 0.733 with eps / 2.)
 lse: 2^-14 + 2^-22 |lse|."""
 import numpy as np
 import pytest
@@ -238,7 +240,7 @@ def check(pool, start, prefix, tables, q, out, lse, scale=None, masks=None):
     assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(np.isnan(glse), np.isnan(wlse))     # (tokens nobody wrote may be NaN)
     none, fine, far = np.isneginf(wlse), np.isfinite(want), np.isfinite(wlse)
     assert np.isfinite(got[fine]).all() and np.array_equal(np.isneginf(glse), none) and (got[none] == 0).all()
-    bound = torch.finfo(out.dtype).eps / 2 * np.abs(want) + (2.0 ** -12 + many * torch.finfo(out.dtype).eps / 4) * mag + torch.finfo(out.dtype).tiny
+    bound = torch.finfo(out.dtype).eps / 2 * np.abs(want) + (2.0 ** -12 + many * torch.finfo(out.dtype).eps / 2) * mag + torch.finfo(out.dtype).tiny
     worst = (np.abs(got - want) / bound)[fine].max() if fine.any() else 0
     assert worst <= 1, worst
     assert (np.abs(glse[far] - wlse[far]) <= 2.0 ** -14 + 2.0 ** -22 * np.abs(wlse[far])).all()
