@@ -39,7 +39,7 @@ __device__ inline dv_seq dv_seq_at(const dv_args &a, int s)
 {
     dv_seq q;
     q.row0 = a.row_start[s];
-    q.rows = min(a.row_start[s + 1], a.rows) - q.row0;
+    q.rows = min(max(a.row_start[s + 1], 0), a.rows) - max(q.row0, 0);        // (no difference that wraps, whatever the table holds)
     if (q.row0 < 0 || q.rows < 0) q.rows = 0;
     return q;
 }
