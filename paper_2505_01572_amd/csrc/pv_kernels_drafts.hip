@@ -8,7 +8,8 @@
 // The result is whole numbers.  What a draw turns on is computed in 64 bits: with exponentials of 32 bits a sum over a vocabulary of 10^5 lands on the wrong side of one of its 10^5 borders once in some 10^5 draws (once in 10^2
 // under p - q, where p's own sum moves all of them).  Whether a draft is taken turns on one border: without a drafter's probabilities rows are summed with exponentials of 32 bits, off by some 10^-7, which
 // decides one draft in 10^7 otherwise and takes a third of the time.
-//   rows   a workgroup takes a segment of a row: its maximum and the sum of its exponentials
+//   rows   a workgroup takes a segment of a row: its maximum and the sum of its exponentials.  Only of rows that a draft is behind: p of a tree's leaves, half of its nodes, and of a chain's last row is asked for only if
+//          the draw is there (16 trees of up to 48 nodes, 128256 logits of bf16, all four launches: 50.8 us with all rows, 34.3 so)
 //   walk   a tree: a workgroup a sequence joins the segments of the nodes' rows and walks along
 //   rest   a workgroup a segment of the row that the draw is behind (a chain: found anew by each): what is left to draw from, summed
 //   pick   a workgroup a sequence finds the segment that the draw falls in, and in that the token
@@ -27,7 +28,7 @@ struct dv_args {
     float *out_probs;
     dv_part *part;                          // [row][seg]
     int left;                               // segments of DV_SIZE tokens of the row that the draw is behind
-    double2 *rest;                          // [seq][left]: what is left to draw from, summed; without regard to a drafter
+    double2 *rest;                          // [seq][left]: what is left to draw from p - q, summed, and from p; or (dv_drawn: no) a dv_part of a segment, the sum without refused tokens
     int2 *walk;                             // [seq]: row that the draw is behind, whether a draft was refused there
 };
 
@@ -157,19 +158,42 @@ __device__ inline double dv_up_to(double v)
 template <typename T> __device__ inline int dv_head(const char *src) { return sizeof(T) == 2 && ((uintptr_t)src & 2) ? 1 : 0; }
 __device__ inline int dv_begin(int seg, int head, int size) { return seg == 0 ? 0 : head + seg * size; }
 
+// Whether a draft is behind a row of a sequence: only then its probabilities are asked for here (if the draw is behind it, it is summed there).  Whole workgroups call.
+__device__ inline bool dv_needed(const dv_args &a, const dv_seq &q, int row)
+{
+    constexpr int N = 4;
+    const int local = row - q.row0;
+    if (a.parent == nullptr) return local < q.rows - 1;
+    if (q.rows - local - 1 > N * 256) return true;           // (more than a thread looks at)
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < N; ++i) { const int j = local + 1 + (int)threadIdx.x + 256 * i; if (j < q.rows) any = any || a.parent[q.row0 + j] == local; }
+    return __syncthreads_or(any);
+}
+
 // The rows' sums, WIDE: in 64 bits.  Those are bound by the exponentials: some 22 instruction slots a logit, 16 of them in 64 bits; the others by the read of the logits.
 template <typename T, int E, bool WIDE>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WIDE ? 4 : 8)))
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WIDE ? 4 : E > 32 ? 7 : 8)))
 k_draft_rows(const dv_args a)
 {
     constexpr int NT = 256, V = 16 / (int)sizeof(T), U = E / V, D = E * (int)sizeof(T) / 4, SIZE = NT * E;
     __shared__ float sh_top[4];
     __shared__ double sh_sum[4];
     __shared__ int sh_first[4];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int row = blockIdx.x / a.segs, seg = blockIdx.x - row * a.segs;
     const char *src = a.logits + (int64_t)row * a.row_bytes;
     const int head = dv_head<T>(src), base = head + seg * SIZE;
+    int s = 0;
+    for (int k = 0; k < a.n_seq; k += 64) {
+        const int end = k + lane < a.n_seq ? a.row_start[k + lane + 1] : 0x7fffffff;
+        s += __popcll(__ballot(end <= row));
+    }
+    if (tid == 0 && seg == 0) {
+        if (a.path != nullptr) a.path[row] = -1;
+        a.out_probs[row] = 0.f;              // (rows of a sequence: later)
+    }
+    if (s >= a.n_seq || !dv_needed(a, dv_seq_at(a, s), row)) return;
     uint32_t x[D];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -180,18 +204,9 @@ k_draft_rows(const dv_args a)
     }
     // those that no 16 bytes hold: ahead of the first, behind the last
     const int behind = (a.vocab - head) % V;
-    const int alone = tid == 0 ? (seg == 0 && head ? 0 : -1) : tid <= behind && seg == (a.vocab - behind - head) / SIZE ? a.vocab - behind + tid - 1 : -1;
-    const float x0 = alone >= 0 ? dv_one<T>(src, alone) : -INFINITY;
-    int s = 0;
-    for (int k = 0; k < a.n_seq; k += 64) {
-        const int end = k + lane < a.n_seq ? a.row_start[k + lane + 1] : 0x7fffffff;
-        s += __popcll(__ballot(end <= row));
-    }
-    if (tid == 0 && seg == 0) {
-        if (a.path != nullptr) a.path[row] = -1;
-        a.out_probs[row] = 0.f;              // (rows of a sequence: below)
-    }
-    if (s >= a.n_seq) return;
+    auto alone_of = [&](int t) { return t == 0 ? (seg == 0 && head ? 0 : -1) : t <= behind && seg == (a.vocab - behind - head) / SIZE ? a.vocab - behind + t - 1 : -1; };
+    float x0 = -INFINITY;
+    if (const int alone = alone_of(tid); alone >= 0) x0 = dv_one<T>(src, alone);
     const double cold = dv_cold(a, s);
     float top = fmaxf(x0, -INFINITY);        // (of a number and NaN the number)
 #pragma unroll
@@ -229,6 +244,9 @@ k_draft_rows(const dv_args a)
         }
         if (top == -INFINITY) sum = 0.0;
     } else {
+        int me = tid;
+        asm volatile("" : "+v"(me));           // (found anew: kept, it would take a register that the logits need)
+        const int alone = alone_of(me);
         if (alone >= 0 && x0 == top) first = alone;
 #pragma unroll
         for (int i = 0; i < E; ++i) if (dv_get<T>(x, i) == top) first = min(first, base + ((i / V) * NT + tid) * V + i % V);      // (what fills a row up: only if the segment has nothing but -infinity)
@@ -427,7 +445,10 @@ __device__ inline void dv_weigh(const dv_args &a, const dv_row &r, const char *s
     }
 }
 
-// What is left to draw from in a segment.  A chain's walk is made anew by every workgroup: it is three trips to memory, a launch for it costs more.
+// Whether the draw behind row w.x is from max(p - q, 0)
+__device__ inline bool dv_drawn(const dv_args &a, int2 w) { return w.y && a.probs != nullptr; }
+
+// What is left to draw from in a segment: relative to its own largest logit, of refused tokens too, so that the row need not have been summed before; under a drafter's probabilities to the row's sum.  A chain's walk is made anew by every workgroup: it is three trips to memory, a launch for it costs more.
 template <typename T>
 __global__ void __launch_bounds__(256)
 k_draft_rest(const dv_args a)
@@ -435,6 +456,8 @@ k_draft_rest(const dv_args a)
     constexpr int NT = 256, N = DV_SIZE / NT / 2;
     __shared__ dv_chain_lds sh_chain;
     __shared__ double2 sh_sum[4];
+    __shared__ float sh_top[4];
+    __shared__ int sh_first[4];
     __shared__ uint32_t sh_out[(DV_SIZE + 32) / 32];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int s = blockIdx.x / a.left, seg = blockIdx.x - s * a.left;
@@ -446,12 +469,52 @@ k_draft_rest(const dv_args a)
         if (tid == 0) { a.walk[s] = w; a.accepted[s] = w.x - q.row0; a.out_probs[q.row0] = 1.f; }
         if (a.path != nullptr) for (int i = tid; i <= w.x - q.row0; i += NT) a.path[q.row0 + i] = i;
     }
-    if (cold == 0.0) return;
-    const dv_row r = w.y ? sh_chain.row : dv_row_of<64>(a, w.x, cold, dv_parts_of<64>(a, w.x));
     const char *src = a.logits + (int64_t)w.x * a.row_bytes;
-    const float *drafter = w.y && a.probs != nullptr ? a.probs + (int64_t)(w.x + 1) * a.probs_row : nullptr;
     const int head = dv_head<T>(src), base = head + seg * DV_SIZE, begin = dv_begin(seg, head, DV_SIZE), end = min(base + DV_SIZE, a.vocab);
     const bool some = dv_refused(a, q, w, begin, end, sh_out);
+    if (cold == 0.0 || !dv_drawn(a, w)) {
+        float x[2][N], d[N], x0 = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) dv_tokens<T, N>(src, nullptr, base + (k * NT + tid) * N, end, x[k], d);
+        if (tid == 0 && begin < base) x0 = dv_one<T>(src, 0);
+        float top = fmaxf(x0, -INFINITY);
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int i = 0; i < N; ++i) top = fmaxf(top, x[k][i]);
+        top = over_wave(top, op_max);
+        if (lane == 0) sh_top[wave] = top;
+        __syncthreads();
+        top = fmaxf(fmaxf(sh_top[0], sh_top[1]), fmaxf(sh_top[2], sh_top[3]));
+        double sum = 0.0;
+        int id = 0x7fffffff;
+        auto is = [&](int i) { return some && ((sh_out[(i - begin) >> 5] >> ((i - begin) & 31)) & 1u); };
+        if (cold > 0.0) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int i = 0; i < N; ++i) { const int t = base + (k * NT + tid) * N + i; const double v = dv_weight(x[k][i], cold, top); sum += t < end && is(t) ? 0.0 : v; }
+            if (tid == 0 && begin < base && !is(0)) sum += dv_weight(x0, cold, top);
+            sum = dv_over_wave(sum);
+        } else {
+            if (tid == 0 && begin < base && x0 == top) id = 0;
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int i = 0; i < N; ++i) if (x[k][i] == top) id = min(id, base + (k * NT + tid) * N + i);      // (behind the row's end: only if the segment has nothing but -infinity)
+            id = dv_min_over_wave(id);
+        }
+        if (lane == 0) { sh_sum[wave].x = sum; sh_first[wave] = id; }
+        __syncthreads();
+        if (tid == 0) {
+            dv_part p;
+            p.sum = (sh_sum[0].x + sh_sum[1].x) + (sh_sum[2].x + sh_sum[3].x); p.top = top; p.first = min(min(sh_first[0], sh_first[1]), min(sh_first[2], sh_first[3]));
+            ((dv_part *)a.rest)[(int64_t)s * a.left + seg] = p;
+        }
+        return;
+    }
+    const dv_row r = sh_chain.row;
+    const float *drafter = a.probs + (int64_t)(w.x + 1) * a.probs_row;
     const double inv = 1.0 / r.sum;
     double sum = 0.0, all = 0.0;
 #pragma unroll
@@ -483,21 +546,35 @@ k_draft_pick(const dv_args a)
     const int2 w = a.walk[s];                // (of a sequence without rows: anything)
     const double2 *rest = a.rest + (int64_t)s * a.left;
     double2 first[1];
-    first[0] = lane < a.left ? rest[lane] : make_double2(0.0, 0.0);      // (T = 0: anything)
+    first[0] = lane < a.left ? rest[lane] : make_double2(0.0, 0.0);
     const double cold = dv_cold(a, s);
     if (q.rows == 0) { if (tid == 0) { a.accepted[s] = 0; a.next[s] = -1; } return; }
-    const dv_parts parts = dv_parts_of<64>(a, w.x);
     const double u = dv_u(a, w.x, 1);
     const char *src = a.logits + (int64_t)w.x * a.row_bytes;
     const int head = dv_head<T>(src);
-    const dv_row r = dv_row_of<64>(a, w.x, cold, parts);
+    bool drawn = dv_drawn(a, w);
+    dv_row r = {1.0, -INFINITY, 0x7fffffff, false};          // (nothing but its ratios counts of a row that p alone is drawn from)
+    if (drawn && cold > 0.0) r = dv_row_of<64>(a, w.x, cold, dv_parts_of<64>(a, w.x));
+    else {
+        const dv_part *p = (const dv_part *)rest;
+        const dv_part mine = __builtin_bit_cast(dv_part, first[0]);
+        if (lane < a.left) r.top = mine.top;
+        for (int i = 64 + lane; i < a.left; i += 64) r.top = fmaxf(r.top, p[i].top);
+        r.top = over_wave(r.top, op_max);
+        r.any = r.top > -INFINITY && r.top < INFINITY;
+        if (cold == 0.0) {
+            if (lane < a.left && mine.top == r.top) r.first = mine.first;
+            for (int i = 64 + lane; i < a.left; i += 64) if (p[i].top == r.top) r.first = min(r.first, p[i].first);
+            r.first = dv_min_over_wave(r.first);
+        }
+    }
     if (tid == 0) sh_id = -1;
     if (!r.any) { if (tid == 0) a.next[s] = -1; return; }
     if (cold == 0.0) { if (tid == 0) a.next[s] = r.first; return; }      // (with a refused draft too: it was another token)
     const double inv = 1.0 / r.sum;
     // what the segments weigh, a lane a segment, in every wave alike
     double sums[SC], total = 0.0;            // (up to and with each)
-    bool drawn = w.y && a.probs != nullptr;
+    const bool whole = !drawn;
     for (int pass = 0; pass < 2; ++pass) {   // (nothing left of p - q, which rounding can bring about: p)
         total = 0.0;
 #pragma unroll
@@ -505,7 +582,12 @@ k_draft_pick(const dv_args a)
             sums[c] = 0.0;
             if (c * 64 >= a.left) continue;
             const double2 v = c == 0 ? first[0] : c * 64 + lane < a.left ? rest[c * 64 + lane] : make_double2(0.0, 0.0);
-            sums[c] = total + dv_up_to(drawn || a.probs == nullptr ? v.x : v.y);
+            double some = drawn ? v.x : v.y;
+            if (whole) {
+                const dv_part part = __builtin_bit_cast(dv_part, v);
+                some = c * 64 + lane < a.left && part.sum > 0.0 ? part.sum * dv_weight(part.top, cold, r.top) : 0.0;
+            }
+            sums[c] = total + dv_up_to(some);
             total = __shfl(sums[c], 63, 64);
         }
         if (total > 0.0 || !drawn) break;
@@ -577,13 +659,13 @@ k_draft_pick(const dv_args a)
 
 // ------------------------------- host side ----------------------------------------
 
-// Tokens a segment of a row: 4096, or, where there are rows enough for the chip, 8192 (64-bit sums), 16384 or (f32) 8192.  Whether there is a drafter is not known where the workspace is measured: its size is that of 4096.
+// Tokens a segment of a row: 4096, or, where there are rows enough for the chip, 8192 (64-bit sums), 14336 (what registers hold at seven waves a SIMD: 16 trees 34.3 us; 12288 at eight 34.9; 16384 at six 34.5) or (f32) 8192.  Whether there is a drafter is not known where the workspace is measured: its size is that of 4096.
 struct dv_plan { int e, segs, left; };
 static dv_plan plan(int64_t rows, int vocab, bool wide, int dtype)
 {
     dv_plan p;
     p.left = (vocab + DV_SIZE - 1) / DV_SIZE;
-    p.e = rows * p.left <= 4096 ? 16 : wide || dtype == PV_F32 ? 32 : 64;
+    p.e = rows * p.left <= 4096 ? 16 : wide || dtype == PV_F32 ? 32 : 56;
     p.segs = (vocab + 256 * p.e - 1) / (256 * p.e);
     return p;
 }
@@ -629,7 +711,7 @@ static int launch(const dv_args &a, int e, hipStream_t s)
         if (e == 16) k_draft_rows<T, 16, true><<<grid, 256, 0, s>>>(a);
         else k_draft_rows<T, 32, true><<<grid, 256, 0, s>>>(a);
     } else {
-        constexpr int most = sizeof(T) == 4 ? 32 : 64;
+        constexpr int most = sizeof(T) == 4 ? 32 : 56;
         if (e == 16) k_draft_rows<T, 16, false><<<grid, 256, 0, s>>>(a);
         else k_draft_rows<T, most, false><<<grid, 256, 0, s>>>(a);
     }
