@@ -284,6 +284,7 @@ __device__ inline void kv16_finish4(const kv16_attn_args &a, const kv16_row &w, 
 
 // Few rows: one workgroup is a kv head, a tile of 16 packed rows of a sequence, a chunk of its keys; the waves take 32 keys in turn, straight from memory to registers, and are joined
 // through LDS at the end.  A weight is a pair of numbers of the cache's type (16 significant bits in bf16, 22 in f16): the matrix cores have the time.  Bound by the read of the cache: the next 32 keys' K is asked for when this one's scores are there, V when its products are.
+// 32 sequences of one row and some 4000 keys of 8 heads of 128, 531 MB: 82.6 us, 6.4 TB/s (a read stream reaches 6.43); 4.6 more for the launch that joins the chunks.
 template <int HD, typename S>
 __global__ void __launch_bounds__(256)
 k_kv16_attn(const kv16_attn_args a)
@@ -439,6 +440,8 @@ k_kv16_attn(const kv16_attn_args a)
 // keys two, because the products with the next step's keys are made while this one's scores become weights: those keep the vector ALU busy, which is what bounds it (an exponential takes four turns), the products the
 // matrix cores.  A weight is one number of the cache's type here, 8 significant bits in bf16: rounded to nearest, they add to an output as much as its own rounding does; a pair of them costs half as many products
 // again.  The sum is of the weights before they are rounded.
+// Two prompts of up to 2048 rows of 32 heads of 128 over up to 6100 keys and themselves, 335 GFLOP, bf16: 341 us, 980 TFLOP/s (a library product of 8192^3: 1242).  There the matrix cores are busy 41 % of the time, the vector ALU 48 %; the same
+// without copies takes 40 us less, without exponentials 18.  One product after the other with the weights between them, as pairs: 504.  Values as whole 16 bytes, sorted into operands by moves: 350, by exchanges of registers: 357.
 template <int HD>
 struct kv16_wide {
     static constexpr int KS = HD / 32;
@@ -728,7 +731,7 @@ __device__ inline int kv16_chunks(const kv16_attn_args &a, int row, int head, in
     return nk <= a.chunk ? 0 : (nk + a.chunk - 1) / a.chunk;
 }
 
-// The chunks of a row's keys joined, up to 16 of them: HD / 4 lanes a row and head, all of its chunks on their way at once.  A wave's heads are of one row: asked for beside the sequence's tables, whatever these turn out to say
+// The chunks of a row's keys joined, up to 16 of them (a trip to the tables beside one to the chunks: 4.6 us for 32 rows of 32 heads, 6.9 for 200 of 64): HD / 4 lanes a row and head, all of its chunks on their way at once.  A wave's heads are of one row: asked for beside the sequence's tables, whatever these turn out to say
 template <int HD, typename S>
 __global__ void __launch_bounds__(256)
 k_kv16_attn_join(const kv16_attn_args a, int TR)
