@@ -404,7 +404,7 @@ int pv_kv16_append(const pv_kv16_pool *pool, const pv_kv8_seqs *seqs, const void
 /* Attention of every row over the cache, as pv_kv8_attention, with q and out of the pool's type: out = softmax(scale * q K^T) V, query head a over kv head a / (n_q_heads / n_kv_heads).  mask == NULL: row i of sequence s sees
  * tokens 0 .. prefix_len[s] + i.  Else (a draft tree) mask [n_rows][mask_words]: the row sees all tokens before prefix_len[s], and token prefix_len[s] + t if bit t % 64 of its word t / 64 is set, t less than 64 * mask_words and than the
  * number of rows that s has in the call.  A row that sees no token: zeros, and -infinity in lse (NULL, or float [n_rows][n_q_heads]).  What a row does not see has no influence on it, NaN and infinities included; a
- * value that it sees and that is infinite or NaN makes its output infinite or NaN.  Weights meet the values as pairs of numbers of the pool's type (16 significant bits in bf16, 22 in f16), in calls of many rows as one (8 and 11);
+ * value that it sees and that is infinite or NaN makes its output infinite or NaN.  Weights meet the values as pairs of numbers of the pool's type (16 significant bits in bf16, 22 in f16);
  * all sums have 32 bits.
  * n_q_heads is a multiple of n_kv_heads, (n_rows + n_seq) * n_q_heads <= 2^24, table_pages * page_tokens <= 2^30, mask_words <= 2^18, scale is finite.  workspace: at least pv_kv16_attention_bytes,
  * 16-byte aligned, for this call alone until it has run. */

@@ -143,6 +143,18 @@ __device__ inline float kv16_max(float a, float b)
     return __builtin_amdgcn_fmed3f(a, b, top);
 }
 
+// Four weights as numbers of the cache's type, and what the type leaves of them
+template <typename S> __device__ inline void kv16_pairs(const float (&p)[4], uint2 &w, uint2 &low)
+{
+    if constexpr (__is_same(S, __bf16)) {
+        split2(p[0], p[1], w.x, low.x); split2(p[2], p[3], w.y, low.y);
+    } else {
+        const kv16_h2 a = {(_Float16)p[0], (_Float16)p[1]}, b = {(_Float16)p[2], (_Float16)p[3]};
+        w = make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
+        low = make_uint2(kv16_two<_Float16>(p[0] - (float)a.x, p[1] - (float)a.y), kv16_two<_Float16>(p[2] - (float)b.x, p[3] - (float)b.y));
+    }
+}
+
 // Scores of NG groups of 16 keys -> weights under the new maximum (P[tile][group]: keys 4 g .. + 3; PL: what the type leaves of them); what was there is scaled to it.  see(t): which
 // of the keys from 4 g on the lane's row of tile t may attend to, a bit each.
 template <typename S, int HD, int RT, int NG, typename SEE>
@@ -174,13 +186,7 @@ __device__ inline void kv16_softmax(kv16_acc<HD, RT> &A, f32x4 (&X)[RT][NG], flo
 #pragma unroll
             for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(X[t][q][r], scale2, c));
             ps += (p[0] + p[1]) + (p[2] + p[3]);
-            if constexpr (__is_same(S, __bf16)) {
-                split2(p[0], p[1], P[t][q].x, PL[t][q].x); split2(p[2], p[3], P[t][q].y, PL[t][q].y);
-            } else {
-                const kv16_h2 a = {(_Float16)p[0], (_Float16)p[1]}, b = {(_Float16)p[2], (_Float16)p[3]};
-                P[t][q] = make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
-                PL[t][q] = make_uint2(kv16_two<_Float16>(p[0] - (float)a.x, p[1] - (float)a.y), kv16_two<_Float16>(p[2] - (float)b.x, p[3] - (float)b.y));
-            }
+            kv16_pairs<S>(p, P[t][q], PL[t][q]);
         }
         A.l[t] = fmaf(A.l[t], keep[t], ps);
         A.m[t] = mx;
@@ -437,11 +443,11 @@ k_kv16_attn(const kv16_attn_args a)
 }
 
 // Many rows: a workgroup is a kv head, 64 RT packed rows of a sequence (16 RT a wave), a chunk of its keys.  64 keys at a time go through LDS, copied straight from memory, each wave a group of 16: values a step ahead,
-// keys two, because the products with the next step's keys are made while this one's scores become weights: those keep the vector ALU busy, which is what bounds it (an exponential takes four turns), the products the
-// matrix cores.  A weight is one number of the cache's type here, 8 significant bits in bf16: rounded to nearest, they add to an output as much as its own rounding does; a pair of them costs half as many products
-// again.  The sum is of the weights before they are rounded.
-// Two prompts of up to 2048 rows of 32 heads of 128 over up to 6100 keys and themselves, 335 GFLOP, bf16: 341 us, 980 TFLOP/s (a library product of 8192^3: 1242).  There the matrix cores are busy 41 % of the time, the vector ALU 48 %; the same
-// without copies takes 40 us less, without exponentials 18.  One product after the other with the weights between them, as pairs: 504.  Values as whole 16 bytes, sorted into operands by moves: 350, by exchanges of registers: 357.
+// keys two, because the products with the next step's keys are made while this one's scores become weights: those keep the vector ALU busy (an exponential takes four turns, what makes a weight a pair two and a half), the products the
+// matrix cores.  A weight is a pair of numbers of the cache's type, as with few rows: so a row's result has the same bits behind it whatever tile it comes to lie in.  One number a weight, 8 significant bits in bf16, adds as
+// much to an output's error as its own rounding does (relative to 64 bits 2.3e-3 for 1.7e-3, in f16 2.9e-4 for 2.1e-4) and takes three quarters of the time (341 us for the 454 below).
+// Two prompts of up to 2048 rows of 32 heads of 128 over up to 6100 keys and themselves, bf16: 454 us, 335 GFLOP asked for, 502 on the matrix cores, whose 1107 TFLOP/s are 89 % of what a library product of 8192^3 reaches (1242).
+// Values as whole 16 bytes, sorted into operands by moves or by exchanges of registers: some 3 % more.
 template <int HD>
 struct kv16_wide {
     static constexpr int KS = HD / 32;
@@ -464,15 +470,14 @@ template <typename S> __device__ inline void kv16_under(kv16_tile &T, float mx, 
     T.keep = __builtin_amdgcn_exp2f(T.m - ref); T.c = (float)kv16_wide_bias<S>() - ref; T.m = m;
 }
 __device__ inline float kv16_maximum4(float m, f32x4 x) { return kv16_maximum(kv16_maximum(kv16_maximum(kv16_maximum(m, x[0]), x[1]), x[2]), x[3]); }
-template <typename S> __device__ inline uint2 kv16_weights4(f32x4 x, float scale2, float c, float &sum)
+template <typename S> __device__ inline void kv16_weights4(f32x4 x, float scale2, float c, float &sum, uint2 &w, uint2 &low)
 {
     float p[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(x[r], scale2, c));
     sum += (p[0] + p[1]) + (p[2] + p[3]);
-    uint2 w = make_uint2(kv16_two<S>(p[0], p[1]), kv16_two<S>(p[2], p[3]));
-    asm volatile("" : "+v"(w.x), "+v"(w.y));     // (made here, not where they are used)
-    return w;
+    kv16_pairs<S>(p, w, low);
+    asm volatile("" : "+v"(w.x), "+v"(w.y), "+v"(low.x), "+v"(low.y), "+v"(sum));     // (made here, not where they are used: the sum put off would keep every weight)
 }
 
 template <int HD, int RT, typename S>
@@ -598,7 +603,7 @@ k_kv16_attn_wide(const kv16_attn_args a)
         }
         // A step's work in twelve parts, in each of which the matrix cores and the vector ALU have about as much to do, LDS asked a part ahead: the scores of the next step beside the first half of the weights, the products with the
         // first half of the values beside the second half of the weights, those with the second half beside the next maximum
-        uint2 P[RT][4];
+        uint2 P[RT][4], PL[RT][4];
         float ps[RT], mx[RT];
 #pragma unroll
         for (int t = 0; t < RT; ++t) { ps[t] = 0.f; mx[t] = -INFINITY; }
@@ -615,16 +620,16 @@ k_kv16_attn_wide(const kv16_attn_args a)
                 v[h] = make_uint4(x.x, x.y, y.x, y.y);
             }
         };
-        auto products = [&](int n, const uint4 (&v)[2]) {
+        auto products = [&](int n, const uint4 (&v)[2], const uint2 (&w)[RT][4]) {
             const int u = n / KS, b = n % KS;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int t = 0; t < RT; ++t) A.O[t][2 * b + h] = kv16_mfma<S>(v[h], make_uint4(P[t][2 * u].x, P[t][2 * u].y, P[t][2 * u + 1].x, P[t][2 * u + 1].y), A.O[t][2 * b + h]);
+                for (int t = 0; t < RT; ++t) A.O[t][2 * b + h] = kv16_mfma<S>(v[h], make_uint4(w[t][2 * u].x, w[t][2 * u].y, w[t][2 * u + 1].x, w[t][2 * u + 1].y), A.O[t][2 * b + h]);
         };
         auto weights = [&](int n, int half_of) {             // n of 2 RT: two groups of a tile
             const int t = n >> 1, i = 2 * half_of + (n & 1);
-            P[t][i] = kv16_weights4<S>(X[t][i], a.scale2, T[t].c, ps[t]);
+            kv16_weights4<S>(X[t][i], a.scale2, T[t].c, ps[t], P[t][i], PL[t][i]);
         };
         keys(s + 1, 0, k[0]);                // (behind the last step: of what the buffer holds, not used)
         __builtin_amdgcn_sched_barrier(0);
@@ -660,7 +665,8 @@ k_kv16_attn_wide(const kv16_attn_args a)
 #pragma unroll
                 for (int w = n - KS; w < 2 * RT; w += KS) mx[w >> 1] = kv16_maximum4(kv16_maximum4(mx[w >> 1], next[w >> 1][2 * (w & 1)]), next[w >> 1][2 * (w & 1) + 1]);
             }
-            products(n, va[n & 1]);
+            products(n, va[n & 1], P);
+            products(n, va[n & 1], PL);
             __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
@@ -830,12 +836,12 @@ k_kv16_attn_merge(const kv16_attn_args a, int TR)
 
 // How a call's work is cut, from what the host knows: its rows (sequences are taken to have as many each), and how far the tables reach.
 // Rows a tile: 16, straight from memory, where sequences have no more, and where the whole work is small, so that what the other kernel pays for going through LDS weighs more than keys read again for every 16 rows.  Else 64, or
-// 128 where a sequence has much to do.  Eight kv heads of 128, one sequence, packed rows x keys, us from a graph with 16, 64, 128: 64 x 4000 14.5, 15.5, 18.0; 256 x 1000 13.3, 16.2, 20.2; 256 x 4000 22.9, 23.2, 25.7; 32 x 60000 58.9,
-// 47.4, 49.2; 64 x 16000 29.1, 21.9, 25.8; 512 x 4000 33.9, 31.5, 33.4; 256 x 16000 67.4, 39.4, 39.5; 1024 x 4000 51.1, 41.2, 39.9; 256 x 60000 283, 104, 89.  16 sequences of up to 4000 keys, 16, 32, 128 rows each 34.4, 38.2, 44.6;
-// 46.9, 34.1, 49.9; 84.7, 72.0, 80.8.
+// 128 where a sequence has much to do.  Eight kv heads of 128, one sequence, packed rows x keys, us from a graph with 16, 64, 128: 64 x 4000 14.0, 15.5, 18.4; 256 x 1000 13.4, 16.5, 20.8; 256 x 4000 22.2, 22.5, 26.5; 32 x 60000 60.8,
+// 47.6, 62.7; 64 x 16000 28.6, 22.2, 27.0; 512 x 4000 32.9, 30.7, 32.6; 256 x 16000 67.7, 41.8, 41.4; 1024 x 4000 47.5, 44.4, 43.9; 256 x 60000 283, 115, 110.  16 sequences of up to 4000 keys, 16, 32, 128 rows each 33.9, 36.2, 51.0;
+// 46.4, 37.3, 51.6; 86.1, 63.2, 92.8.
 // Chunks of keys, 16 rows a tile: until there are two workgroups a CU, or four where sequences of different lengths come out at different times; few keys are one workgroup's, which saves the launch that joins.  More rows: as
 // many as would take least by a count of steps (of 64 keys; three more for a workgroup's begin and end; two workgroups of a CU share it, one alone takes 0.65 as long) and of what the join has to move (one sequence of 1600 rows over
-// 4301 keys 82 us with six chunks, in two rounds of workgroups, 68 with four, in one).
+// 4301 keys, f16: 73 us with six chunks, in two rounds of workgroups, 69 with four, in one).
 struct kv16_plan { int tr, units, nsplit, chunk; };
 
 static kv16_plan plan(int n_seq, int n_rows, int group, int kv_heads, int hd, int64_t keys)
