@@ -427,7 +427,7 @@ int pv_kv16_keep(const pv_kv16_pool *pool, const pv_kv8_seqs *seqs, const int32_
  *   A draw behind row r: the lowest id at which the sum of the (remaining) probabilities in the order of ids passes u[r][1] times their whole sum.
  * So tokens are distributed as the target alone would have them, whatever the drafts.  accepted [n_seq]: drafts taken; next_token [n_seq]; path [rows] (NULL where there is no tree): row_start[s] + d = the number in its sequence of the d-th row reached, from
  * the first row (0) on, -1 behind the last and in rows of no sequence; probs [rows]: p of each row's draft (1 in a sequence's first row, 0 in rows of no sequence).  A sequence without rows: 0 and -1.  Draws are made in 64 bits, and with draft_probs all of it; without, a row's sum has exponentials of 32 bits, so that p is off by 2^-17 of itself at most (some 10^-7), where a
- * draft is taken or not and in probs.
+ * chain's draft is taken or not and in probs; a tree's child that this would decide is judged in 64 bits.  A row that has probabilities, all of whose tokens are children's, has one of the children taken.
  * A logit of -infinity or NaN has probability 0; a row with +infinity, or of nothing else, has no probabilities: no draft is taken behind it, and a draw there is -1 (as where no token has any left).  A token outside [0, vocab) is never taken.
  * vocab <= 2^21, rows and n_seq <= 2^20, each times ceil(vocab / 4096) < 2^24; workspace: at least pv_verify_drafts_bytes, 16-byte aligned, for this call alone until it has run. */
 int pv_verify_drafts_bytes(int64_t rows, int32_t n_seq, int32_t vocab, size_t *bytes);

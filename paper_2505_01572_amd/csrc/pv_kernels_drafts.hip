@@ -7,7 +7,7 @@
 //
 // The result is whole numbers.  What a draw turns on is computed in 64 bits: with exponentials of 32 bits a sum over a vocabulary of 10^5 lands on the wrong side of one of its 10^5 borders once in some 10^5 draws (once in 10^2
 // under p - q, where p's own sum moves all of them).  Whether a draft is taken turns on one border: without a drafter's probabilities rows are summed with exponentials of 32 bits, off by some 10^-7, which
-// decides one draft in 10^7 otherwise and takes a third of the time.
+// decides one draft of a chain in 10^7 otherwise and takes a third of the time.  (What remains of a row behind refused children of a tree may be less than that: there the walk looks twice.)
 //   rows   a workgroup takes a segment of a row: its maximum and the sum of its exponentials.  Only of rows that a draft is behind: p of a tree's leaves, half of its nodes, and of a chain's last row is asked for only if
 //          the draw is there (16 trees of up to 48 nodes, 128256 logits of bf16, all four launches: 50.8 us with all rows, 34.3 so)
 //   walk   a tree: a workgroup a sequence joins the segments of the nodes' rows and walks along
@@ -345,21 +345,67 @@ template <typename T> __device__ inline int2 dv_chain(const dv_args &a, const dv
 }
 
 // The walk along a sequence's tree: node by node what each child's p is, then one wave.  Some five trips to memory, one behind the other, for each 64 nodes.
+//
+// What is left behind refused children is 1 less their p, and every p of a row is off by the same small part of itself, that of the row's sum (2^-17 at most): a child whose u times what is left comes so near to its p that this decides
+// is judged by what the tokens that are left weigh themselves, in 64 bits, the refused ones not among them, and what is left behind it is known from there to 2^-35 of that.  So the last child that a row allows is always taken,
+// and there is a token left to draw behind refused children.  Of random numbers some 10^-5 come so near.
 #define DV_NODES 1024                       // nodes at a time
+#define DV_NEAR 0x1p-17
+#define DV_NEAR_JUDGED 0x1p-35
+struct dv_judge_lds { double sum[16], mine; uint32_t out[DV_SIZE / 32]; };
+struct dv_judged { bool taken; double left, near; };       // left: behind the child, should it be refused; near: as far as that may be off
+// ... for child k of node `at`.  Whole workgroups call.  (Sums of numbers that are not negative are no less than any of them, however they are rounded: of a token alone they are its weight.)
+template <typename T> __device__ inline dv_judged dv_judge(const dv_args &a, const dv_seq &q, int at, int k, double cold, dv_judge_lds *sh)
+{
+    constexpr int NT = 1024;
+    const int tid = threadIdx.x, row = q.row0 + at, token = a.tokens[q.row0 + k];
+    const char *src = a.logits + (int64_t)row * a.row_bytes;
+    const dv_row r = dv_row_of<64>(a, row, cold, dv_parts_of<64>(a, row));
+    const double top = r.top;
+    double sum = 0.0;
+    for (int begin = 0; begin < a.vocab; begin += DV_SIZE) {
+        for (int i = tid; i < DV_SIZE / 32; i += NT) sh->out[i] = 0u;
+        __syncthreads();
+        for (int i = at + 1 + tid; i < k; i += NT) {          // (child k has a token that none before it had)
+            const int t = a.tokens[q.row0 + i];
+            if (a.parent[q.row0 + i] == at && t >= begin && t < begin + DV_SIZE) atomicOr(&sh->out[(t - begin) >> 5], 1u << ((t - begin) & 31));
+        }
+        __syncthreads();
+        for (int i = tid; i < DV_SIZE && begin + i < a.vocab; i += NT) {
+            if ((sh->out[i >> 5] >> (i & 31)) & 1u) continue;
+            const double w = dv_weight(dv_one<T>(src, begin + i), cold, top);
+            if (begin + i == token) sh->mine = w;
+            sum += w;
+        }
+        __syncthreads();
+    }
+    sum = dv_over_wave(sum);
+    if ((tid & 63) == 0) sh->sum[tid >> 6] = sum;
+    __syncthreads();
+    sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < NT / 64; ++i) sum += sh->sum[i];
+    const double mine = sh->mine;
+    __syncthreads();
+    return {dv_u(a, q.row0 + k, 0) * sum < mine, (sum - mine) / r.sum, DV_NEAR_JUDGED * (sum / r.sum)};
+}
+
 template <typename T>
 __global__ void __launch_bounds__(1024)
 k_draft_walk(const dv_args a)
 {
     constexpr int NT = 1024, GL = 16;
-    __shared__ double sh_p[DV_NODES], sh_u[DV_NODES], sh_left;
-    __shared__ int sh_parent[DV_NODES], sh_token[DV_NODES], sh_walk[2];
+    __shared__ double sh_p[DV_NODES], sh_u[DV_NODES], sh_left[2];
+    __shared__ int sh_parent[DV_NODES], sh_token[DV_NODES], sh_walk[3];
+    __shared__ dv_judge_lds sh_judge;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, s = blockIdx.x;
     const dv_seq q = dv_seq_at(a, s);
     if (q.rows == 0) return;
     const double cold = dv_cold(a, s);
     if (tid == 0) { a.path[q.row0] = 0; a.out_probs[q.row0] = 1.f; }
     int at = 0, depth = 0;
-    double left = 1.0;
+    const double off = cold > 0.0 ? DV_NEAR : 0.0;           // (the most probable token alone: p is 1 or 0)
+    double left = 1.0, near = off;           // of p behind the refused children of `at`; as far as that, and p, may be off
     for (int n0 = 1; n0 < q.rows; n0 += DV_NODES) {
         const int n = min(DV_NODES, q.rows - n0);
         for (int i0 = 0; i0 < n; i0 += NT / GL) {
@@ -373,36 +419,50 @@ k_draft_walk(const dv_args a)
             if (tid % GL == 0) { sh_p[i] = p; sh_u[i] = u; sh_parent[i] = good ? up : -1; sh_token[i] = token; a.out_probs[row] = (float)p; }
         }
         __syncthreads();
-        if (wave == 0) {
-            for (int b = 0; b < n; b += 64) {
-                const int i = b + lane;
-                const int up = i < n ? sh_parent[i] : -2;
-                uint64_t todo = __ballot(up == at);
-                while (todo) {
-                    const int k = b + __ffsll((unsigned long long)todo) - 1, token = sh_token[k];
-                    // a token that an earlier child has had
-                    bool had = false;
-                    for (int j = at + 1 - n0; j < k; j += 64) {
-                        const int c = j + lane;
-                        bool same = false;
-                        if (c < k) same = c >= 0 ? sh_parent[c] == at && sh_token[c] == token : a.parent[q.row0 + n0 + c] == at && a.tokens[q.row0 + n0 + c] == token;
-                        had = had || __any(same);
+        int from = 0;                        // the first node to look at; from the second turn on it has been judged
+        bool judged = false;
+        dv_judged verdict = {};
+        for (;;) {
+            if (wave == 0) {
+                int ask = -1;
+                for (int b = from & ~63; b < n && ask < 0; b += 64) {
+                    const int i = b + lane;
+                    const int up = i < n ? sh_parent[i] : -2;
+                    uint64_t todo = __ballot(up == at) & (b < from ? ~0ull << (from - b) : ~0ull);
+                    while (todo) {
+                        const int k = b + __ffsll((unsigned long long)todo) - 1, token = sh_token[k];
+                        // a token that an earlier child has had
+                        bool had = false;
+                        for (int j = at + 1 - n0; j < k; j += 64) {
+                            const int c = j + lane;
+                            bool same = false;
+                            if (c < k) same = c >= 0 ? sh_parent[c] == at && sh_token[c] == token : a.parent[q.row0 + n0 + c] == at && a.tokens[q.row0 + n0 + c] == token;
+                            had = had || __any(same);
+                        }
+                        const double p = had ? 0.0 : sh_p[k], u = sh_u[k];
+                        bool taken = u * (left + near) < p;
+                        const bool known = judged && k == from;
+                        if (known) taken = verdict.taken;
+                        else if (u * (left - near) < p && !taken && p > 0.0) { ask = k; break; }
+                        todo &= todo - 1;
+                        if (taken) {
+                            at = n0 + k; ++depth; left = 1.0; near = off;
+                            if (lane == 0) a.path[q.row0 + depth] = at;
+                            const uint64_t past = k - b == 63 ? 0ull : ~0ull << (k - b + 1);
+                            todo = __ballot(up == at) & past;
+                        } else if (known) { left = verdict.left; near = verdict.near; }
+                        else left -= p;
                     }
-                    const double p = had ? 0.0 : sh_p[k];
-                    todo &= todo - 1;
-                    if (sh_u[k] * left < p) {
-                        at = n0 + k; ++depth; left = 1.0;
-                        if (lane == 0) a.path[q.row0 + depth] = at;
-                        const uint64_t past = k - b == 63 ? 0ull : ~0ull << (k - b + 1);
-                        todo = __ballot(up == at) & past;
-                    } else left -= p;
                 }
+                if (lane == 0) { sh_walk[0] = at; sh_walk[1] = depth; sh_walk[2] = ask; sh_left[0] = left; sh_left[1] = near; }
             }
-            if (lane == 0) { sh_walk[0] = at; sh_walk[1] = depth; sh_left = left; }
+            __syncthreads();
+            at = sh_walk[0]; depth = sh_walk[1]; left = sh_left[0]; near = sh_left[1]; from = sh_walk[2];
+            __syncthreads();
+            if (from < 0) break;
+            verdict = dv_judge<T>(a, q, at, n0 + from, cold, &sh_judge);
+            judged = true;
         }
-        __syncthreads();
-        at = sh_walk[0]; depth = sh_walk[1]; left = sh_left;
-        __syncthreads();
     }
     if (tid == 0) { a.walk[s] = make_int2(q.row0 + at, 0); a.accepted[s] = depth; }
 }
