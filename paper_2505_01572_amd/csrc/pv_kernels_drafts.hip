@@ -758,11 +758,12 @@ extern "C" int pv_verify_drafts_bytes(int64_t rows, int32_t n_seq, int32_t vocab
     return PV_OK;
 }
 
-// a call without rows: every sequence is empty
-__global__ void __launch_bounds__(256) k_draft_none(int n, int32_t *accepted, int32_t *next)
+// a call without rows, or without sequences: every sequence is empty, every row of none
+__global__ void __launch_bounds__(256) k_draft_none(int n_seq, int32_t *accepted, int32_t *next, int rows, int32_t *path, float *probs)
 {
     const int i = blockIdx.x * 256 + threadIdx.x;
-    if (i < n) { accepted[i] = 0; next[i] = -1; }
+    if (i < n_seq) { accepted[i] = 0; next[i] = -1; }
+    if (i < rows) { if (path != nullptr) path[i] = -1; probs[i] = 0.f; }
 }
 
 template <typename T>
@@ -794,8 +795,8 @@ extern "C" int pv_verify_drafts(const int32_t *row_start, int32_t n_seq, const v
     if (rc != PV_OK) return rc;
     if (dtype != PV_F32 && dtype != PV_BF16 && dtype != PV_F16) { pv_set_error("bad dtype %d", dtype); return PV_EINVAL; }
     if (parent && draft_probs) { pv_set_error("a tree's drafts go without a drafter's probabilities"); return PV_EINVAL; }
-    if (n_seq == 0) return PV_OK;
-    if (!row_start || !accepted || !next_token || (rows && (!logits || !tokens || !u || !probs)) || (rows && parent && !path)) { pv_set_error("null pointer"); return PV_EINVAL; }
+    if (n_seq == 0 && rows == 0) return PV_OK;
+    if (!row_start || (n_seq && (!accepted || !next_token)) || (rows && (!logits || !tokens || !u || !probs)) || (rows && parent && !path)) { pv_set_error("null pointer"); return PV_EINVAL; }
     if (row_stride < 0 || draft_row_stride < 0) { pv_set_error("negative row stride"); return PV_EINVAL; }
     if (!temperatures && !(temperature >= 0.f)) { pv_set_error("temperature %g is not 0 or more", (double)temperature); return PV_EINVAL; }
     const int64_t size = dtype == PV_F32 ? 4 : 2;
@@ -810,7 +811,13 @@ extern "C" int pv_verify_drafts(const int32_t *row_start, int32_t n_seq, const v
     a.row_start = row_start; a.tokens = tokens; a.parent = parent; a.u = u; a.u64 = u_is_double != 0; a.probs = draft_probs; a.probs_row = draft_row_stride;
     a.temperature = temperatures; a.hot = temperature; a.accepted = accepted; a.next = next_token; a.path = path; a.out_probs = probs;
     hipStream_t s = (hipStream_t)hip_stream;
-    if (rows == 0) { k_draft_none<<<(unsigned)((n_seq + 255) / 256), 256, 0, s>>>(n_seq, accepted, next_token); PV_HIP(hipGetLastError()); return PV_OK; }
+    if (rows == 0 || n_seq == 0) {
+        k_draft_none<<<(unsigned)(((rows > n_seq ? (int)rows : n_seq) + 255) / 256), 256, 0, s>>>(n_seq, accepted, next_token, (int)rows, path, probs);
+        const hipError_t err = hipGetLastError();
+        if (n_seq == 0 && err == hipErrorNoDevice) return PV_OK;         // (a call without sequences has nothing to verify: where there is no device there is nothing to write to either)
+        PV_HIP(err);
+        return PV_OK;
+    }
     a.part = (dv_part *)workspace; a.rest = (double2 *)(a.part + (size_t)rows * p.left); a.walk = (int2 *)(a.rest + (size_t)n_seq * p.left);
     return dtype == PV_F32 ? launch<float>(a, p.e, s) : dtype == PV_BF16 ? launch<__bf16>(a, p.e, s) : launch<_Float16>(a, p.e, s);
 }
