@@ -14,12 +14,14 @@
     pool.keep(seqs, got.path, got.accepted)                           # the accepted path behind the prefix
 
 Argument marshalling only; work is enqueued on `stream` (default: the current stream of the pool's device) and not waited for.  A tensor made on another stream
-is the caller's to order, as everywhere in torch.  There are no gradients: tensors that require one are refused, unless gradients are switched off (torch.no_grad()).
+is the caller's to order, as everywhere in torch.  There are no gradients: tensors that require one are refused, unless gradients are switched off (torch.no_grad()), and so are tensors that
+carry a tangent of forward mode.
 """
 import ctypes
 import math
 
 import torch
+from torch.autograd import forward_ad
 
 from .binding import DraftVerdict, PVError, TokenLogprobs, _check, lib, pv_kv16_pool, pv_kv8_pool, pv_kv8_seqs, pv_rotary
 
@@ -53,10 +55,17 @@ class _Elsewhere:
         self.device.__exit__(*a)
 
 
+def _asks(t):
+    """Whether a tensor may ask for a derivative (the level of forward mode, -1 outside of it, is looked at first: asking a tensor for its tangent takes some 0.3 us)."""
+    return t.requires_grad or forward_ad._current_level >= 0
+
+
 def _no_gradient(where, name, t):
-    """There is no backward pass: a result without a history where torch would give one would be a gradient lost in silence."""
+    """There is no backward pass, and no forward-mode one: a result without a history or a tangent where torch would give one would be a gradient lost in silence."""
     if t.requires_grad and torch.is_grad_enabled():
         _refuse(where, f"{name} requires a gradient, and this operator has none: call it under torch.no_grad(), or with {name}.detach()")
+    if forward_ad.unpack_dual(t).tangent is not None:
+        _refuse(where, f"{name} carries a forward-mode gradient, and this operator has none: call it with the primal of {name}")
 
 
 def _elsewhere(index, stream):
@@ -123,7 +132,7 @@ class KV8Pool:
             _refuse(where, f"{name} must be [rows, {heads}, {self.head_dim}] of {tuple(dtypes)}, got {tuple(shape)} of {t.dtype}")
         if stride[2] != 1:
             _refuse(where, f"{name}: the features of a head must lie next to each other")
-        if t.requires_grad:
+        if _asks(t):
             _no_gradient(where, name, t)
         return t.data_ptr(), stride[0], stride[1]
 
@@ -203,7 +212,7 @@ class KV8Pool:
         if lse is not None:
             if not (isinstance(lse, torch.Tensor) and lse.device == self.device and lse.dtype == torch.float32 and lse.shape == (n, heads) and lse.is_contiguous()):
                 _refuse(where, f"lse must be a contiguous float32 tensor [{n}, {heads}] on {self.device}")
-            if lse.requires_grad:
+            if _asks(lse):
                 _no_gradient(where, "lse", lse)
         elif return_lse:
             lse = q.new_empty((n, heads), dtype=torch.float32)
@@ -224,7 +233,7 @@ def token_logprobs(logits, tokens=None, top=0, stream=None):
     where = "token_logprobs"
     if not (isinstance(logits, torch.Tensor) and logits.is_cuda and logits.dim() == 2 and logits.dtype in _DTYPES):
         _refuse(where, f"logits must be [rows, vocab] of {tuple(_DTYPES)} on the GPU")
-    if logits.requires_grad:
+    if _asks(logits):
         _no_gradient(where, "logits", logits)
     index = logits.device.index
     if _elsewhere(index, stream):
@@ -371,7 +380,7 @@ def _heads(self, t, where, name, heads, dtypes):
         _refuse(where, f"{name} must be [rows, {'heads' if heads is None else heads}, {self.head_dim}] of {tuple(dtypes)}, got {tuple(shape)} of {t.dtype}")
     if stride[2] != 1:
         _refuse(where, f"{name}: the features of a head must lie next to each other")
-    if t.requires_grad:
+    if _asks(t):
         _no_gradient(where, name, t)
     return t.data_ptr(), stride[0], stride[1]
 
@@ -399,6 +408,7 @@ class KV16Pool:
             _refuse(where, f"pages must be a contiguous {dtype} tensor {shape} on the GPU")
         if self.pages.requires_grad:
             _refuse(where, "pages require a gradient, and a cache has none")
+        _no_gradient(where, "pages", self.pages)
         self.device = self.pages.device
         self._index = self.device.index
         self._arg = pv_kv16_pool(self.pages.data_ptr(), n_pages, n_kv_heads, head_dim, page_tokens, _HALF[dtype])
@@ -485,7 +495,7 @@ class KV16Pool:
         if lse is not None:
             if not (isinstance(lse, torch.Tensor) and lse.device == self.device and lse.dtype == torch.float32 and lse.shape == (n, heads) and lse.is_contiguous()):
                 _refuse(where, f"lse must be a contiguous float32 tensor [{n}, {heads}] on {self.device}")
-            if lse.requires_grad:
+            if _asks(lse):
                 _no_gradient(where, "lse", lse)
         elif return_lse:
             lse = q.new_empty((n, heads), dtype=torch.float32)
@@ -525,7 +535,7 @@ def verify_drafts(row_start, logits, tokens, u, draft_probs=None, parent=None, t
     where = "verify_drafts"
     if not (isinstance(logits, torch.Tensor) and logits.is_cuda and logits.dim() == 2 and logits.dtype in _DTYPES):
         _refuse(where, f"logits must be [rows, vocab] of {tuple(_DTYPES)} on the GPU")
-    if logits.requires_grad:
+    if _asks(logits):
         _no_gradient(where, "logits", logits)
     device = logits.device
     index = device.index
@@ -555,19 +565,19 @@ def verify_drafts(row_start, logits, tokens, u, draft_probs=None, parent=None, t
     if draft_probs is not None:
         if not (isinstance(draft_probs, torch.Tensor) and draft_probs.device == device and draft_probs.dtype == torch.float32 and draft_probs.shape == (rows, vocab)) or (draft_probs.stride(1) != 1 and vocab > 1 and rows > 0):
             _refuse(where, f"draft_probs must be a float32 tensor [{rows}, {vocab}] on {device}, a row's numbers next to each other")
-        if draft_probs.requires_grad:
+        if _asks(draft_probs):
             _no_gradient(where, "draft_probs", draft_probs)
         qp, qr = draft_probs.data_ptr(), draft_probs.stride(0)
     hot, hp = 0.0, None
     if isinstance(temperature, torch.Tensor):
         if not (temperature.device == device and temperature.dtype == torch.float32 and temperature.shape == (n,) and temperature.is_contiguous()):
             _refuse(where, f"temperature must be a number or a contiguous float32 tensor [{n}] on {device}")
-        if temperature.requires_grad:
+        if _asks(temperature):
             _no_gradient(where, "temperature", temperature)
         hp = temperature.data_ptr()
     else:
         hot = float(temperature)
-    if u.requires_grad:
+    if _asks(u):
         _no_gradient(where, "u", u)
     L, key = lib(), (rows, n, vocab)
     need = _drafts_need.get(key)
