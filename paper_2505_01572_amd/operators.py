@@ -300,6 +300,9 @@ class Rotary:
         else:
             if scaling is not None or not (isinstance(turns, torch.Tensor) and turns.is_cuda and turns.dtype == torch.float64 and turns.shape == (n // 2,) and turns.is_contiguous()):
                 _refuse(where, f"turns must be a contiguous float64 tensor [{n // 2}] on the GPU, without a scaling")
+            if turns.requires_grad:
+                _refuse(where, "turns require a gradient, and a rotation has none")
+            _no_gradient(where, "turns", turns)
             self.turns = turns
         if not self.turns.is_cuda:
             _refuse(where, "the device must be a GPU")

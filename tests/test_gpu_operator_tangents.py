@@ -50,3 +50,16 @@ def test_inside_a_jvp(pv):  # noqa: F811
     q, seqs = torch.randn(3, 4, 64, device="cuda").bfloat16(), s.seqs()
     with pytest.raises(pv.PVError, match="gradient"):
         torch.func.jvp(lambda y: s.pool.attention(seqs, y), (q,), (torch.ones_like(q),))
+
+
+def test_frequencies_that_require_a_gradient(pv):  # noqa: F811
+    """A Rotary keeps them: refused when it is made, whatever the mode."""
+    turns = torch.rand(32, dtype=torch.float64, device="cuda")
+    pv.Rotary(64, turns=turns)
+    with forward_ad.dual_level(), pytest.raises(pv.PVError, match="gradient"):
+        pv.Rotary(64, turns=forward_ad.make_dual(turns, turns))
+    turns.requires_grad_()
+    with pytest.raises(pv.PVError, match="gradient"):
+        pv.Rotary(64, turns=turns)
+    with torch.no_grad(), pytest.raises(pv.PVError, match="gradient"):
+        pv.Rotary(64, turns=turns)
