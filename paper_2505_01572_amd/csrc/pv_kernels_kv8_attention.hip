@@ -61,7 +61,7 @@ template <int HD, int TR> __device__ inline bool kv8_unit(const kv8_seqs &q, con
         return true;
     }
     for (int k = 0; k < q.n_seq; k += 64) {
-        const int i = min(k + lane, q.n_seq - 1), r0 = q.row_start[i], r1 = q.row_start[i + 1], len = q.prefix_len[i], r = min(r1, q.n_rows) - r0;
+        const int i = min(k + lane, q.n_seq - 1), r0 = q.row_start[i], r1 = q.row_start[i + 1], len = q.prefix_len[i], r = min(max(r1, 0), q.n_rows) - max(r0, 0);
         const int rows = k + lane >= q.n_seq || r0 < 0 || r < 0 || len < 0 ? 0 : r;
         const int mine = (rows * group + TR - 1) / TR, upto = kv8_sums(mine);
         const uint64_t past = __ballot(upto > unit);

@@ -69,7 +69,7 @@ template <int HD> __device__ inline kv8_seq kv8_seq_in(const kv8_seqs &q, const 
     }
     r.table = q.page_table + (size_t)s * q.table_pages; r.table_pages = q.table_pages;
     r.row0 = q.row_start[s];
-    r.rows = min(q.row_start[s + 1], q.n_rows) - r.row0;
+    r.rows = min(max(q.row_start[s + 1], 0), q.n_rows) - max(r.row0, 0);      // (no difference that wraps, whatever the table holds)
     r.len = q.prefix_len[s];
     if (r.row0 < 0 || r.rows < 0 || r.len < 0) r.rows = 0;
     return r;
