@@ -19,9 +19,6 @@ struct kv16_attn_args {
     uint32_t q_and, q_xor;                  // what q passes through: its sign is the scale's
 };
 
-// A pointer that came out of memory is one to global memory: loads through it are then no flat ones, for which every wait for LDS would wait too
-template <typename T> __device__ inline T *kv16_global(T *p) { return (T *)(__attribute__((address_space(1))) T *)(uintptr_t)p; }
-
 // A lane's value added to those of the lanes before it
 __device__ inline int kv16_sums(int v)
 {

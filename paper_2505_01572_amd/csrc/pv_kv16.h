@@ -60,37 +60,11 @@ __device__ inline int kv16_page(const kv16_seq &s, int n_pages, int logical)
     return p >= 0 && p < n_pages ? p : -1;
 }
 
-// Eight consecutive numbers in 32 bits, and back
+// Two numbers of a 16-bit type
 typedef __attribute__((ext_vector_type(2))) _Float16 kv16_h2;
-template <typename T> __device__ inline void kv16_load8(const char *p, float v[8]);
-template <> __device__ inline void kv16_load8<float>(const char *p, float v[8])
-{
-    const float4 a = ((const float4 *)p)[0], b = ((const float4 *)p)[1];
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-}
-template <> __device__ inline void kv16_load8<__bf16>(const char *p, float v[8])
-{
-    const uint4 a = *(const uint4 *)p;
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-}
-template <> __device__ inline void kv16_load8<_Float16>(const char *p, float v[8])
-{
-    const uint4 a = *(const uint4 *)p;
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { const kv16_h2 h = __builtin_bit_cast(kv16_h2, w[i]); v[2 * i] = (float)h.x; v[2 * i + 1] = (float)h.y; }
-}
 template <typename S> __device__ inline uint32_t kv16_two(float a, float b);
 template <> __device__ inline uint32_t kv16_two<__bf16>(float a, float b) { return pack_bf16(a, b); }
 template <> __device__ inline uint32_t kv16_two<_Float16>(float a, float b) { const kv16_h2 h = {(_Float16)a, (_Float16)b}; return __builtin_bit_cast(uint32_t, h); }
-template <typename S> __device__ inline uint4 kv16_pack8(const float v[8]) { return make_uint4(kv16_two<S>(v[0], v[1]), kv16_two<S>(v[2], v[3]), kv16_two<S>(v[4], v[5]), kv16_two<S>(v[6], v[7])); }
-template <typename T> __device__ inline void kv16_store8(char *p, const float v[8])
-{
-    if constexpr (__is_same(T, float)) { ((float4 *)p)[0] = make_float4(v[0], v[1], v[2], v[3]); ((float4 *)p)[1] = make_float4(v[4], v[5], v[6], v[7]); }
-    else *(uint4 *)p = kv16_pack8<T>(v);
-}
 
 // ---- host side ----
 int pv_kv16_check_pool(const pv_kv16_pool *p);

@@ -351,8 +351,6 @@ def _turns(n, base, scaling):
             _refuse(where, f"the numbers of a scaling must be above 0, got {scaling}")
         s = scaling["factor"]
         if kind == "base":
-            if n < 4:
-                _refuse(where, "a scaled base needs two pairs")
             base = base * s ** (n / (n - 2))
     freq = [base ** (-2.0 * i / n) for i in range(n // 2)]
     if kind == "linear":
