@@ -396,7 +396,8 @@ int pv_kv16_bytes(const pv_kv16_pool *pool, size_t *bytes);
 
 /* Write keys and values: row i of sequence s (pv_kv8_seqs, whose rules for rows of no sequence and pages that do not exist hold here as well) becomes token prefix_len[s] + i of it, rounded to the pool's type.  With a rotary (else NULL),
  * keys are rotated on the way by positions [n_rows] (int32; NULL: the tokens' own), and, where q is not NULL, the queries of the same rows, into q_out (which may be q; rows of no sequence are left as they are).  k, v, q, q_out:
- * addressed as in pv_rotate, of type dtype (pv_dtype).  A page must not be the place of rows twice in a call.  n_rows <= 2^20 - 16. */
+ * addressed as in pv_rotate, of type dtype (pv_dtype).  (q_out too: queries of another type than the pool's have to be converted before pv_kv16_attention takes them.)  A page must not be the place of rows twice in a call.
+ * n_rows <= 2^20 - 16. */
 int pv_kv16_append(const pv_kv16_pool *pool, const pv_kv8_seqs *seqs, const void *k, int64_t k_row_stride, int64_t k_head_stride, const void *v, int64_t v_row_stride, int64_t v_head_stride,
                    const pv_rotary *rotary, const int32_t *positions, const void *q, int64_t q_row_stride, int64_t q_head_stride, int32_t n_q_heads,
                    void *q_out, int64_t q_out_row_stride, int64_t q_out_head_stride, int32_t dtype, void *hip_stream);
@@ -405,7 +406,7 @@ int pv_kv16_append(const pv_kv16_pool *pool, const pv_kv8_seqs *seqs, const void
  * tokens 0 .. prefix_len[s] + i.  Else (a draft tree) mask [n_rows][mask_words]: the row sees all tokens before prefix_len[s], and token prefix_len[s] + t if bit t % 64 of its word t / 64 is set, t less than 64 * mask_words and than the
  * number of rows that s has in the call.  A row that sees no token: zeros, and -infinity in lse (NULL, or float [n_rows][n_q_heads]).  What a row does not see has no influence on it, NaN and infinities included; a
  * value that it sees and that is infinite or NaN makes its output infinite or NaN.  Weights meet the values as pairs of numbers of the pool's type (16 significant bits in bf16, 22 in f16);
- * all sums have 32 bits.
+ * all sums have 32 bits, relative to the row's largest weight or one up to 2^8 less: an output is sure to be finite where the largest value that the row sees, times the tokens, stays below 2^120.
  * n_q_heads is a multiple of n_kv_heads, (n_rows + n_seq) * n_q_heads <= 2^24, table_pages * page_tokens <= 2^30, mask_words <= 2^18, scale is finite.  workspace: at least pv_kv16_attention_bytes,
  * 16-byte aligned, for this call alone until it has run. */
 int pv_kv16_attention_bytes(const pv_kv16_pool *pool, const pv_kv8_seqs *seqs, int32_t n_q_heads, size_t *bytes);

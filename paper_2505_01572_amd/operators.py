@@ -422,7 +422,8 @@ class KV16Pool:
 
     def append(self, seqs, k, v, rotary=None, positions=None, q=None, q_out=None, stream=None):
         """Write k, v [rows, n_kv_heads, head_dim] (float32, bfloat16 or float16) into the pages of their sequences.  rotary: a Rotary that turns the keys on the way, by positions (int32 [rows]) or the tokens' own.  q [rows, heads,
-        head_dim]: queries of the same rows, turned alike and returned (q_out: where to, q itself if wanted; rows of no sequence are left as they are)."""
+        head_dim]: queries of the same rows and of k's type, turned alike and returned as such (q_out: where to, q itself if wanted; rows of no sequence are left as they are); attention() takes the pool's type, so
+        that queries of another one have to be converted first."""
         where = "KV16Pool.append"
         if _elsewhere(self._index, stream):
             with _Elsewhere(self.device, stream):
