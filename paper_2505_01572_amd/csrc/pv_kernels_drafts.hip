@@ -229,19 +229,22 @@ k_draft_rows(const dv_args a)
             for (int i = 0; i < E; ++i) { const double w = dv_power(dv_get<T>(x, i), cold, most); if (i & 1) odd += w; else sum += w; }
             sum = dv_over_wave((sum + odd) + dv_power(x0, cold, most));
         } else {
-            // (x - top as it is, then the factor: a factor's product with top would be off by as much for all)
-            const float c = (float)fmin(cold, 1e30);
+            // (x - top as it is, then the factor: a factor's product with top would be off by as much for all, and so would its own rounding be: it is a number of 32 bits just below it, and what is left of it, above 0 as well so
+            // that -infinity stays what it is.)
+            const double most = fmin(cold, 1e30);
+            const float c = fmaxf((float)(most * (1.0 - 0x1p-23)), 0x1p-149f), c2 = fmaxf((float)(most - (double)c), 0x1p-149f);
+            auto exponent = [&](float v) { const float d = v - top; return fmaf(d, c, d * c2); };
             float even = 0.f, odd = 0.f;
 #pragma unroll
-            for (int i = 0; i < E; ++i) { const float w = __builtin_amdgcn_exp2f((dv_get<T>(x, i) - top) * c); if (i & 1) odd += w; else even += w; }
-            if (__any(!(even + odd < INFINITY))) {            // NaN among them (or -infinity at an infinite T): once more, with care
+            for (int i = 0; i < E; ++i) { const float w = __builtin_amdgcn_exp2f(exponent(dv_get<T>(x, i))); if (i & 1) odd += w; else even += w; }
+            if (__any(!(even + odd < INFINITY))) {            // NaN among them: once more, with care
                 even = odd = 0.f;
 #pragma unroll
                 for (int d = 0; d < D; ++d) if (sizeof(T) == 2) asm volatile("" : "+v"(x[d]));
 #pragma unroll
-                for (int i = 0; i < E; ++i) { even += __builtin_amdgcn_exp2f(fmaxf((dv_get<T>(x, i) - top) * c, -256.f)); asm volatile("" : "+v"(even)); }      // (2^-256 is 0; of NaN and a number the number; one after the other: no registers for more)
+                for (int i = 0; i < E; ++i) { even += __builtin_amdgcn_exp2f(fmaxf(exponent(dv_get<T>(x, i)), -256.f)); asm volatile("" : "+v"(even)); }      // (2^-256 is 0; of NaN and a number the number; one after the other: no registers for more)
             }
-            even += __builtin_amdgcn_exp2f(fmaxf((x0 - top) * c, -256.f));
+            even += __builtin_amdgcn_exp2f(fmaxf(exponent(x0), -256.f));
             sum = dv_over_wave((double)even + (double)odd);
         }
         if (top == -INFINITY) sum = 0.0;
