@@ -9,12 +9,12 @@
 // under p - q, where p's own sum moves all of them).  Whether a draft is taken turns on one border: without a drafter's probabilities rows are summed with exponentials of 32 bits, off by some 10^-7, which
 // decides one draft of a chain in 10^7 otherwise and takes a third of the time.  (What remains of a row behind refused children of a tree may be less than that: there the walk looks twice.)
 //   rows   a workgroup takes a segment of a row: its maximum and the sum of its exponentials.  Only of rows that a draft is behind: p of a tree's leaves, half of its nodes, and of a chain's last row is asked for only if
-//          the draw is there (16 trees of up to 48 nodes, 128256 logits of bf16, all four launches: 50.8 us with all rows, 34.3 so)
+//          the draw is there (16 trees of up to 48 nodes, 128256 logits of bf16, all four launches: 36.9 us; with all rows 16 more)
 //   walk   a tree: a workgroup a sequence joins the segments of the nodes' rows and walks along
 //   rest   a workgroup a segment of the row that the draw is behind (a chain: found anew by each): what is left to draw from, summed
 //   pick   a workgroup a sequence finds the segment that the draw falls in, and in that the token
-// Of the 34.3 us the rows take 16.5 (44 MB of the 143 that the logits have; most workgroups find that they have nothing to do, which with all tables asked for at once took no less), walk 5.5, rest 7.4, pick 7.2: trips to memory, one
-// behind the other.  The draw by the last workgroup of the launch before it, which saves a launch, was slower: 25 -> 31 us (64 chains), 50 -> 58 (16 trees).
+// In a trace, each by itself, the rows take 17.4 us (44 MB of the 143 that the logits have; most workgroups find that they have nothing to do, which with all tables asked for at once took no less), walk 7.0, rest 7.4, pick 7.0: trips
+// to memory, one behind the other (in a graph a launch's beginning lies beside the end of the one before it).  The draw by the last workgroup of the launch before it, which saves a launch, was slower: 25 -> 31 us (64 chains), 50 -> 58 (16 trees).
 #include "pv_matrix_common.h"
 
 struct __align__(16) dv_part { double sum; float top; int first; };       // of a segment: sum of e^((x - top) / T), largest logit, its lowest id (T = 0: no sum)
@@ -724,7 +724,7 @@ k_draft_pick(const dv_args a)
 
 // ------------------------------- host side ----------------------------------------
 
-// Tokens a segment of a row: 4096, or, where there are rows enough for the chip, 8192 (64-bit sums), 14336 (what registers hold at seven waves a SIMD: 16 trees 34.3 us; 12288 at eight 34.9; 16384 at six 34.5) or (f32) 8192.  Whether there is a drafter is not known where the workspace is measured: its size is that of 4096.
+// Tokens a segment of a row: 4096, or, where there are rows enough for the chip, 8192 (64-bit sums), 14336 (what registers hold at seven waves a SIMD; of 16 trees' 35 us 12288 at eight took 0.6 more, 16384 at six 0.2) or (f32) 8192.  Whether there is a drafter is not known where the workspace is measured: its size is that of 4096.
 struct dv_plan { int e, segs, left; };
 static dv_plan plan(int64_t rows, int vocab, bool wide, int dtype)
 {

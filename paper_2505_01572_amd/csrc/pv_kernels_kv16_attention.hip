@@ -442,8 +442,9 @@ k_kv16_attn(const kv16_attn_args a)
 // Many rows: a workgroup is a kv head, 64 RT packed rows of a sequence (16 RT a wave), a chunk of its keys.  64 keys at a time go through LDS, copied straight from memory, each wave a group of 16: values a step ahead,
 // keys two, because the products with the next step's keys are made while this one's scores become weights: those keep the vector ALU busy (an exponential takes four turns, what makes a weight a pair two and a half), the products the
 // matrix cores.  A weight is a pair of numbers of the cache's type, as with few rows: so a row's result has the same bits behind it whatever tile it comes to lie in.  One number a weight, 8 significant bits in bf16, adds as
-// much to an output's error as its own rounding does (relative to 64 bits 2.3e-3 for 1.7e-3, in f16 2.9e-4 for 2.1e-4) and takes three quarters of the time (341 us for the 454 below).
-// Two prompts of up to 2048 rows of 32 heads of 128 over up to 6100 keys and themselves, bf16: 454 us, 335 GFLOP asked for, 502 on the matrix cores, whose 1107 TFLOP/s are 89 % of what a library product of 8192^3 reaches (1242).
+// much to an output's error as its own rounding does (relative to 64 bits 2.3e-3 for 1.7e-3, in f16 2.9e-4 for 2.1e-4) and takes three quarters of the time (341 us for the 445 below).
+// Two prompts of up to 2048 rows of 32 heads of 128 over up to 6100 keys and themselves, bf16: 445 us, 335 GFLOP asked for, 502 on the matrix cores, whose 1128 TFLOP/s are 91 % of what a library product of 8192^3 reaches (1242);
+// they are busy 49 % of the cycles, the vector ALU 52 %.
 // Values as whole 16 bytes, sorted into operands by moves or by exchanges of registers: some 3 % more.
 template <int HD>
 struct kv16_wide {
