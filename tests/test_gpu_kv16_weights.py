@@ -42,3 +42,22 @@ def test_values_that_cancel(pv, case, dtype, hd, masked):  # noqa: F811
     bound = torch.finfo(s.dtype).eps / 2 * np.abs(want) + (2.0 ** -14 if dtype == "bf16" else 2.0 ** -16) * mag
     worst = (np.abs(out - want) / bound).max()
     assert worst <= 1, worst
+
+
+@pytest.mark.parametrize("case", list(CASES.values()), ids=list(CASES))
+@pytest.mark.parametrize("hd", [64, 128])
+def test_values_up_to_where_outputs_are_sure_to_be_finite(pv, case, hd):  # noqa: F811
+    """All of one sign and nearly 2^120 / tokens, scores that rise by less than results are rescaled at: sums relative to a weight 2^8 below the largest."""
+    s = Far(pv, case, hd, "bf16")
+    total = [p + w for p, w in zip(s.prefix, s.rows)]
+    n = sum(total)
+    place = np.concatenate([np.arange(m) / max(m, 2) for m in total])
+    k, v = torch.zeros(n, s.heads, hd), torch.from_numpy(s.r.uniform(0.5, 0.99, (n, s.heads, hd)) * 2.0 ** 120 / max(total)).float()
+    k[:, :, 0] = torch.from_numpy(np.floor(place * 5.5 * 16) / 16).float()[:, None]
+    s.put(np.concatenate([[0], np.cumsum(total)]).astype(np.int32), [0] * len(total), k.to(s.dtype), v.to(s.dtype))
+    q = torch.zeros(s.n, s.q_heads, hd)
+    q[..., 0] = 1.0
+    q = q.to(s.dtype)
+    out = s.pool.attention(s.seqs(), q.cuda(), scale=1.0).double().cpu().numpy()
+    want, _, mag = s.ref.attention(s.start, s.prefix, s.tables, q.double().numpy(), 1.0)
+    assert np.isfinite(out).all() and (np.abs(out - want) <= torch.finfo(s.dtype).eps / 2 * np.abs(want) + 2.0 ** -14 * mag).all()
